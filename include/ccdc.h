@@ -58,7 +58,8 @@ extern "C" {
 
 typedef struct ccdc_plan_s ccdc_plan_t;     /* opaque; created and destroyed by the library */
 
-typedef enum { CCDC_I32 = 0, CCDC_F32 = 1 } ccdc_dtype_t;
+/* Element types.  Plans take the first two (32-bit words); the block operators (below) the floating ones. */
+typedef enum { CCDC_I32 = 0, CCDC_F32 = 1, CCDC_BF16 = 2, CCDC_F16 = 3 } ccdc_dtype_t;
 
 typedef enum {
     CCDC_OK = 0,
@@ -467,6 +468,99 @@ int ccdc_peer_buffer_copy(void *dst, const void *src, size_t bytes, void *stream
 size_t ccdc_static_scratch_bytes(void);
 int ccdc_decode_reduce_static(ccdc_plan_t *plan, const void *const *part, const void *coded, void *out,
                               void *stream);
+
+/* -------------------------------------------------------- block operators
+ * The Map of a language model's job: a file is a batch of token rows, and the
+ * intermediate values are parameter gradients.  These calls compute a gated
+ * feed-forward block with the norms, gate, dropout and residual around it,
+ * forward and backward.  Every sum has one order and no atomics are used, so the
+ * r replicas of a file are bit-identical at the nodes that map it (same shapes,
+ * strides, alignment and GPU model).
+ *
+ * Conventions (besides those at the top): M rows (tokens); matrices are
+ * row-major with a row stride in elements (ld..., >= the row's length; the
+ * elements of a row are contiguous); dtype is CCDC_F32, CCDC_BF16 or CCDC_F16
+ * for all tensors of a call, sums are binary32, results are rounded once.
+ * Pointers need only their type's alignment; rows whose addresses are multiples
+ * of 16 bytes are read faster.  grad_dtype: type of the parameters' gradients,
+ * dtype or CCDC_F32 (then a gradient can be written straight into a partition).
+ * M = 0 is valid: nothing is computed, parameter gradients are zero.
+ * Output tensors must not overlap inputs unless a call says so.  The calls
+ * enqueue kernels only (no allocation, no synchronisation) and can be captured
+ * in a CUDA graph. */
+
+/* Dropout: y[m][n] = x[m][n] * 65536/(65536-c) where the element is kept, else 0
+ * (also where x is not finite); c = round(65536 p).  Element e = offset +
+ * m*cols + n takes 16 bits (the e mod 8-th of the 128, least significant first)
+ * of Philox 4x32-10 with the seed as key and e / 8 as counter, and is kept
+ * where they are at least c.  The mask depends on (seed, e) alone and is never
+ * stored: the backward pass is the same call on the gradient, and a replica
+ * draws the same mask at every node.  0 <= p <= 1; y may be x itself (same
+ * stride).  CCDC_ESIZE beyond 2^46 elements. */
+int ccdc_dropout(long long rows, long long cols, int dtype, const void *x, long long ldx, void *y, long long ldy,
+                 double p, unsigned long long seed, unsigned long long offset, void *stream);
+
+/* Norms before and after a block, with its gate, dropout and residual scale:
+ *     n   = unit(y) * w_post            (w_post NULL: n = y, no norm)
+ *     out = alpha * x + drop(gate * n)  (gate NULL: 1; p = 0: no dropout)
+ *     z   = unit(out) * w_pre           (w_pre and z NULL: not computed)
+ * unit: CCDC_NORM_RMS v / sqrt(mean v^2 + eps), CCDC_NORM_LAYER the same after
+ * the row's mean is subtracted.  x is the residual stream, y what the block
+ * returned, z what the next block reads.  y NULL: out = alpha * x, the norm
+ * before the first block.  out may be NULL if z is wanted alone.  z is computed
+ * from `out` before it is rounded.
+ * gate: [max(1, ceil(M / rows_per_gate))][D] contiguous, row m uses gate row
+ * m / rows_per_gate: one gate per channel (rows_per_gate = M), per sample, or
+ * per token (1).  Dropout as ccdc_dropout, element offset + m*D + d.
+ * out may be x or y itself, z may be y itself (same stride).
+ * stats: NULL, or [M][4] binary32 (16-byte aligned) for the backward pass.
+ *
+ * Backward: dout, dz = gradients of out and z (either may be NULL: zero; dz as
+ * w_pre), x, y, stats as in the forward call.  Writes dx, dy (each may be NULL),
+ * dw_post[D], dw_pre[D] and dgate (shape of gate) in grad_dtype (each may be
+ * NULL).  workspace: ccdc_residual_norm_workspace_bytes for the current device,
+ * 16-byte aligned.
+ * D <= 32768 (CCDC_ESIZE). */
+typedef enum { CCDC_NORM_RMS = 0, CCDC_NORM_LAYER = 1 } ccdc_norm_t;
+int ccdc_residual_norm_forward(long long M, long long D, int dtype, int kind, float eps, const void *x, long long ldx,
+                               const void *y, long long ldy, const void *w_post, const void *w_pre, const void *gate,
+                               long long rows_per_gate, float alpha, double p, unsigned long long seed,
+                               unsigned long long offset, void *out, long long ldo, void *z, long long ldz,
+                               void *stats, void *stream);
+size_t ccdc_residual_norm_workspace_bytes(long long M, long long D);
+int ccdc_residual_norm_backward(long long M, long long D, int dtype, int grad_dtype, int kind, const void *dout,
+                                long long lddout, const void *dz, long long lddz, const void *x, long long ldx,
+                                const void *y, long long ldy, const void *stats, const void *w_post,
+                                const void *w_pre, const void *gate, long long rows_per_gate, float alpha, double p,
+                                unsigned long long seed, unsigned long long offset, void *dx, long long lddx, void *dy,
+                                long long lddy, void *dw_post, void *dw_pre, void *dgate, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* Gated feed-forward block:
+ *     h = x w_gate^T,  u = x w_up^T,  a = act(h) * u,  y = a w_down^T
+ * x [M][D], w_gate and w_up [F][D] (row stride ldw), w_down [D][F] (ldd), y [M][D].
+ * saved: NULL, or ccdc_ffn_saved_bytes for the backward pass (h, u and a).
+ * Backward: from dy, x, the weights and saved,
+ *     da = dy w_down,  dh = da * u * act'(h),  du = da * act(h),
+ *     dx = dh w_gate + du w_up,  dw_gate = dh^T x,  dw_up = du^T x,  dw_down = dy^T a;
+ * dx [M][D], dw_gate and dw_up [F][D], dw_down [D][F] contiguous, each may be NULL.
+ * a, dh and du, which enter further products, are kept in the tensors' type; h
+ * and u in binary32 (rounding them too would take the gradients' error from 1.4
+ * to 1.8 times that of their own rounding).
+ * workspace: ccdc_ffn_workspace_bytes(..., backward, aligned), 16-byte aligned;
+ * aligned != 0 promises that every pointer and row stride is a multiple of 16
+ * bytes (D and F too), which needs less.  workspace_bytes smaller than the call
+ * needs gives CCDC_ESIZE.  saved must be 16-byte aligned. */
+typedef enum { CCDC_ACT_SILU = 0, CCDC_ACT_GELU = 1, CCDC_ACT_GELU_TANH = 2, CCDC_ACT_RELU = 3 } ccdc_act_t;
+size_t ccdc_ffn_saved_bytes(long long M, long long F, int dtype);
+size_t ccdc_ffn_workspace_bytes(long long M, long long D, long long F, int dtype, int backward, int aligned);
+int ccdc_ffn_forward(long long M, long long D, long long F, int dtype, int act, const void *x, long long ldx,
+                     const void *w_gate, const void *w_up, long long ldw, const void *w_down, long long ldd, void *y,
+                     long long ldy, void *saved, void *workspace, size_t workspace_bytes, void *stream);
+int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad_dtype, int act, const void *dy,
+                      long long lddy, const void *x, long long ldx, const void *w_gate, const void *w_up, long long ldw,
+                      const void *w_down, long long ldd, const void *saved, void *dx, long long lddx, void *dw_gate,
+                      void *dw_up, void *dw_down, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------- diagnostics */
 const char *ccdc_strerror(int status);

@@ -16,11 +16,14 @@ from pathlib import Path
 _LIB_PATH = Path(__file__).resolve().parent / "libccdc.so"
 _lib = None
 
-I32, F32 = 0, 1
+I32, F32, BF16, F16 = 0, 1, 2, 3
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+NORMS = {"rms": 0, "layer": 1}
 OK, EINVAL, ENOMEM, ECUDA, ESIZE, ESTATE = 0, -1, -2, -3, -4, -5
 MAX_K = 32
 
 _P, _I, _LL, _SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t
+_ULL, _FL, _DB = ctypes.c_ulonglong, ctypes.c_float, ctypes.c_double
 _PP = ctypes.POINTER(ctypes.c_void_p)
 
 # name -> (restype, argtypes); mirrors include/ccdc.h
@@ -88,6 +91,17 @@ SIGNATURES = {
     "ccdc_peer_buffer_close": (_I, [_P]),
     "ccdc_peer_buffer_destroy": (_I, [_P]),
     "ccdc_peer_buffer_copy": (_I, [_P, _P, _SZ, _P]),
+    "ccdc_dropout": (_I, [_LL, _LL, _I, _P, _LL, _P, _LL, _DB, _ULL, _ULL, _P]),
+    "ccdc_residual_norm_forward": (_I, [_LL, _LL, _I, _I, _FL, _P, _LL, _P, _LL, _P, _P, _P, _LL, _FL, _DB, _ULL, _ULL,
+                                        _P, _LL, _P, _LL, _P, _P]),
+    "ccdc_residual_norm_workspace_bytes": (_SZ, [_LL, _LL]),
+    "ccdc_residual_norm_backward": (_I, [_LL, _LL, _I, _I, _I, _P, _LL, _P, _LL, _P, _LL, _P, _LL, _P, _P, _P, _P, _LL,
+                                         _FL, _DB, _ULL, _ULL, _P, _LL, _P, _LL, _P, _P, _P, _P, _SZ, _P]),
+    "ccdc_ffn_saved_bytes": (_SZ, [_LL, _LL, _I]),
+    "ccdc_ffn_workspace_bytes": (_SZ, [_LL, _LL, _LL, _I, _I, _I]),
+    "ccdc_ffn_forward": (_I, [_LL, _LL, _LL, _I, _I, _P, _LL, _P, _P, _LL, _P, _LL, _P, _LL, _P, _P, _SZ, _P]),
+    "ccdc_ffn_backward": (_I, [_LL, _LL, _LL, _I, _I, _I, _P, _LL, _P, _LL, _P, _P, _LL, _P, _LL, _P, _P, _LL, _P, _P,
+                               _P, _P, _SZ, _P]),
     "ccdc_strerror": (ctypes.c_char_p, [_I]),
     "ccdc_last_cuda_error": (_I, []),
     "ccdc_num_kernel_launches": (_I, []),
@@ -470,6 +484,249 @@ class Plan:
         ws = workspace.data_ptr() if workspace is not None and workspace.numel() else None
         _check(lib().ccdc_shuffle(self._h, _ptr_array(part), coded.data_ptr(), out.data_ptr(), ws,
                                   _stream_handle(stream)), "ccdc_shuffle")
+
+
+# ---- block operators ------------------------------------------------------
+# Tensors are 2-D [rows][columns] with contiguous columns and any row stride, all of one dtype (float32,
+# bfloat16, float16) on one device.  Outputs and scratch that are not passed in come from torch's allocator,
+# on the stream the call runs on.
+
+
+def _block_dtype(t):
+    import torch
+
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"float32, bfloat16 or float16 expected, got {t.dtype}")
+    return code
+
+
+def _rows(t, name, like=None, shape=None):
+    """row stride of a 2-D tensor; raises where it is not what the call takes."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: a 2-D tensor with contiguous columns expected")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name}: {like.dtype} on {like.device} expected, got {t.dtype} on {t.device}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor expected")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t, name, like, n):
+    if t.numel() != n or not t.is_contiguous() or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: {n} contiguous {like.dtype} on {like.device} expected")
+    return t.data_ptr()
+
+
+class _OnStream:
+    """makes the call's device and stream torch's current ones, for the allocations and the launch."""
+
+    def __init__(self, tensor, stream):
+        import torch
+
+        if stream is not None and stream.device != tensor.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        self.ctx = None
+        if stream is not None:
+            self.ctx = torch.cuda.stream(stream)
+        elif tensor.device.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(tensor.device)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _handle():
+    import torch
+
+    return torch.cuda.current_stream().cuda_stream
+
+
+def dropout(x, p, seed, offset=0, out=None, stream=None):
+    """``ccdc_dropout``: x with elements dropped by the counter-based mask of (seed, offset + element).
+    The backward pass is the same call on the gradient.  ``out`` may be ``x``."""
+    import torch
+
+    ldx = _rows(x, "x")
+    code = _block_dtype(x)
+    with _OnStream(x, stream):
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        ldy = _rows(y, "out", x, x.shape)
+        _check(lib().ccdc_dropout(x.shape[0], x.shape[1], code, x.data_ptr(), ldx, y.data_ptr(), ldy, p, seed, offset,
+                                  _handle()), "ccdc_dropout")
+    return y
+
+
+def _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate):
+    M, D = x.shape
+    ldx = _rows(x, "x")
+    ldy = D if y is None else _rows(y, "y", x, x.shape)
+    pw = None if w_post is None else _vector(w_post, "w_post", x, D)
+    pp = None if w_pre is None else _vector(w_pre, "w_pre", x, D)
+    pg, per = None, 1
+    if gate is not None:
+        per = rows_per_gate
+        if per is None:
+            per = max(M, 1) if gate.numel() == D else 1
+        if per < 1:
+            raise ValueError("rows_per_gate must be at least 1")
+        pg = _vector(gate, "gate", x, max(1, -(-M // per)) * D)
+    return M, D, ldx, ldy, pw, pp, pg, per
+
+
+def residual_norm_forward(x, y=None, *, w_post=None, w_pre=None, gate=None, rows_per_gate=None, alpha=1.0, p=0.0, seed=0,
+                          offset=0, kind="rms", eps=1e-5, save=False, out=None, z=None, stream=None):
+    """``ccdc_residual_norm_forward``: out = alpha*x + drop(gate * norm(y)*w_post), z = norm(out)*w_pre.
+    Returns (out, z), or (out, z, stats) with ``save``; z is None without ``w_pre``."""
+    import torch
+
+    M, D, ldx, ldy, pw, pp, pg, per = _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate)
+    code = _block_dtype(x)
+    with _OnStream(x, stream):
+        out = torch.empty((M, D), dtype=x.dtype, device=x.device) if out is None else out
+        if w_pre is not None:
+            z = torch.empty((M, D), dtype=x.dtype, device=x.device) if z is None else z
+        elif z is not None:
+            raise ValueError("z needs w_pre")
+        stats = torch.empty((M, 4), dtype=torch.float32, device=x.device) if save else None
+        _check(lib().ccdc_residual_norm_forward(
+            M, D, code, NORMS[kind], eps, x.data_ptr(), ldx, None if y is None else y.data_ptr(), ldy, pw, pp, pg, per,
+            alpha, p, seed, offset, out.data_ptr(), _rows(out, "out", x, x.shape),
+            None if z is None else z.data_ptr(), D if z is None else _rows(z, "z", x, x.shape),
+            stats.data_ptr() if save else None, _handle()), "ccdc_residual_norm_forward")
+    return (out, z, stats) if save else (out, z)
+
+
+def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, gate=None, rows_per_gate=None, alpha=1.0,
+                           p=0.0, seed=0, offset=0, kind="rms", eps=None, grad_dtype=None, dx=None, dy=None,
+                           dw_post=None, dw_pre=None, dgate=None, workspace=None, stream=None):
+    """``ccdc_residual_norm_backward``: (dx, dy, dw_post, dw_pre, dgate), None for what the forward call lacked.
+    ``dout`` or ``dz`` may be None (zero).  ``eps`` is accepted for symmetry; the forward's is in ``stats``."""
+    import torch
+
+    M, D, ldx, ldy, pw, pp, pg, per = _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate)
+    code, like = _block_dtype(x), x
+    gt = x.dtype if grad_dtype is None else grad_dtype
+    if gt not in (x.dtype, torch.float32):
+        raise TypeError("grad_dtype is the tensors' dtype or float32")
+    if tuple(stats.shape) != (M, 4) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != x.device:
+        raise ValueError("stats: what residual_norm_forward(save=True) returned expected")
+    with _OnStream(x, stream):
+        def empty(t, wanted, shape, dtype, name):
+            if not wanted:
+                if t is not None:
+                    raise ValueError(f"{name}: the forward call has no such input")
+                return None
+            if t is None:
+                return torch.empty(shape, dtype=dtype, device=x.device)
+            if t.device != x.device or t.dtype != dtype or (name[:2] == "dw" or name == "dgate") and (
+                    not t.is_contiguous() or t.numel() != (D if name[:2] == "dw" else gate.numel())):
+                raise ValueError(f"{name}: {tuple(shape)} {dtype} on {x.device} expected")
+            return t
+
+        dx = empty(dx, True, (M, D), x.dtype, "dx")
+        dy = empty(dy, y is not None, (M, D), x.dtype, "dy")
+        dw_post = empty(dw_post, w_post is not None, (D,), gt, "dw_post")
+        dw_pre = empty(dw_pre, w_pre is not None, (D,), gt, "dw_pre")
+        dgate = empty(dgate, gate is not None, None if gate is None else gate.shape, gt, "dgate")
+        need = lib().ccdc_residual_norm_workspace_bytes(M, D)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+
+        def ptr(t):
+            return None if t is None else t.data_ptr()
+
+        def ld(t, name):
+            return D if t is None else _rows(t, name, like, like.shape)
+
+        _check(lib().ccdc_residual_norm_backward(
+            M, D, code, F32 if gt == torch.float32 else code, NORMS[kind], ptr(dout), ld(dout, "dout"), ptr(dz), ld(dz, "dz"),
+            x.data_ptr(), ldx, ptr(y), ldy, stats.data_ptr(), pw, pp, pg, per, alpha, p, seed, offset,
+            dx.data_ptr(), ld(dx, "dx"), ptr(dy), ld(dy, "dy"), ptr(dw_post), ptr(dw_pre), ptr(dgate),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle()), "ccdc_residual_norm_backward")
+    return dx, dy, dw_post, dw_pre, dgate
+
+
+def _ffn_tensors(x, w_gate, w_up, w_down):
+    M, D = x.shape
+    F = w_gate.shape[0]
+    ldx = _rows(x, "x")
+    ldw = _rows(w_gate, "w_gate", x, (F, D))
+    if _rows(w_up, "w_up", x, (F, D)) != ldw:
+        raise ValueError("w_gate and w_up need one row stride")
+    return M, D, F, ldx, ldw, _rows(w_down, "w_down", x, (D, F))
+
+
+def _ffn_aligned(size, D, F, tensors):
+    """whether every pointer and row stride is a multiple of 16 bytes"""
+    if D * size % 16 or F * size % 16:
+        return 0
+    return int(all(t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or t.stride(0) * size % 16 == 0) for t in tensors))
+
+
+def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved=None, workspace=None, stream=None):
+    """``ccdc_ffn_forward``: (act(x w_gate^T) * (x w_up^T)) w_down^T.  Returns y, or (y, saved) with ``save``;
+    ``saved`` is opaque and goes to ``ffn_backward``."""
+    import torch
+
+    M, D, F, ldx, ldw, ldd = _ffn_tensors(x, w_gate, w_up, w_down)
+    code, L = _block_dtype(x), lib()
+    with _OnStream(x, stream):
+        y = torch.empty((M, D), dtype=x.dtype, device=x.device) if out is None else out
+        ldy = _rows(y, "out", x, x.shape)
+        if save and saved is None:
+            saved = torch.empty(L.ccdc_ffn_saved_bytes(M, F, code), dtype=torch.uint8, device=x.device)
+        if workspace is None:
+            aligned = _ffn_aligned(x.element_size(), D, F, (x, w_gate, w_up, w_down, y))
+            workspace = torch.empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 0, aligned), dtype=torch.uint8,
+                                    device=x.device)
+        _check(L.ccdc_ffn_forward(M, D, F, code, ACTS[act], x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), ldw,
+                                  w_down.data_ptr(), ldd, y.data_ptr(), ldy, saved.data_ptr() if save else None,
+                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle()),
+               "ccdc_ffn_forward")
+    return (y, saved) if save else y
+
+
+def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None, dx=None, dw_gate=None, dw_up=None,
+                 dw_down=None, workspace=None, stream=None):
+    """``ccdc_ffn_backward``: (dx, dw_gate, dw_up, dw_down).  Gradients may be passed in (contiguous, e.g. slices of
+    a partition row); ``grad_dtype`` float32 keeps the sums' 32 bits."""
+    import torch
+
+    M, D, F, ldx, ldw, ldd = _ffn_tensors(x, w_gate, w_up, w_down)
+    code, L = _block_dtype(x), lib()
+    gt = x.dtype if grad_dtype is None else grad_dtype
+    if gt not in (x.dtype, torch.float32):
+        raise TypeError("grad_dtype is the tensors' dtype or float32")
+    lddy = _rows(dy, "dy", x, x.shape)
+    if saved.numel() * saved.element_size() < L.ccdc_ffn_saved_bytes(M, F, code) or saved.device != x.device:
+        raise ValueError("saved: what ffn_forward(save=True) returned expected")
+    with _OnStream(x, stream):
+        dx = torch.empty((M, D), dtype=x.dtype, device=x.device) if dx is None else dx
+        grads = []
+        for t, rows, cols, name in ((dw_gate, F, D, "dw_gate"), (dw_up, F, D, "dw_up"), (dw_down, D, F, "dw_down")):
+            if t is None:
+                t = torch.empty((rows, cols), dtype=gt, device=x.device)
+            elif t.numel() != rows * cols or not t.is_contiguous() or t.dtype != gt or t.device != x.device:
+                raise ValueError(f"{name}: {rows}x{cols} contiguous {gt} on {x.device} expected")
+            grads.append(t)
+        if workspace is None:
+            aligned = _ffn_aligned(x.element_size(), D, F, (dy, x, w_gate, w_up, w_down, dx))
+            workspace = torch.empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 1, aligned), dtype=torch.uint8,
+                                    device=x.device)
+        _check(L.ccdc_ffn_backward(
+            M, D, F, code, F32 if gt == torch.float32 else code, ACTS[act], dy.data_ptr(), lddy, x.data_ptr(), ldx,
+            w_gate.data_ptr(), w_up.data_ptr(), ldw, w_down.data_ptr(), ldd, saved.data_ptr(), dx.data_ptr(),
+            _rows(dx, "dx", x, x.shape), *(t.data_ptr() for t in grads), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), _handle()), "ccdc_ffn_backward")
+    return dx, *grads
 
 
 def num_kernel_launches() -> int:
