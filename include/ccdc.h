@@ -562,6 +562,12 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
                       const void *w_down, long long ldd, const void *saved, void *dx, long long lddx, void *dw_gate,
                       void *dw_up, void *dw_down, void *workspace, size_t workspace_bytes, void *stream);
 
+/* The feed-forward kernels wait for copies and products through bounded polls.
+ * After the stream was synchronised: CCDC_OK, or CCDC_ESTATE if a wait of any
+ * call on the current device ever ran out (outputs since then are not valid).
+ * Synchronous; copies one word back. */
+int ccdc_block_status(void);
+
 /* ------------------------------------------------------------- diagnostics */
 const char *ccdc_strerror(int status);
 int ccdc_last_cuda_error(void);          /* cudaError_t of the last CCDC_ECUDA on this thread */

@@ -102,6 +102,7 @@ SIGNATURES = {
     "ccdc_ffn_forward": (_I, [_LL, _LL, _LL, _I, _I, _P, _LL, _P, _P, _LL, _P, _LL, _P, _LL, _P, _P, _SZ, _P]),
     "ccdc_ffn_backward": (_I, [_LL, _LL, _LL, _I, _I, _I, _P, _LL, _P, _LL, _P, _P, _LL, _P, _LL, _P, _P, _LL, _P, _P,
                                _P, _P, _SZ, _P]),
+    "ccdc_block_status": (_I, []),
     "ccdc_strerror": (ctypes.c_char_p, [_I]),
     "ccdc_last_cuda_error": (_I, []),
     "ccdc_num_kernel_launches": (_I, []),
@@ -727,6 +728,11 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
             _rows(dx, "dx", x, x.shape), *(t.data_ptr() for t in grads), workspace.data_ptr(),
             workspace.numel() * workspace.element_size(), _handle()), "ccdc_ffn_backward")
     return dx, *grads
+
+
+def block_status():
+    """after a synchronise: raises if a bounded wait inside a feed-forward kernel ever ran out on this device."""
+    _check(lib().ccdc_block_status(), "ccdc_block_status")
 
 
 def num_kernel_launches() -> int:

@@ -1,119 +1,330 @@
-// Gated feed-forward block, forward and backward: the products, with the activation, its derivative and the
-// elementwise products in their epilogues.
+// Gated feed-forward block, forward and backward: what is computed in which order, where it is kept, and the small
+// kernels around the products (copies into the layout the tensor cores read, sums of products cut along k).
 #include <algorithm>
 
 #include "ccdc_ffn.h"
+#include "ccdc_ffn_mma.h"
 
 namespace {
 
-// C[m][n] = sum over segments s and k of A_s(m, k) B_s(n, k); strides in elements.
-struct Operand {
-    const void *p;
-    long long rs, ks;
-};
-enum Epilogue { STORE, GATE, GATE_BACK };
-struct Product {
-    long long M, N, K;
-    int segments;               // GATE: the two products stay apart
-    Operand a[2], b[2];
-    void *c;                    // STORE
-    long long ldc;
-    int c_f32;
-    float *h, *u;               // GATE: out (may be NULL); GATE_BACK: in
-    void *v;                    // GATE: a
-    void *dh, *du;
-    long long ldf;
-    int act;
-};
+constexpr int MAX_COPIES = 5, MAX_JOINS = 4;
 
-constexpr int TILE = 64, STEP = 16;
-
-template <class T, int EPI>
-__global__ void __launch_bounds__(256) k_product(const Product p) {
-    __shared__ float sa[STEP][TILE + 1], sb[2][STEP][TILE + 1];
-    constexpr int NB = EPI == GATE ? 2 : 1;
-    const long long m0 = (long long)blockIdx.y * TILE, n0 = (long long)blockIdx.x * TILE;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[NB][4][4] = {};
-    for (int s = 0; s < (EPI == GATE ? 1 : p.segments); ++s)
-        for (long long k0 = 0; k0 < p.K; k0 += STEP) {
-            for (int i = threadIdx.x; i < TILE * STEP; i += 256) {
-                // neighbouring threads along the operand's contiguous direction
-                auto fetch = [&](const Operand &o, long long r0, long long rows, float *to) {
-                    const int r = o.ks == 1 ? i / STEP : i % TILE, k = o.ks == 1 ? i % STEP : i / TILE;
-                    const bool in = r0 + r < rows && k0 + k < p.K;
-                    to[k * (TILE + 1) + r] = in ? to_f32<T>(static_cast<const T *>(o.p)[(r0 + r) * o.rs + (k0 + k) * o.ks]) : 0.0f;
-                };
-                fetch(p.a[s], m0, p.M, &sa[0][0]);
+// ------------------------------------------------------------------ copies
+// A matrix the tensor cores cannot read as it lies: rows that TMA cannot address (16-byte rule) are copied to padded
+// rows; binary32 is split into three bf16 planes, v = hi + mid + lo with hi = bf16(v), mid = bf16(v - hi) and
+// lo = bf16(v - hi - mid), which hold 24 bits between them.
+struct Copy {
+    const void *from;
+    void *to;
+    long long rows, cols, ld, ld_to;
+};
+struct Copies {
+    Copy c[MAX_COPIES];
+    int count, f32;
+};
+__global__ void __launch_bounds__(256) k_ffn_copy(const Copies a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Copy &c = a.c[blockIdx.y];
+    const long long pairs = c.ld_to / 2, n = c.rows * pairs;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
+        const long long r = i / pairs, k = (i - r * pairs) * 2;
+        if (k >= c.cols) continue;
+        const bool two = k + 1 < c.cols;
+        if (a.f32) {
+            const float *p = static_cast<const float *>(c.from) + r * c.ld + k;
+            float x = p[0], y = two ? p[1] : 0.0f;
+            uint32_t *q = static_cast<uint32_t *>(c.to) + i;
 #pragma unroll
-                for (int j = 0; j < NB; ++j) fetch(p.b[EPI == GATE ? j : s], n0, p.N, &sb[j][0][0]);
+            for (int z = 0; z < 3; ++z) {
+                const uint32_t v = pack2<bf16>(x, y);
+                q[z * n] = v;
+                const float2 f = unpack2<bf16>(v);
+                // infinities and NaN stay in the first plane
+                x = isfinite(f.x) ? x - f.x : 0.0f, y = isfinite(f.y) ? y - f.y : 0.0f;
             }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < STEP; ++k)
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) acc[j][y][x] += sa[k][ty + 16 * y] * sb[j][k][tx + 16 * x];
-            __syncthreads();
+        } else {
+            const uint16_t *p = static_cast<const uint16_t *>(c.from) + r * c.ld + k;
+            static_cast<uint32_t *>(c.to)[i] = p[0] | (two ? (uint32_t)p[1] << 16 : 0u);
         }
+    }
+}
+
+// ------------------------------------------------------------------ joins
+// The sum of a product's parts along k, in order.
+struct Join {
+    const float *parts;
+    void *to;
+    long long rows, cols, ld_parts, ld_to;
+    int splits, type;
+};
+struct Joins {
+    Join j[MAX_JOINS];
+    int count;
+};
+__global__ void __launch_bounds__(256) k_ffn_join(const Joins a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Join &j = a.j[blockIdx.y];
+    const long long quads = (j.cols + 3) / 4, n = j.rows * quads, plane = j.rows * j.ld_parts;
+    const bool wide = j.ld_to % 4 == 0 && (reinterpret_cast<uintptr_t>(j.to) & 15) == 0;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < n; i += gridDim.x * 256LL) {
+        const long long r = i / quads, k = (i - r * quads) * 4;
+        const float *p = j.parts + r * j.ld_parts + k;
+        float4 v = *reinterpret_cast<const float4 *>(p);
+        for (int s = 1; s < j.splits; ++s) {
+            const float4 o = *reinterpret_cast<const float4 *>(p + s * plane);
+            v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        }
+        const long long at = r * j.ld_to + k;
+        if (wide && k + 4 <= j.cols) {
+            if (j.type == CCDC_F32)
+                *reinterpret_cast<float4 *>(static_cast<float *>(j.to) + at) = v;
+            else
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(j.to) + at) =
+                    j.type == CCDC_BF16 ? make_uint2(pack2<bf16>(v.x, v.y), pack2<bf16>(v.z, v.w))
+                                        : make_uint2(pack2<fp16>(v.x, v.y), pack2<fp16>(v.z, v.w));
+        } else {
+            const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const long long m = m0 + ty + 16 * y, n = n0 + tx + 16 * x;
-            if (m >= p.M || n >= p.N) continue;
-            if constexpr (EPI == STORE) {
-                if (p.c_f32)
-                    static_cast<float *>(p.c)[m * p.ldc + n] = acc[0][y][x];
-                else
-                    static_cast<T *>(p.c)[m * p.ldc + n] = from_f32<T>(acc[0][y][x]);
-            } else if constexpr (EPI == GATE) {
-                const float h = acc[0][y][x], u = acc[NB - 1][y][x];
-                float slope;
-                const float f = act_value(p.act, h, &slope);
-                if (p.h) {
-                    p.h[m * p.ldf + n] = h;
-                    p.u[m * p.ldf + n] = u;
+            for (int e = 0; e < 4; ++e)
+                if (k + e < j.cols) {
+                    if (j.type == CCDC_F32)
+                        static_cast<float *>(j.to)[at + e] = f[e];
+                    else if (j.type == CCDC_BF16)
+                        static_cast<bf16 *>(j.to)[at + e] = from_f32<bf16>(f[e]);
+                    else
+                        static_cast<fp16 *>(j.to)[at + e] = from_f32<fp16>(f[e]);
                 }
-                static_cast<T *>(p.v)[m * p.ldf + n] = from_f32<T>(f * u);
-            } else {
-                const float h = p.h[m * p.ldf + n], u = p.u[m * p.ldf + n];
-                float slope;
-                const float f = act_value(p.act, h, &slope), d = acc[0][y][x];
-                static_cast<T *>(p.dh)[m * p.ldf + n] = from_f32<T>(d * u * slope);
-                static_cast<T *>(p.du)[m * p.ldf + n] = from_f32<T>(d * f);
-            }
         }
+    }
 }
 
-template <class T, int EPI>
-int launch(const Product &p, cudaStream_t s) {
-    if (p.M == 0 || p.N == 0) return CCDC_OK;
-    const dim3 grid((unsigned)((p.N + TILE - 1) / TILE), (unsigned)((p.M + TILE - 1) / TILE));
-    k_product<T, EPI><<<grid, 256, 0, s>>>(p);
-    return block_launch_status();
+template <class P>
+int launch_small(void (*kernel)(P), const P &p, long long items, int rows, int sms, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::max<long long>(1, std::min<long long>((items + 255) / 256, 16LL * sms)), (unsigned)rows);
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    ccdc_internal_count_launch();
+    return CCDC_OK;
 }
 
-template <class F>
-int by_type(int dtype, F f) {
-    if (dtype == CCDC_F32) return f(float());
-    if (dtype == CCDC_BF16) return f(bf16());
-    return f(fp16());
+// ------------------------------------------------------------------ layouts
+long long pitch(long long cols) { return (long long)round_up((size_t)cols, 8); }
+int planes_of(int dtype) { return dtype == CCDC_F32 ? 3 : 1; }
+size_t inner_bytes(long long M, long long F, int dtype) {       // a, dh, du
+    return round_up((size_t)planes_of(dtype) * M * pitch(F) * 2, 256);
+}
+size_t wide_bytes(long long M, long long F) {                   // h, u
+    return round_up((size_t)((M + 31) / 32) * ffn_saved_groups(F) * 128 * sizeof(float), 256);
+}
+size_t copy_bytes(long long rows, long long cols, int dtype) {
+    return round_up((size_t)planes_of(dtype) * rows * pitch(cols) * 2, 256);
+}
+bool readable(const void *p, long long ld, long long rows, int dtype) {
+    return is_16bit(dtype) && aligned_to(p, 16) && (rows < 2 || ld % 8 == 0);
 }
 
-// planes of [M][F] between the products, rows padded to 16 bytes
-long long inner_stride(long long F) { return (long long)round_up((size_t)F, 8); }
-size_t plane_bytes(long long M, long long F, int dtype) {
-    return round_up((size_t)M * inner_stride(F) * type_bytes(dtype), 256);
+// the workspace, handed out front to back; a null base only counts
+struct Space {
+    char *base;
+    size_t used = 0;
+    void *take(size_t bytes) {
+        void *p = base ? base + used : nullptr;
+        used += round_up(bytes, 256);
+        return p;
+    }
+};
+
+// ------------------------------------------------------------------ tiles and cuts
+// How a launch's products are tiled: pairs of SMs or single ones, and how often each product is cut along k.  The
+// estimate: a step of 64 k takes 512 cycles on a pair's 256 x 256 tile and about 300 on a single 128 x 128 one (their
+// multiplications, and the operands' way from L2 for the small tile); an item costs about 2000 cycles besides; a cut
+// product is written and read again in binary32 and needs another launch.
+struct Shape {
+    long long M, N, steps;      // steps of 64 k over all segments
+    int splits;
+};
+bool choose_tiles(Shape *q, int count, bool gate, bool may_cut, int sms) {
+    double best = 1e30;
+    bool pair = false;
+    int cuts[4] = {};
+    for (int two = 0; two < 2; ++two) {
+        const long long tile = two ? 256 : 128, tile_n = gate ? tile / 2 : tile;
+        const double step = two ? 512 : 300, units = two ? sms / 2 : sms;
+        for (long long most = may_cut ? 8 : 1LL << 40;; most = most >= 256 ? 1LL << 40 : most * 2) {
+            double total = 0, longest = 0, items = 0, parts = 0;
+            int c[4];
+            for (int i = 0; i < count; ++i) {
+                const long long tiles = ((q[i].M + tile - 1) / tile) * ((q[i].N + tile_n - 1) / tile_n);
+                c[i] = (int)std::min<long long>(std::max<long long>(1, (q[i].steps + most / 2) / most), 64);
+                const double cost = (double)q[i].steps / c[i] * step + 2000;
+                total += cost * tiles * c[i], items += (double)tiles * c[i];
+                longest = std::max(longest, cost);
+                if (c[i] > 1) parts += 8.0 * c[i] * q[i].M * q[i].N;
+            }
+            double t = items <= units ? longest : std::max(longest, total / units) + longest / 2;
+            if (parts > 0) t += 4000 + parts / 2000;        // cycles; parts mostly stay in L2
+            if (t < best) {
+                best = t, pair = two;
+                for (int i = 0; i < count; ++i) cuts[i] = c[i];
+            }
+            if (most >= 1LL << 40) break;
+        }
+    }
+    for (int i = 0; i < count; ++i) q[i].splits = cuts[i];
+    return pair;
 }
+
+long long steps_of(long long K, int segments) { return (K + 63) / 64 * segments; }
+int segments_of(int dtype, int terms) { return dtype == CCDC_F32 ? 6 * terms : terms; }
 
 int check_ffn(long long M, long long D, long long F, int dtype, int act) {
     if (M < 0 || D < 1 || F < 1 || !is_float_type(dtype) || act < CCDC_ACT_SILU || act > CCDC_ACT_RELU) return CCDC_EINVAL;
     if (M > (1LL << 21) || D > (1LL << 20) || F > (1LL << 20)) return CCDC_ESIZE;
     return CCDC_OK;
+}
+
+// One call: the operands as the tensor cores read them, the workspace, the launches.  With plan_only set the same
+// steps only count the workspace.
+struct Call {
+    long long M, D, F;
+    int dtype, act, sms;
+    bool plan_only, aligned;
+    Space space;
+    cudaStream_t s;
+    Copies copies = {};
+    Joins joins = {};
+    int rc = CCDC_OK;
+
+    int type() const { return dtype == CCDC_F16 ? CCDC_F16 : CCDC_BF16; }
+
+    MmaMatrix operand(const void *p, long long rows, long long cols, long long ld) {
+        const bool direct = plan_only ? aligned && is_16bit(dtype) : readable(p, ld, rows, dtype);
+        if (direct) return {p, rows, cols, rows < 2 ? pitch(cols) : ld, 1};
+        void *to = space.take(copy_bytes(rows, cols, dtype));
+        copies.c[copies.count++] = {p, to, rows, cols, ld, pitch(cols)};
+        return {to, rows, cols, pitch(cols), planes_of(dtype)};
+    }
+    void run_copies() {
+        if (plan_only || !copies.count || rc != CCDC_OK) return;
+        copies.f32 = dtype == CCDC_F32;
+        long long most = 0;
+        for (int i = 0; i < copies.count; ++i) most = std::max(most, copies.c[i].rows * copies.c[i].ld_to / 2);
+        rc = launch_small(k_ffn_copy, copies, most, copies.count, sms, s);
+    }
+    MmaMatrix inner(void *p) const { return {p, M, F, pitch(F), planes_of(dtype)}; }
+    // where a product goes: its output, or parts of it to be joined
+    void to_output(MmaProduct &q, int splits, void *c, long long ldc, int c_type) {
+        q.splits = splits;
+        q.c = c, q.ldc = ldc, q.c_type = c_type;
+        if (splits == 1) return;
+        q.ldc = (q.N + 3) / 4 * 4;
+        q.c = space.take((size_t)splits * q.M * q.ldc * sizeof(float));
+        q.c_type = CCDC_F32;
+        joins.j[joins.count++] = {static_cast<const float *>(q.c), c, q.M, q.N, q.ldc, ldc, splits, c_type};
+    }
+    void run_products(const MmaProduct *q, int count, MmaEpilogue e, bool pair) {
+        if (plan_only || rc != CCDC_OK) return;
+        rc = mma_launch(q, count, e, type(), pair, sms, s);
+    }
+    void run_joins() {
+        if (plan_only || !joins.count || rc != CCDC_OK) return;
+        long long most = 0;
+        for (int i = 0; i < joins.count; ++i) most = std::max(most, joins.j[i].rows * (joins.j[i].cols / 4 + 1));
+        rc = launch_small(k_ffn_join, joins, most, joins.count, sms, s);
+    }
+
+    void forward(const void *x, long long ldx, const void *wg, const void *wu, long long ldw, const void *wd, long long ldd,
+                 void *y, long long ldy, char *saved) {
+        const MmaMatrix X = operand(x, M, D, ldx), G = operand(wg, F, D, ldw), U = operand(wu, F, D, ldw);
+        const MmaMatrix W = operand(wd, D, F, ldd);
+        void *a = saved ? saved + 2 * wide_bytes(M, F) : space.take(inner_bytes(M, F, dtype));
+        MmaProduct p = {};
+        p.M = M, p.N = F, p.K = D, p.terms = 1, p.act = act;
+        p.a[0] = {X, false}, p.b[0] = {G, false}, p.b[1] = {U, false};
+        if (saved) p.h = reinterpret_cast<float *>(saved), p.u = reinterpret_cast<float *>(saved + wide_bytes(M, F));
+        p.out[0] = inner(a);
+        Shape first = {M, F, steps_of(D, segments_of(dtype, 1)), 1};
+        const bool pair = choose_tiles(&first, 1, true, false, sms);
+        MmaProduct q = {};
+        q.M = M, q.N = D, q.K = F, q.terms = 1, q.a[0] = {inner(a), false}, q.b[0] = {W, false};
+        Shape second = {M, D, steps_of(F, segments_of(dtype, 1)), 1};
+        const bool pair2 = choose_tiles(&second, 1, false, true, sms);
+        to_output(q, second.splits, y, ldy, dtype);
+        run_copies();
+        run_products(&p, 1, MMA_GATE, pair);
+        run_products(&q, 1, MMA_STORE, pair2);
+        run_joins();
+    }
+
+    void backward(const void *dy, long long lddy, const void *x, long long ldx, const void *wg, const void *wu, long long ldw,
+                  const void *wd, long long ldd, char *saved, void *dx, long long lddx, void *dwg, void *dwu, void *dwd,
+                  int grad_dtype) {
+        const MmaMatrix DY = operand(dy, M, D, lddy), X = operand(x, M, D, ldx), G = operand(wg, F, D, ldw);
+        const MmaMatrix U = operand(wu, F, D, ldw), W = operand(wd, D, F, ldd);
+        const MmaMatrix A = inner(saved + 2 * wide_bytes(M, F));
+        const MmaMatrix DH = inner(space.take(inner_bytes(M, F, dtype))), DU = inner(space.take(inner_bytes(M, F, dtype)));
+        MmaProduct p = {};
+        p.M = M, p.N = F, p.K = D, p.terms = 1, p.act = act;
+        p.a[0] = {DY, false}, p.b[0] = {W, true};
+        p.h = reinterpret_cast<float *>(saved), p.u = reinterpret_cast<float *>(saved + wide_bytes(M, F));
+        p.out[0] = DH, p.out[1] = DU;
+        Shape first = {M, F, steps_of(D, segments_of(dtype, 1)), 1};
+        const bool pair = choose_tiles(&first, 1, false, false, sms);
+        MmaProduct q[4] = {};
+        Shape shapes[4];
+        void *to[4];
+        int n = 0;
+        auto add = [&](long long m, long long nn, long long k, int terms, void *c) {
+            q[n].M = m, q[n].N = nn, q[n].K = k, q[n].terms = terms;
+            shapes[n] = {m, nn, steps_of(k, segments_of(dtype, terms)), 1};
+            to[n] = c;
+            return &q[n++];
+        };
+        MmaProduct *r = add(M, D, F, 2, dx);        // the longest items first
+        r->a[0] = {DH, false}, r->b[0] = {G, true}, r->a[1] = {DU, false}, r->b[1] = {U, true};
+        r = add(F, D, M, 1, dwg);
+        r->a[0] = {DH, true}, r->b[0] = {X, true};
+        r = add(F, D, M, 1, dwu);
+        r->a[0] = {DU, true}, r->b[0] = {X, true};
+        r = add(D, F, M, 1, dwd);
+        r->a[0] = {DY, true}, r->b[0] = {A, true};
+        // tiles and cuts are those of the whole set, so that leaving an output out changes no other output's bits
+        const bool pair2 = choose_tiles(shapes, n, false, true, sms);
+        int wanted = 0;
+        for (int i = 0; i < n; ++i) {
+            if (!to[i] && !plan_only) continue;
+            const bool is_dx = q[i].terms == 2;
+            to_output(q[i], shapes[i].splits, to[i], is_dx ? lddx : q[i].N, is_dx ? dtype : grad_dtype);
+            q[wanted++] = q[i];
+        }
+        n = wanted;
+        run_copies();
+        run_products(&p, 1, MMA_GATE_BACK, pair);
+        run_products(q, n, MMA_STORE, pair2);
+        run_joins();
+    }
+};
+
+// The most that a call of these sizes can need: with everything wanted.
+size_t forward_bytes(long long M, long long D, long long F, int dtype, bool aligned, int sms) {
+    Call c = {M, D, F, dtype, 0, sms, true, aligned};
+    c.forward(nullptr, D, nullptr, nullptr, D, nullptr, F, nullptr, D, nullptr);
+    return c.space.used + 256;
+}
+size_t backward_bytes(long long M, long long D, long long F, int dtype, bool aligned, int sms) {
+    Call c = {M, D, F, dtype, 0, sms, true, aligned};
+    c.backward(nullptr, D, nullptr, D, nullptr, nullptr, D, nullptr, F, nullptr, nullptr, D, nullptr, nullptr, nullptr, dtype);
+    return c.space.used + 256;
 }
 
 }  // namespace
@@ -122,13 +333,16 @@ extern "C" {
 
 size_t ccdc_ffn_saved_bytes(long long M, long long F, int dtype) {
     if (check_ffn(M, 1, F, dtype, 0) != CCDC_OK) return 0;
-    return 2 * plane_bytes(M, F, CCDC_F32) + plane_bytes(M, F, dtype);
+    return 2 * wide_bytes(M, F) + inner_bytes(M, F, dtype);
 }
 
 size_t ccdc_ffn_workspace_bytes(long long M, long long D, long long F, int dtype, int backward, int aligned) {
     if (check_ffn(M, D, F, dtype, 0) != CCDC_OK) return 0;
-    (void)aligned;
-    return (backward ? 2 : 1) * plane_bytes(M, F, dtype);
+    if (M == 0) return 256;
+    int rc;
+    int sms = block_sm_count(&rc);
+    if (rc != CCDC_OK) sms = 148;
+    return backward ? backward_bytes(M, D, F, dtype, aligned != 0, sms) : forward_bytes(M, D, F, dtype, aligned != 0, sms);
 }
 
 int ccdc_ffn_forward(long long M, long long D, long long F, int dtype, int act, const void *x, long long ldx,
@@ -140,25 +354,19 @@ int ccdc_ffn_forward(long long M, long long D, long long F, int dtype, int act, 
     if (!x || !w_gate || !w_up || !w_down || !y || !workspace || ldx < D || ldw < D || ldd < F || ldy < D ||
         !aligned_to(saved, 16) || !aligned_to(workspace, 16))
         return CCDC_EINVAL;
-    if (workspace_bytes < ccdc_ffn_workspace_bytes(M, D, F, dtype, 0, 0)) return CCDC_ESIZE;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const long long ldf = inner_stride(F);
-    return by_type(dtype, [&](auto t) {
-        using T = decltype(t);
-        Product p = {};
-        p.M = M, p.N = F, p.K = D, p.segments = 2, p.act = act, p.ldf = ldf;
-        p.a[0] = p.a[1] = {x, ldx, 1}, p.b[0] = {w_gate, ldw, 1}, p.b[1] = {w_up, ldw, 1};
-        char *keep = static_cast<char *>(saved);
-        const size_t wide = plane_bytes(M, F, CCDC_F32);
-        if (keep) p.h = reinterpret_cast<float *>(keep), p.u = reinterpret_cast<float *>(keep + wide);
-        p.v = keep ? static_cast<void *>(keep + 2 * wide) : workspace;
-        int r = launch<T, GATE>(p, s);
-        if (r != CCDC_OK) return r;
-        Product q = {};
-        q.M = M, q.N = D, q.K = F, q.segments = 1;
-        q.a[0] = {p.v, ldf, 1}, q.b[0] = {w_down, ldd, 1}, q.c = y, q.ldc = ldy, q.c_f32 = dtype == CCDC_F32;
-        return launch<T, STORE>(q, s);
-    });
+    if (workspace_bytes < 256) return CCDC_ESIZE;
+    Call c = {M, D, F, dtype, act, 0, false, false};
+    c.sms = block_sm_count(&rc);
+    if (rc != CCDC_OK) return rc;
+    c.space.base = static_cast<char *>(workspace);
+    c.s = static_cast<cudaStream_t>(stream);
+    // what this call takes: the same steps, counted
+    Call count = c;
+    count.rc = -100;
+    count.forward(x, ldx, w_gate, w_up, ldw, w_down, ldd, y, ldy, static_cast<char *>(saved));
+    if (count.space.used > workspace_bytes) return CCDC_ESIZE;
+    c.forward(x, ldx, w_gate, w_up, ldw, w_down, ldd, y, ldy, static_cast<char *>(saved));
+    return c.rc;
 }
 
 int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad_dtype, int act, const void *dy,
@@ -180,37 +388,19 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
     if (!dy || !x || !w_gate || !w_up || !w_down || !saved || !workspace || lddy < D || ldx < D || ldw < D || ldd < F ||
         (dx && lddx < D) || !aligned_to(saved, 16) || !aligned_to(workspace, 16))
         return CCDC_EINVAL;
-    if (workspace_bytes < ccdc_ffn_workspace_bytes(M, D, F, dtype, 1, 0)) return CCDC_ESIZE;
-    const size_t plane = plane_bytes(M, F, dtype);
-    const long long ldf = inner_stride(F);
-    return by_type(dtype, [&](auto t) {
-        using T = decltype(t);
-        char *keep = const_cast<char *>(static_cast<const char *>(saved));
-        const size_t wide = plane_bytes(M, F, CCDC_F32);
-        char *dh = static_cast<char *>(workspace), *du = dh + plane;
-        Product p = {};
-        p.M = M, p.N = F, p.K = D, p.segments = 1, p.act = act, p.ldf = ldf;
-        p.a[0] = {dy, lddy, 1}, p.b[0] = {w_down, 1, ldd};
-        p.h = reinterpret_cast<float *>(keep), p.u = reinterpret_cast<float *>(keep + wide), p.dh = dh, p.du = du;
-        int r = launch<T, GATE_BACK>(p, s);
-        auto product = [&](long long m, long long n, long long k, Operand a, Operand b, void *c, long long ldc, int f32) {
-            if (r != CCDC_OK || !c) return;
-            Product q = {};
-            q.M = m, q.N = n, q.K = k, q.segments = 1, q.a[0] = a, q.b[0] = b, q.c = c, q.ldc = ldc, q.c_f32 = f32;
-            r = launch<T, STORE>(q, s);
-        };
-        const int g32 = grad_dtype == CCDC_F32;
-        if (r == CCDC_OK && dx) {
-            Product q = {};
-            q.M = M, q.N = D, q.K = F, q.segments = 2, q.c = dx, q.ldc = lddx, q.c_f32 = dtype == CCDC_F32;
-            q.a[0] = {dh, ldf, 1}, q.b[0] = {w_gate, 1, ldw}, q.a[1] = {du, ldf, 1}, q.b[1] = {w_up, 1, ldw};
-            r = launch<T, STORE>(q, s);
-        }
-        product(F, D, M, {dh, 1, ldf}, {x, 1, ldx}, dw_gate, D, g32);
-        product(F, D, M, {du, 1, ldf}, {x, 1, ldx}, dw_up, D, g32);
-        product(D, F, M, {dy, 1, lddy}, {keep + 2 * wide, 1, ldf}, dw_down, F, g32);
-        return r;
-    });
+    if (workspace_bytes < 256) return CCDC_ESIZE;
+    Call c = {M, D, F, dtype, act, 0, false, false};
+    c.sms = block_sm_count(&rc);
+    if (rc != CCDC_OK) return rc;
+    c.space.base = static_cast<char *>(workspace);
+    c.s = s;
+    char *keep = static_cast<char *>(const_cast<void *>(saved));
+    Call count = c;
+    count.rc = -100;
+    count.backward(dy, lddy, x, ldx, w_gate, w_up, ldw, w_down, ldd, keep, dx, lddx, dw_gate, dw_up, dw_down, grad_dtype);
+    if (count.space.used > workspace_bytes) return CCDC_ESIZE;
+    c.backward(dy, lddy, x, ldx, w_gate, w_up, ldw, w_down, ldd, keep, dx, lddx, dw_gate, dw_up, dw_down, grad_dtype);
+    return c.rc;
 }
 
 }  // extern "C"
