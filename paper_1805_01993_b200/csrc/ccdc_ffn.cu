@@ -145,47 +145,49 @@ struct Space {
 };
 
 // ------------------------------------------------------------------ tiles and cuts
-// How a launch's products are tiled: pairs of SMs or single ones, and how often each product is cut along k.  The
-// estimate: a step of 64 k takes 512 cycles on a pair's 256 x 256 tile and about 300 on a single 128 x 128 one (their
-// multiplications, and the operands' way from L2 for the small tile); an item costs about 2000 cycles besides; a cut
-// product is written and read again in binary32 and needs another launch.
+// How a launch's products are tiled, and how often each is cut along k.  The estimate, in cycles: a step of 64 k is
+// bounded by the fetch of its blocks (48 KiB for the 256 x 512 tile, 72 KiB for binary32, 32 KiB for the others, at about
+// 39 bytes a cycle);
+// an item costs about 2000 cycles besides, and its epilogue where it is not hidden (256 x 512); a cut product is
+// written and read again in binary32 and needs another launch.
 struct Shape {
-    long long M, N, steps;      // steps of 64 k over all segments
+    long long M, N, steps;      // steps of 64 k over all terms
     int splits;
 };
-bool choose_tiles(Shape *q, int count, bool gate, bool may_cut, int sms) {
+MmaTile choose_tiles(Shape *q, int count, MmaEpilogue e, bool planes, int sms) {
     double best = 1e30;
-    bool pair = false;
+    MmaTile tile = MMA_SINGLE;
     int cuts[4] = {};
-    for (int two = 0; two < 2; ++two) {
-        const long long tile = two ? 256 : 128, tile_n = gate ? tile / 2 : tile;
-        const double step = two ? 512 : 300, units = two ? sms / 2 : sms;
-        for (long long most = may_cut ? 8 : 1LL << 40;; most = most >= 256 ? 1LL << 40 : most * 2) {
+    for (int shape = planes ? MMA_PLANES : MMA_WIDE; shape <= (planes ? MMA_PLANES : MMA_SINGLE); ++shape) {
+        const MmaTile at = (MmaTile)shape;
+        const long long rows = mma_tile_rows(at), cols = mma_tile_columns(at) / (e == MMA_GATE ? 2 : 1);
+        const double step = planes ? 1890 : at == MMA_WIDE ? 1260 : 840, units = at == MMA_SINGLE ? sms : sms / 2;
+        const double item = 2000 + (at != MMA_WIDE ? 0 : e == MMA_STORE ? 2000 : e == MMA_GATE ? 4000 : 8000);
+        for (long long most = e == MMA_STORE ? 8 : 1LL << 40;; most = most >= 256 ? 1LL << 40 : most * 2) {
             double total = 0, longest = 0, items = 0, parts = 0;
             int c[4];
             for (int i = 0; i < count; ++i) {
-                const long long tiles = ((q[i].M + tile - 1) / tile) * ((q[i].N + tile_n - 1) / tile_n);
+                const long long tiles = ((q[i].M + rows - 1) / rows) * ((q[i].N + cols - 1) / cols);
                 c[i] = (int)std::min<long long>(std::max<long long>(1, (q[i].steps + most / 2) / most), 64);
-                const double cost = (double)q[i].steps / c[i] * step + 2000;
+                const double cost = (double)q[i].steps / c[i] * step + item;
                 total += cost * tiles * c[i], items += (double)tiles * c[i];
                 longest = std::max(longest, cost);
                 if (c[i] > 1) parts += 8.0 * c[i] * q[i].M * q[i].N;
             }
             double t = items <= units ? longest : std::max(longest, total / units) + longest / 2;
-            if (parts > 0) t += 4000 + parts / 2000;        // cycles; parts mostly stay in L2
+            if (parts > 0) t += 4000 + parts / 2000;        // parts mostly stay in L2
             if (t < best) {
-                best = t, pair = two;
+                best = t, tile = at;
                 for (int i = 0; i < count; ++i) cuts[i] = c[i];
             }
             if (most >= 1LL << 40) break;
         }
     }
     for (int i = 0; i < count; ++i) q[i].splits = cuts[i];
-    return pair;
+    return tile;
 }
 
-long long steps_of(long long K, int segments) { return (K + 63) / 64 * segments; }
-int segments_of(int dtype, int terms) { return dtype == CCDC_F32 ? 6 * terms : terms; }
+long long steps_of(long long K, int terms) { return (K + 63) / 64 * terms; }
 
 int check_ffn(long long M, long long D, long long F, int dtype, int act) {
     if (M < 0 || D < 1 || F < 1 || !is_float_type(dtype) || act < CCDC_ACT_SILU || act > CCDC_ACT_RELU) return CCDC_EINVAL;
@@ -232,9 +234,9 @@ struct Call {
         q.c_type = CCDC_F32;
         joins.j[joins.count++] = {static_cast<const float *>(q.c), c, q.M, q.N, q.ldc, ldc, splits, c_type};
     }
-    void run_products(const MmaProduct *q, int count, MmaEpilogue e, bool pair) {
+    void run_products(const MmaProduct *q, int count, MmaEpilogue e, MmaTile tile) {
         if (plan_only || rc != CCDC_OK) return;
-        rc = mma_launch(q, count, e, type(), pair, sms, s);
+        rc = mma_launch(q, count, e, type(), tile, sms, s);
     }
     void run_joins() {
         if (plan_only || !joins.count || rc != CCDC_OK) return;
@@ -253,16 +255,16 @@ struct Call {
         p.a[0] = {X, false}, p.b[0] = {G, false}, p.b[1] = {U, false};
         if (saved) p.h = reinterpret_cast<float *>(saved), p.u = reinterpret_cast<float *>(saved + wide_bytes(M, F));
         p.out[0] = inner(a);
-        Shape first = {M, F, steps_of(D, segments_of(dtype, 1)), 1};
-        const bool pair = choose_tiles(&first, 1, true, false, sms);
+        Shape first = {M, F, steps_of(D, 1), 1};
+        const MmaTile tile = choose_tiles(&first, 1, MMA_GATE, dtype == CCDC_F32, sms);
         MmaProduct q = {};
         q.M = M, q.N = D, q.K = F, q.terms = 1, q.a[0] = {inner(a), false}, q.b[0] = {W, false};
-        Shape second = {M, D, steps_of(F, segments_of(dtype, 1)), 1};
-        const bool pair2 = choose_tiles(&second, 1, false, true, sms);
+        Shape second = {M, D, steps_of(F, 1), 1};
+        const MmaTile tile2 = choose_tiles(&second, 1, MMA_STORE, dtype == CCDC_F32, sms);
         to_output(q, second.splits, y, ldy, dtype);
         run_copies();
-        run_products(&p, 1, MMA_GATE, pair);
-        run_products(&q, 1, MMA_STORE, pair2);
+        run_products(&p, 1, MMA_GATE, tile);
+        run_products(&q, 1, MMA_STORE, tile2);
         run_joins();
     }
 
@@ -278,15 +280,15 @@ struct Call {
         p.a[0] = {DY, false}, p.b[0] = {W, true};
         p.h = reinterpret_cast<float *>(saved), p.u = reinterpret_cast<float *>(saved + wide_bytes(M, F));
         p.out[0] = DH, p.out[1] = DU;
-        Shape first = {M, F, steps_of(D, segments_of(dtype, 1)), 1};
-        const bool pair = choose_tiles(&first, 1, false, false, sms);
+        Shape first = {M, F, steps_of(D, 1), 1};
+        const MmaTile tile = choose_tiles(&first, 1, MMA_GATE_BACK, dtype == CCDC_F32, sms);
         MmaProduct q[4] = {};
         Shape shapes[4];
         void *to[4];
         int n = 0;
         auto add = [&](long long m, long long nn, long long k, int terms, void *c) {
             q[n].M = m, q[n].N = nn, q[n].K = k, q[n].terms = terms;
-            shapes[n] = {m, nn, steps_of(k, segments_of(dtype, terms)), 1};
+            shapes[n] = {m, nn, steps_of(k, terms), 1};
             to[n] = c;
             return &q[n++];
         };
@@ -299,7 +301,7 @@ struct Call {
         r = add(D, F, M, 1, dwd);
         r->a[0] = {DY, true}, r->b[0] = {A, true};
         // tiles and cuts are those of the whole set, so that leaving an output out changes no other output's bits
-        const bool pair2 = choose_tiles(shapes, n, false, true, sms);
+        const MmaTile tile2 = choose_tiles(shapes, n, MMA_STORE, dtype == CCDC_F32, sms);
         int wanted = 0;
         for (int i = 0; i < n; ++i) {
             if (!to[i] && !plan_only) continue;
@@ -309,8 +311,8 @@ struct Call {
         }
         n = wanted;
         run_copies();
-        run_products(&p, 1, MMA_GATE_BACK, pair);
-        run_products(q, n, MMA_STORE, pair2);
+        run_products(&p, 1, MMA_GATE_BACK, tile);
+        run_products(q, n, MMA_STORE, tile2);
         run_joins();
     }
 };

@@ -1,18 +1,29 @@
 // The matrix products of the feed-forward block on tcgen05 tensor cores.
 //
 // A product is C[m][n] = sum_k A(m, k) B(n, k) in 16-bit operands and binary32 sums.  One persistent block per SM
-// walks output tiles; two SMs of a cluster share a 256 x 256 tile (cta_group::2: each holds 128 rows of A and 128
-// columns of B, the tensor cores read both) or one SM computes a 128 x 128 tile.  Warps have roles:
-//   0      fetches: 128 x 64 blocks of A and B by TMA into a ring of 32 KiB stages (four 8 KiB boxes a stage)
+// walks output tiles; two SMs of a cluster share a 256 x 512 or 256 x 256 tile (cta_group::2: each holds 128 rows of A
+// and half of the columns of B, the tensor cores read both) or one SM computes a 128 x 128 tile.  What bounds the
+// products is the way into an SM: its TMA path was measured at 35 to 41 bytes a cycle, whatever the tile order, the
+// number of stages or of SMs in use, and the full rate of the tensor cores needs 64 bytes a cycle and SM for the
+// 256 x 256 tile and 48 for 256 x 512.  Hence the largest tile that tensor memory holds, where there are enough tiles.
+// Warps have roles:
+//   0      fetches: 128 x 64 blocks of A and B by TMA into a ring of 32 KiB stages
 //   1      issues tcgen05.mma, one thread, four K = 16 steps a stage, accumulating in tensor memory
-//   2..5   epilogue: accumulators from tensor memory, 32 rows a warp, the elementwise work, and the results through
+//   2..9   epilogue: accumulators from tensor memory, 32 rows a warp, the elementwise work, and the results through
 //          a small shared-memory ring and TMA to global memory
-// Two accumulators alternate, so that a tile's epilogue runs under the next tile's products.
+// Two accumulators alternate where both fit, so that a tile's epilogue runs under the next tile's products; 256 x 512
+// fills tensor memory, and its epilogue (a few thousand cycles to the products' 16 K) is waited for.
 //
-// Either side may lie along k (rows of 64 k) or across it (rows of 64 indices): both are 8 KiB boxes with the
-// 128-byte swizzle, only the descriptor's strides and the instruction's transpose bits differ, so the backward pass
+// Either side may lie along k (a 16 KiB box of 128 rows of 64 k) or across it (two 8 KiB boxes of 64 rows of 64
+// indices), both with the 128-byte swizzle: only the descriptor's strides and the instruction's transpose bits differ, so the backward pass
 // needs no transposed copies.  Several products (the backward pass has four) share one launch, and a product with
 // few tiles and a long k is cut along k.
+//
+// Binary32 blocks: an operand is three bf16 planes, and a product the six plane products that reach 2^-24.  The tensor
+// cores add to an accumulator with truncation, a bias of about 2^-24 of the running sum for every K = 16 step: 10^-5 at
+// K = 4096, harmless under the rounding of 16-bit results but not here.  So a stage holds all planes of 64 k (each is
+// fetched once for its products), the small products accumulate first, and after every stage the accumulator (one of
+// four) is added to registers with rounding.  Tile 256 x 128 by a pair: the registers' share of it fits.
 //
 // All waits are bounded: one that runs out sets g_wait_failed and the thread goes on without waiting.
 #include <cuda.h>
@@ -25,26 +36,23 @@
 
 namespace {
 
-constexpr int MAX_PRODUCTS = 4, MAX_SEGMENTS = 12;
-constexpr int STAGES = 6, STAGE_BYTES = 32768, BOX_BYTES = 8192;
+constexpr int MAX_PRODUCTS = 4;
+constexpr int BLOCK_BYTES = 16384, BOX_BYTES = 8192;    // 128 x 64 of an operand; half of it
+constexpr int FETCH_BYTES = 12 * BLOCK_BYTES;           // ring of fetched blocks
 constexpr int BLOCK_K = 64;
-constexpr int THREADS = 192, EPI_WARPS = 4;
-constexpr int RING_SLOT = 4096, RING_SLOTS = 2;
-constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_WARPS * RING_SLOT * RING_SLOTS + 1024 + 256;
+constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
+constexpr int RING_SLOT = 2048, RING_SLOTS = 2;         // 32 rows of 64 bytes
+constexpr int SMEM_BYTES = FETCH_BYTES + EPI_WARPS * RING_SLOT * RING_SLOTS + 1024 + 256;
 constexpr int WAIT_LIMIT = 1 << 20;
 
 __device__ int g_wait_failed;
 
-struct Segment {
-    uint8_t a, b, za, zb;       // which maps and planes
-};
 struct alignas(64) Problem {
     CUtensorMap a[2], b[2], c[2];
-    Segment seg[MAX_SEGMENTS];
     void *cp;                   // STORE without TMA
     long long ldc, split_stride;
     float *h, *u;
-    int M, N, tiles_m, tiles_n, splits, first, kblocks, segments;
+    int M, N, tiles_m, tiles_n, splits, first, kblocks, terms;
     int a_across, b_across, c_f32, c_tma, planes, act, groups;
     uint32_t idesc;
 };
@@ -160,13 +168,13 @@ __device__ __forceinline__ Tile tile_of(const Work &w, int item) {
     i -= band * 8 * p.tiles_n;
     t.n = i / rows;
     t.m = band * 8 + i - t.n * rows;
-    const long long its = (long long)p.kblocks * p.segments;
+    const long long its = (long long)p.kblocks * p.terms;
     t.it0 = (int)(its * t.split / p.splits);
     t.it1 = (int)(its * (t.split + 1) / p.splits);
     return t;
 }
 
-// The epilogue warps' way out: 32 rows x 32 columns a slot, swizzled so that the row writes meet no bank conflict.
+// The epilogue warps' way out: 32 rows of 64 bytes a slot, swizzled so that the row writes meet no bank conflict.
 struct Ring {
     char *base;
     int slot;
@@ -185,17 +193,14 @@ __device__ __forceinline__ void out_by_tma(const CUtensorMap *map, int x, int y,
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
 }
-__device__ __forceinline__ char *slot16(char *slot, int row, int chunk) {       // 64-byte rows
+__device__ __forceinline__ char *slot_at(char *slot, int row, int chunk) {      // 16 bytes of a row of 64
     return slot + row * 64 + ((chunk ^ (row >> 1 & 3)) << 4);
-}
-__device__ __forceinline__ char *slot32(char *slot, int row, int chunk) {       // 128-byte rows
-    return slot + row * 128 + ((chunk ^ (row & 7)) << 4);
 }
 template <class T>
 __device__ __forceinline__ void put16(char *slot, int row, const float (&f)[32]) {
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        *reinterpret_cast<uint4 *>(slot16(slot, row, c)) =
+        *reinterpret_cast<uint4 *>(slot_at(slot, row, c)) =
             make_uint4(pack2<T>(f[8 * c], f[8 * c + 1]), pack2<T>(f[8 * c + 2], f[8 * c + 3]),
                        pack2<T>(f[8 * c + 4], f[8 * c + 5]), pack2<T>(f[8 * c + 6], f[8 * c + 7]));
 }
@@ -219,24 +224,117 @@ __device__ __forceinline__ void emit(const Problem &p, const CUtensorMap *map, i
     }
 }
 
-template <int CG, int EPI>
+// The values of a tile that leave as they are: 32 columns from `col` on.
+__device__ __forceinline__ void store_columns(const Problem &p, int f16, const float (&f)[32], int col, int row0, int split,
+                                              int lane, Ring &ring) {
+    const int width = p.c_f32 ? 16 : 32;            // columns of a slot
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (half && !p.c_f32) break;
+        const int at = col + 16 * half;
+        if (at >= p.N) break;
+        char *slot = ring.next(lane);
+        if (p.c_f32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4 *>(slot_at(slot, lane, i)) = make_float4(
+                    f[16 * half + 4 * i], f[16 * half + 4 * i + 1], f[16 * half + 4 * i + 2], f[16 * half + 4 * i + 3]);
+        } else if (f16) {
+            put16<fp16>(slot, lane, f);
+        } else {
+            put16<bf16>(slot, lane, f);
+        }
+        if (p.c_tma) {
+            out_by_tma(&p.c[0], at, row0, split, slot, lane);
+            continue;
+        }
+        // rows that TMA cannot address: a row (binary32: two) at a time, neighbouring threads neighbouring words
+        __syncwarp();
+        const int c = lane & (width - 1), step = 32 / width;
+        const int end = min(32, p.M - row0);
+        if (at + c < p.N)
+            for (int r = lane / width; r < end; r += step) {
+                const long long to = split * p.split_stride + (row0 + r) * p.ldc + at + c;
+                if (p.c_f32)
+                    static_cast<float *>(p.cp)[to] = *reinterpret_cast<float *>(slot_at(slot, r, c >> 2) + (c & 3) * 4);
+                else
+                    static_cast<uint16_t *>(p.cp)[to] = *reinterpret_cast<uint16_t *>(slot_at(slot, r, c >> 3) + (c & 7) * 2);
+            }
+        __syncwarp();
+    }
+}
+// h and u of 32 columns of this thread's row
+__device__ __forceinline__ void load_saved(const Problem &p, long long block, int col, int lane, float4 (&h)[8], float4 (&u)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        h[i] = u[i] = make_float4(0, 0, 0, 0);
+        if ((col >> 2) + i < p.groups) {
+            const long long at = (block + (col >> 2) + i) * 32 + lane;
+            h[i] = reinterpret_cast<const float4 *>(p.h)[at];
+            u[i] = reinterpret_cast<const float4 *>(p.u)[at];
+        }
+    }
+}
+template <bool EXACT>
+__device__ __forceinline__ void gate_columns(const Problem &p, int f16, float (&h)[32], float (&u)[32], long long block, int col,
+                                             int row0, int lane, Ring &ring) {
+    if (p.h) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((col >> 2) + i < p.groups) {
+                const long long at = (block + (col >> 2) + i) * 32 + lane;
+                reinterpret_cast<float4 *>(p.h)[at] = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+                reinterpret_cast<float4 *>(p.u)[at] = make_float4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+            }
+    }
+    act_apply<EXACT>(p.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float slope;
+            u[i] *= act(h[i], &slope);
+        }
+    });
+    emit(p, &p.c[0], f16, u, col, row0, lane, ring);
+}
+// d (da on entry) becomes dh, du the other
+template <bool EXACT>
+__device__ __forceinline__ void gate_back_columns(const Problem &p, float (&d)[32], float (&du)[32], const float4 (&h)[8],
+                                                  const float4 (&u)[8]) {
+    act_apply<EXACT>(p.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float4 hv = h[i >> 2], uv = u[i >> 2];
+            const float x = (i & 3) == 0 ? hv.x : (i & 3) == 1 ? hv.y : (i & 3) == 2 ? hv.z : hv.w;
+            const float y = (i & 3) == 0 ? uv.x : (i & 3) == 1 ? uv.y : (i & 3) == 2 ? uv.z : uv.w;
+            float slope;
+            du[i] = d[i] * act(x, &slope);
+            d[i] *= y * slope;
+        }
+    });
+}
+// CG SMs to a tile of 128 CG rows and 128 CG NB columns.  PLANES: binary32 blocks, see above; 256 rows, 128 columns.
+template <int CG, int NB, int EPI, bool PLANES>
 __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ Work w) {
     extern __shared__ char smem_raw[];
-    constexpr int TILE_M = 128 * CG, TILE_N = 128 * CG;
-    constexpr uint32_t TMEM_COLUMNS = 2 * TILE_N;
+    constexpr int HALF_N = PLANES ? 128 : 128 * CG, TILE_M = 128 * CG, TILE_N = HALF_N * NB;
+    constexpr int STAGE_BYTES = PLANES ? 3 * (BLOCK_BYTES + BOX_BYTES) : (1 + NB) * BLOCK_BYTES;
+    constexpr int B_AT = PLANES ? 3 * BLOCK_BYTES : BLOCK_BYTES;    // A's blocks come first
+    constexpr int STAGES = FETCH_BYTES / STAGE_BYTES;
+    constexpr int ACCS = PLANES ? 4 : 512 / TILE_N < 2 ? 1 : 2;     // accumulators in tensor memory
+    constexpr uint32_t TMEM_COLUMNS = ACCS * TILE_N;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank = 0;
     if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    char *ring_base = smem + STAGES * STAGE_BYTES;
+    char *ring_base = smem + FETCH_BYTES;
     uint64_t *bars = reinterpret_cast<uint64_t *>(ring_base + EPI_WARPS * RING_SLOT * RING_SLOTS);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * STAGES + 4);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * STAGES + 8);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 32;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, EPI_WARPS * CG);
+        for (int i = 0; i < ACCS; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, EPI_WARPS * CG);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -264,165 +362,114 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
     int limit = WAIT_LIMIT;
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t n = 0;
+            const uint32_t ring = smem_u32(smem), first_full = CG == 2 ? in_first(full) : full;
+            uint32_t stage = 0, phase = 0;
             for (int item = cluster; item < w.items; item += clusters) {
                 const Tile t = tile_of(w, item);
                 const Problem &p = w.p[t.problem];
                 const int am = t.m * TILE_M + 128 * (int)rank;
-                int seg = t.it0 / p.kblocks, kb = t.it0 - seg * p.kblocks;
-                for (int it = t.it0; it < t.it1; ++it, ++n) {
-                    const uint32_t s = n % STAGES, turn = n / STAGES;
-                    bar_wait<CG>(empty + 8 * s, (turn & 1) ^ 1, limit);
-                    const uint32_t bar = CG == 2 ? in_first(full + 8 * s) : full + 8 * s;
-                    if (rank == 0) bar_expect(full + 8 * s, CG * STAGE_BYTES);
-                    const uint32_t dst = smem_u32(smem + s * STAGE_BYTES);
-                    const Segment g = p.seg[seg];
-                    const int k = kb * BLOCK_K;
+                // The tile's B: halves of HALF_N columns, each half's 128 CG rows shared out over the blocks.  GATE: the
+                // first half of the columns is h's, the second u's; with one half, its blocks (or boxes) are.
+                const bool a_across = p.a_across, b_across = p.b_across;
+                for (int it = t.it0; it < t.it1;) {
+                    const int term = it / p.kblocks, end = min(t.it1, (term + 1) * p.kblocks);
+                    const CUtensorMap *ma = &p.a[term];
+                    const CUtensorMap *mb = &p.b[EPI != MMA_GATE ? term : NB == 1 && CG == 2 ? (int)rank : 0];
+                    const int bn = EPI != MMA_GATE ? t.n * TILE_N + HALF_N / CG * (int)rank
+                                                   : t.n * (TILE_N / 2) + (NB == 2 ? 128 * (int)rank : 0);
+                    for (int k = (it - term * p.kblocks) * BLOCK_K; it < end; ++it, k += BLOCK_K) {
+                        bar_wait<CG>(empty + 8 * stage, phase ^ 1, limit);
+                        const uint32_t bar = first_full + 8 * stage, dst = ring + stage * STAGE_BYTES;
+                        if (rank == 0) bar_expect(full + 8 * stage, CG * STAGE_BYTES);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int r = am + 64 * i;
-                        tma_load<CG>(dst + i * BOX_BYTES, &p.a[g.a], p.a_across ? r : k, p.a_across ? k : r, g.za, bar);
-                    }
+                        for (int z = 0; z < (PLANES ? 3 : 1); ++z) {
+                            const uint32_t to = dst + z * BLOCK_BYTES;
+                            if (!a_across) {
+                                tma_load<CG>(to, ma, k, am, z, bar);
+                            } else {
+                                tma_load<CG>(to, ma, am, k, z, bar);
+                                tma_load<CG>(to + BOX_BYTES, ma, am + 64, k, z, bar);
+                            }
+                        }
+                        if constexpr (PLANES) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        // GATE: the tile's first half of columns is h's, the second u's
-                        const int which = EPI != MMA_GATE ? g.b : CG == 2 ? (int)rank : i;
-                        const int r = EPI != MMA_GATE ? t.n * TILE_N + 128 * (int)rank + 64 * i
-                                                      : t.n * (TILE_N / 2) + (CG == 2 ? 64 * i : 0);
-                        tma_load<CG>(dst + (2 + i) * BOX_BYTES, &p.b[which], p.b_across ? r : k, p.b_across ? k : r, g.zb, bar);
+                            for (int z = 0; z < 3; ++z)
+                                tma_load<CG>(dst + B_AT + z * BOX_BYTES, mb, b_across ? bn : k, b_across ? k : bn, z, bar);
+                        } else if constexpr (EPI == MMA_GATE && CG == 1 && NB == 1) {
+                            tma_load<CG>(dst + B_AT, mb, k, bn, 0, bar);
+                            tma_load<CG>(dst + B_AT + BOX_BYTES, mb + 1, k, bn, 0, bar);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < NB; ++j) {
+                                const CUtensorMap *m = EPI == MMA_GATE ? mb + j : mb;
+                                const int n = EPI == MMA_GATE ? bn : bn + HALF_N * j;
+                                const uint32_t to = dst + B_AT + j * BLOCK_BYTES;
+                                if (!b_across) {
+                                    tma_load<CG>(to, m, k, n, 0, bar);
+                                } else {
+                                    tma_load<CG>(to, m, n, k, 0, bar);
+                                    tma_load<CG>(to + BOX_BYTES, m, n + 64, k, 0, bar);
+                                }
+                            }
+                        }
+                        if (++stage == STAGES) stage = 0, phase ^= 1;
                     }
-                    if (++kb == p.kblocks) kb = 0, ++seg;
                 }
             }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t n = 0, tiles = 0;
-            for (int item = cluster; item < w.items; item += clusters, ++tiles) {
+            uint32_t stage = 0, phase = 0, sums = 0;
+            for (int item = cluster; item < w.items; item += clusters) {
                 const Tile t = tile_of(w, item);
                 const Problem &p = w.p[t.problem];
-                const uint32_t acc = tiles & 1, d = tmem + acc * TILE_N;
-                bar_wait<CG>(acc_empty + 8 * acc, (tiles >> 1 & 1) ^ 1, limit);
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const int a_step = p.a_across ? 2048 >> 4 : 32 >> 4, b_step = p.b_across ? 2048 >> 4 : 32 >> 4;
-                for (int it = t.it0; it < t.it1; ++it, ++n) {
-                    const uint32_t s = n % STAGES;
-                    bar_wait<CG>(full + 8 * s, n / STAGES & 1, limit);
+                const uint32_t idesc = p.idesc;
+                const uint64_t a0 = operand_desc(smem_u32(smem), p.a_across);
+                const uint64_t b0 = operand_desc(smem_u32(smem) + B_AT, p.b_across);
+                const uint32_t a_step = p.a_across ? 2048 >> 4 : 32 >> 4, b_step = p.b_across ? 2048 >> 4 : 32 >> 4;
+                for (int it = t.it0; it < t.it1; ++sums) {
+                    const int end = PLANES ? it + 1 : t.it1;
+                    const uint32_t acc = sums % ACCS, d = tmem + acc * TILE_N;
+                    bar_wait<CG>(acc_empty + 8 * acc, (sums / ACCS & 1) ^ 1, limit);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t at = smem_u32(smem + s * STAGE_BYTES);
-                    const uint64_t a = operand_desc(at, p.a_across), b = operand_desc(at + 2 * BOX_BYTES, p.b_across);
+                    bool add = false;
+                    for (; it < end; ++it) {
+                        bar_wait<CG>(full + 8 * stage, phase, limit);
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t a = a0 + stage * (STAGE_BYTES >> 4), b = b0 + stage * (STAGE_BYTES >> 4);
+                        if constexpr (PLANES) {
+                            // plane products, the small ones first: lo hi, hi lo, mid mid, mid hi, hi mid, hi hi
+                            constexpr int order[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma<CG>(d, a + k * a_step, b + k * b_step, p.idesc, it > t.it0 || k > 0);
-                    mma_commit<CG>(empty + 8 * s);
+                            for (int i = 0; i < 6; ++i)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    mma<CG>(d, a + order[i][0] * (BLOCK_BYTES >> 4) + k * a_step,
+                                            b + order[i][1] * (BOX_BYTES >> 4) + k * b_step, idesc, add);
+                                    add = true;
+                                }
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                                for (int j = 0; j < NB; ++j)
+                                    mma<CG>(d + j * HALF_N, a + k * a_step, b + j * (BLOCK_BYTES >> 4) + k * b_step, idesc, add);
+                                add = true;
+                            }
+                        }
+                        mma_commit<CG>(empty + 8 * stage);
+                        if (++stage == STAGES) stage = 0, phase ^= 1;
+                    }
+                    mma_commit<CG>(acc_full + 8 * acc);
                 }
-                mma_commit<CG>(acc_full + 8 * acc);
             }
         }
     } else {
-        const int quarter = warp & 3;       // the tensor-memory lanes a warp may read
+        const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
+        const int part = (warp - 2) >> 2;           // two warps a quarter: each takes half of the columns
         Ring ring = {ring_base + (warp - 2) * RING_SLOT * RING_SLOTS, 0};
-        uint32_t tiles = 0;
-        for (int item = cluster; item < w.items; item += clusters, ++tiles) {
-            const Tile t = tile_of(w, item);
-            const Problem &p = w.p[t.problem];
-            const uint32_t acc = tiles & 1;
-            const int row0 = t.m * TILE_M + 128 * (int)rank + 32 * quarter;
-            const uint32_t from = tmem + acc * TILE_N + ((uint32_t)(32 * quarter) << 16);
-            const bool rows = row0 < p.M;
-            const int col0 = t.n * (EPI == MMA_GATE ? TILE_N / 2 : TILE_N);
-            const long long block = (long long)(row0 >> 5) * p.groups;
-            bar_wait<CG>(acc_full + 8 * acc, tiles >> 1 & 1, limit);
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            if constexpr (EPI == MMA_STORE) {
-                for (int c = 0; c < TILE_N; c += 32) {
-                    const int col = col0 + c;
-                    if (!rows || col >= p.N) break;
-                    float f[32];
-                    tmem_load(from + c, f);
-                    tmem_wait();
-                    char *slot = ring.next(lane);
-                    if (p.c_f32) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            *reinterpret_cast<float4 *>(slot32(slot, lane, i)) =
-                                make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-                    } else if (w.f16) {
-                        put16<fp16>(slot, lane, f);
-                    } else {
-                        put16<bf16>(slot, lane, f);
-                    }
-                    if (p.c_tma) {
-                        out_by_tma(&p.c[0], col, row0, t.split, slot, lane);
-                    } else {        // rows that TMA cannot address: a row at a time, neighbouring threads neighbouring words
-                        __syncwarp();
-                        if (col + lane < p.N) {
-                            const long long at = t.split * p.split_stride + (long long)row0 * p.ldc + col + lane;
-                            const int end = min(32, p.M - row0);
-                            for (int r = 0; r < end; ++r) {
-                                if (p.c_f32)
-                                    static_cast<float *>(p.cp)[at + r * p.ldc] =
-                                        *reinterpret_cast<float *>(slot32(slot, r, lane >> 2) + (lane & 3) * 4);
-                                else
-                                    static_cast<uint16_t *>(p.cp)[at + r * p.ldc] =
-                                        *reinterpret_cast<uint16_t *>(slot16(slot, r, lane >> 3) + (lane & 7) * 2);
-                            }
-                        }
-                        __syncwarp();
-                    }
-                }
-            } else if constexpr (EPI == MMA_GATE) {
-                for (int c = 0; c < TILE_N / 2; c += 32) {
-                    const int col = col0 + c;
-                    if (!rows || col >= p.N) break;
-                    float h[32], u[32];
-                    tmem_load(from + c, h);
-                    tmem_load(from + TILE_N / 2 + c, u);
-                    tmem_wait();
-                    if (p.h) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if ((col >> 2) + i < p.groups) {
-                                const long long at = (block + (col >> 2) + i) * 32 + lane;
-                                reinterpret_cast<float4 *>(p.h)[at] = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
-                                reinterpret_cast<float4 *>(p.u)[at] = make_float4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
-                            }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        float slope;
-                        u[i] *= act_value(p.act, h[i], &slope);
-                    }
-                    emit(p, &p.c[0], w.f16, u, col, row0, lane, ring);
-                }
-            } else {
-                for (int c = 0; c < TILE_N; c += 32) {
-                    const int col = col0 + c;
-                    if (!rows || col >= p.N) break;
-                    float d[32], h[32], u[32];
-                    tmem_load(from + c, d);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float4 a = make_float4(0, 0, 0, 0), b = a;
-                        if ((col >> 2) + i < p.groups) {
-                            const long long at = (block + (col >> 2) + i) * 32 + lane;
-                            a = reinterpret_cast<const float4 *>(p.h)[at];
-                            b = reinterpret_cast<const float4 *>(p.u)[at];
-                        }
-                        h[4 * i] = a.x, h[4 * i + 1] = a.y, h[4 * i + 2] = a.z, h[4 * i + 3] = a.w;
-                        u[4 * i] = b.x, u[4 * i + 1] = b.y, u[4 * i + 2] = b.z, u[4 * i + 3] = b.w;
-                    }
-                    tmem_wait();
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        float slope;
-                        const float v = act_value(p.act, h[i], &slope);
-                        h[i] = d[i] * u[i] * slope;
-                        u[i] = d[i] * v;
-                    }
-                    emit(p, &p.c[0], w.f16, h, col, row0, lane, ring);
-                    emit(p, &p.c[1], w.f16, u, col, row0, lane, ring);
-                }
-            }
+        uint32_t sums = 0;
+        auto release = [&](uint32_t acc) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
@@ -430,6 +477,81 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                     bar_arrive_cluster(in_first(acc_empty + 8 * acc));
                 else
                     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
+            }
+        };
+        constexpr int COLS = EPI == MMA_GATE ? TILE_N / 2 : TILE_N;     // output columns of a tile
+        for (int item = cluster; item < w.items; item += clusters) {
+            const Tile t = tile_of(w, item);
+            const Problem &p = w.p[t.problem];
+            const int row0 = t.m * TILE_M + 128 * (int)rank + 32 * quarter;
+            const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+            const bool rows = row0 < p.M;
+            const int col0 = t.n * COLS + part * (COLS / 2), col1 = min(p.N, col0 + COLS / 2);
+            const long long block = (long long)(row0 >> 5) * p.groups;
+            if constexpr (!PLANES) {
+                const uint32_t acc = sums % ACCS, from = tmem + acc * TILE_N + part * (COLS / 2) + lanes;
+                float4 h[8], u[8];
+                if (EPI == MMA_GATE_BACK && rows && col0 < col1) load_saved(p, block, col0, lane, h, u);
+                bar_wait<CG>(acc_full + 8 * acc, sums / ACCS & 1, limit);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int c = 0; rows && col0 + c < col1; c += 32) {
+                    float f[32];
+                    tmem_load(from + c, f);
+                    if constexpr (EPI == MMA_STORE) {
+                        tmem_wait();
+                        store_columns(p, w.f16, f, col0 + c, row0, t.split, lane, ring);
+                    } else if constexpr (EPI == MMA_GATE) {
+                        float g[32];
+                        tmem_load(from + COLS + c, g);
+                        tmem_wait();
+                        gate_columns<false>(p, w.f16, f, g, block, col0 + c, row0, lane, ring);
+                    } else {
+                        tmem_wait();
+                        float g[32];
+                        gate_back_columns<false>(p, f, g, h, u);
+                        if (col0 + c + 32 < col1) load_saved(p, block, col0 + c + 32, lane, h, u);     // on their way during the stores
+                        emit(p, &p.c[0], w.f16, f, col0 + c, row0, lane, ring);
+                        emit(p, &p.c[1], w.f16, g, col0 + c, row0, lane, ring);
+                    }
+                }
+                release(acc);
+                ++sums;
+            } else {
+                // this warp's 64 columns: GATE 32 of h and the 32 of u that belong to them
+                constexpr int SECOND = EPI == MMA_GATE ? TILE_N / 2 : 32;
+                float f[2][32] = {};
+                for (int it = t.it0; it < t.it1; ++it, ++sums) {
+                    const uint32_t acc = sums % ACCS, from = tmem + acc * TILE_N + part * (COLS / 2) + lanes;
+                    bar_wait<CG>(acc_full + 8 * acc, sums / ACCS & 1, limit);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    float v[2][32];
+                    tmem_load(from, v[0]);
+                    tmem_load(from + SECOND, v[1]);
+                    tmem_wait();
+                    release(acc);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[0][i] += v[0][i], f[1][i] += v[1][i];
+                }
+                if (rows && col0 < col1) {
+                    if constexpr (EPI == MMA_GATE) {
+                        gate_columns<true>(p, w.f16, f[0], f[1], block, col0, row0, lane, ring);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            if (col0 + 32 * j >= col1) break;
+                            if constexpr (EPI == MMA_STORE) {
+                                store_columns(p, w.f16, f[j], col0 + 32 * j, row0, t.split, lane, ring);
+                            } else {
+                                float4 h[8], u[8];
+                                load_saved(p, block, col0 + 32 * j, lane, h, u);
+                                float g[32];
+                                gate_back_columns<true>(p, f[j], g, h, u);
+                                emit(p, &p.c[0], w.f16, f[j], col0 + 32 * j, row0, lane, ring);
+                                emit(p, &p.c[1], w.f16, g, col0 + 32 * j, row0, lane, ring);
+                            }
+                        }
+                    }
+                }
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -484,9 +606,10 @@ bool encode(CUtensorMap *map, int type, const void *p, long long cols, long long
                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, int EPI>
+template <int CG, int NB, int EPI, bool PLANES>
 int launch(const Work &w, int sms, cudaStream_t s) {
-    cudaError_t e = cudaFuncSetAttribute(k_ffn_mma<CG, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    auto *kernel = k_ffn_mma<CG, NB, EPI, PLANES>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
     if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min(w.items, std::max(1, sms / CG)) * CG));
@@ -500,20 +623,27 @@ int launch(const Work &w, int sms, cudaStream_t s) {
     at[1].val.clusterDim.x = CG, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, k_ffn_mma<CG, EPI>, w);
+    e = cudaLaunchKernelEx(&cfg, kernel, w);
     if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
     ccdc_internal_count_launch();
     return CCDC_OK;
 }
+template <int EPI>
+int launch_tile(const Work &w, MmaTile tile, int sms, cudaStream_t s) {
+    return tile == MMA_PLANES ? launch<2, 1, EPI, true>(w, sms, s)
+           : tile == MMA_WIDE ? launch<2, 2, EPI, false>(w, sms, s)
+           : tile == MMA_PAIR ? launch<2, 1, EPI, false>(w, sms, s) : launch<1, 1, EPI, false>(w, sms, s);
+}
 
 }  // namespace
 
-int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int type, bool pair, int sms, cudaStream_t s) {
+int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int type, MmaTile shape, int sms, cudaStream_t s) {
     if (count < 1) return CCDC_OK;
     if (!encoder()) return CCDC_ECUDA;
     static thread_local Work w;
     w.count = count, w.items = 0, w.f16 = type == CCDC_F16;
-    const int tile = pair ? 256 : 128, tile_n = epilogue == MMA_GATE ? tile / 2 : tile;
+    const bool halves = shape == MMA_PLANES || (epilogue == MMA_GATE && shape == MMA_SINGLE);      // boxes of 64 B rows
+    const int tile = mma_tile_rows(shape), tile_n = mma_tile_columns(shape) / (epilogue == MMA_GATE ? 2 : 1);
     for (int i = 0; i < count; ++i) {
         const MmaProduct &q = products[i];
         Problem &p = w.p[i];
@@ -527,24 +657,19 @@ int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int 
         p.act = q.act, p.h = q.h, p.u = q.u, p.groups = (int)ffn_saved_groups(q.N);
         const uint32_t f = type == CCDC_BF16 ? 1 : 0;
         p.idesc = 1u << 4 | f << 7 | f << 10 | (uint32_t)p.a_across << 15 | (uint32_t)p.b_across << 16 |
-                  (uint32_t)(tile >> 3) << 17 | (uint32_t)(tile >> 4) << 24;
-        // terms, and within a term of three planes the six products that reach 2^-24, the small ones first
-        static const uint8_t order[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
-        const int planes = q.a[0].m.planes;
-        p.segments = 0;
-        for (int k = planes == 1 ? 5 : 0; k < 6; ++k)
-            for (int t = 0; t < q.terms; ++t) p.seg[p.segments++] = {(uint8_t)t, (uint8_t)t, order[k][0], order[k][1]};
+                  (uint32_t)((shape == MMA_PLANES ? 128 : tile) >> 3) << 17 | (uint32_t)(tile >> 4) << 24;
+        p.terms = q.terms;
         const int nb = epilogue == MMA_GATE ? 2 : q.terms;
         bool ok = true;
-        auto side = [&](CUtensorMap *map, const MmaSide &d) {
-            ok = ok && encode(map, type, d.m.p, d.m.cols, d.m.rows, d.m.ld, d.m.planes, 64, 64);
+        auto side = [&](CUtensorMap *map, const MmaSide &d, bool half) {
+            ok = ok && encode(map, type, d.m.p, d.m.cols, d.m.rows, d.m.ld, d.m.planes, 64, half ? 64 : 128);
         };
-        for (int t = 0; t < q.terms; ++t) side(&p.a[t], q.a[t]);
-        for (int t = 0; t < nb; ++t) side(&p.b[t], q.b[t]);
+        for (int t = 0; t < q.terms; ++t) side(&p.a[t], q.a[t], q.a[t].transposed);
+        for (int t = 0; t < nb; ++t) side(&p.b[t], q.b[t], q.b[t].transposed || halves);
         if (epilogue == MMA_STORE) {
             p.cp = q.c, p.ldc = q.ldc, p.split_stride = q.M * q.ldc, p.c_f32 = q.c_type == CCDC_F32, p.planes = 1;
             p.c_tma = aligned_to(q.c, 16) && q.ldc * type_bytes(q.c_type) % 16 == 0;
-            if (p.c_tma) ok = ok && encode(&p.c[0], q.c_type, q.c, q.N, q.M, q.ldc, p.splits, 32, 32);
+            if (p.c_tma) ok = ok && encode(&p.c[0], q.c_type, q.c, q.N, q.M, q.ldc, p.splits, p.c_f32 ? 16 : 32, 32);
         } else {
             p.planes = q.out[0].planes;
             for (int t = 0; t < (epilogue == MMA_GATE ? 1 : 2); ++t)
@@ -552,11 +677,9 @@ int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int 
         }
         if (!ok) return CCDC_ECUDA;
     }
-    if (pair)
-        return epilogue == MMA_STORE ? launch<2, MMA_STORE>(w, sms, s)
-               : epilogue == MMA_GATE ? launch<2, MMA_GATE>(w, sms, s) : launch<2, MMA_GATE_BACK>(w, sms, s);
-    return epilogue == MMA_STORE ? launch<1, MMA_STORE>(w, sms, s)
-           : epilogue == MMA_GATE ? launch<1, MMA_GATE>(w, sms, s) : launch<1, MMA_GATE_BACK>(w, sms, s);
+    return epilogue == MMA_STORE  ? launch_tile<MMA_STORE>(w, shape, sms, s)
+           : epilogue == MMA_GATE ? launch_tile<MMA_GATE>(w, shape, sms, s)
+                                  : launch_tile<MMA_GATE_BACK>(w, shape, sms, s);
 }
 
 extern "C" int ccdc_block_status(void) {

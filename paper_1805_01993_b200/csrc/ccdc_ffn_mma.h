@@ -17,7 +17,7 @@ struct MmaSide {
 };
 enum MmaEpilogue { MMA_STORE = 0, MMA_GATE = 1, MMA_GATE_BACK = 2 };
 
-// C = sum over terms of A_t B_t^T.  With three planes a side, a term is the six plane products that matter at 32 bits.
+// C = sum over terms of A_t B_t^T.
 // GATE: two B sides and one A: h = A B_0^T and u = A B_1^T.
 struct MmaProduct {
     long long M, N, K;
@@ -41,6 +41,13 @@ __host__ __device__ __forceinline__ long long ffn_saved_index(long long m, long 
 }
 __host__ __device__ __forceinline__ long long ffn_saved_groups(long long F) { return (F + 3) / 4; }
 
-// All products of a call go through one launch: `type` CCDC_BF16 or CCDC_F16; pair: two SMs to a 256 x 256 tile, else
-// one to a 128 x 128 tile.
-int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int type, bool pair, int sms, cudaStream_t s);
+// Tile shapes: two SMs to 256 x 512 or 256 x 256, one SM to 128 x 128; binary32 blocks: two SMs to 256 x 128.
+enum MmaTile { MMA_WIDE = 0, MMA_PAIR = 1, MMA_SINGLE = 2, MMA_PLANES = 3 };
+inline int mma_tile_rows(MmaTile t) { return t == MMA_SINGLE ? 128 : 256; }
+inline int mma_tile_columns(MmaTile t) {        // GATE: of h and u together
+    return t == MMA_WIDE ? 512 : t == MMA_PAIR ? 256 : 128;
+}
+
+// All products of a call go through one launch: `type` CCDC_BF16 or CCDC_F16.  Matrices of three planes take
+// MMA_PLANES, others one of the first three.
+int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int type, MmaTile tile, int sms, cudaStream_t s);
