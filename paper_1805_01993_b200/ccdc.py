@@ -493,80 +493,87 @@ class Plan:
 # on the stream the call runs on.
 
 
-def _block_dtype(t):
-    import torch
+# Small calls are bound by the host, so the checks compare plain integers and make no device or stream objects.
 
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+
+def _block_dtype(t):
+    """type code of a tensor; raises for types the block operators do not take."""
+    if not _BLOCK_TYPES:
+        import torch
+
+        _BLOCK_TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    code = _BLOCK_TYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"float32, bfloat16 or float16 expected, got {t.dtype}")
     return code
 
 
+_BLOCK_TYPES = {}
+
+
 def _rows(t, name, like=None, shape=None):
     """row stride of a 2-D tensor; raises where it is not what the call takes."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.size(1) > 1):
         raise ValueError(f"{name}: a 2-D tensor with contiguous columns expected")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+    if like is None:
+        if not t.is_cuda:
+            raise ValueError(f"{name}: a CUDA tensor expected")
+    elif t.dtype != like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: {like.dtype} on {like.device} expected, got {t.dtype} on {t.device}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: a CUDA tensor expected")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if t.size(0) > 1 else t.size(1)
 
 
-def _vector(t, name, like, n):
-    if t.numel() != n or not t.is_contiguous() or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name}: {n} contiguous {like.dtype} on {like.device} expected")
+def _vector(t, name, like, n, dtype=None):
+    """address of n contiguous values of like's (or the given) dtype."""
+    if t.numel() != n or not t.is_contiguous() or t.dtype != (dtype or like.dtype) or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: {n} contiguous {dtype or like.dtype} on {like.device} expected")
     return t.data_ptr()
 
 
-class _OnStream:
-    """makes the call's device and stream torch's current ones, for the allocations and the launch."""
-
-    def __init__(self, tensor, stream):
-        import torch
-
-        if stream is not None and stream.device != tensor.device:
-            raise ValueError("the stream belongs to another device than the tensors")
-        self.ctx = None
-        if stream is not None:
-            self.ctx = torch.cuda.stream(stream)
-        elif tensor.device.index != torch.cuda.current_device():
-            self.ctx = torch.cuda.device(tensor.device)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
-
-
-def _handle():
+def _elsewhere(x, stream):
+    """a context that makes the call's stream and device torch's current ones, or None where they already are."""
     import torch
 
-    return torch.cuda.current_stream().cuda_stream
+    if stream is not None:
+        if stream.device != x.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        return torch.cuda.stream(stream)
+    if x.is_cuda and x.get_device() != torch.cuda.current_device():
+        return torch.cuda.device(x.device)
+    return None
+
+
+def _handle(x):
+    """the current stream of x's device (which is the current device)."""
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
 
 
 def dropout(x, p, seed, offset=0, out=None, stream=None):
     """``ccdc_dropout``: x with elements dropped by the counter-based mask of (seed, offset + element).
     The backward pass is the same call on the gradient.  ``out`` may be ``x``."""
-    import torch
-
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return dropout(x, p, seed, offset, out)
     ldx = _rows(x, "x")
     code = _block_dtype(x)
-    with _OnStream(x, stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-        ldy = _rows(y, "out", x, x.shape)
-        _check(lib().ccdc_dropout(x.shape[0], x.shape[1], code, x.data_ptr(), ldx, y.data_ptr(), ldy, p, seed, offset,
-                                  _handle()), "ccdc_dropout")
-    return y
+    rows, cols = x.shape
+    if out is None:
+        out, ldy = x.new_empty((rows, cols)), cols
+    else:
+        ldy = _rows(out, "out", x, x.shape)
+    status = lib().ccdc_dropout(rows, cols, code, x.data_ptr(), ldx, out.data_ptr(), ldy, p, seed, offset, _handle(x))
+    if status:
+        _check(status, "ccdc_dropout")
+    return out
 
 
 def _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate):
-    M, D = x.shape
+    M, D = x.shape if x.dim() == 2 else (0, 0)
     ldx = _rows(x, "x")
     ldy = D if y is None else _rows(y, "y", x, x.shape)
     pw = None if w_post is None else _vector(w_post, "w_post", x, D)
@@ -586,22 +593,38 @@ def residual_norm_forward(x, y=None, *, w_post=None, w_pre=None, gate=None, rows
                           offset=0, kind="rms", eps=1e-5, save=False, out=None, z=None, stream=None):
     """``ccdc_residual_norm_forward``: out = alpha*x + drop(gate * norm(y)*w_post), z = norm(out)*w_pre.
     Returns (out, z), or (out, z, stats) with ``save``; z is None without ``w_pre``."""
-    import torch
-
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return residual_norm_forward(x, y, w_post=w_post, w_pre=w_pre, gate=gate, rows_per_gate=rows_per_gate,
+                                         alpha=alpha, p=p, seed=seed, offset=offset, kind=kind, eps=eps, save=save,
+                                         out=out, z=z)
     M, D, ldx, ldy, pw, pp, pg, per = _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate)
     code = _block_dtype(x)
-    with _OnStream(x, stream):
-        out = torch.empty((M, D), dtype=x.dtype, device=x.device) if out is None else out
-        if w_pre is not None:
-            z = torch.empty((M, D), dtype=x.dtype, device=x.device) if z is None else z
-        elif z is not None:
+    if out is None:
+        out, ldo = x.new_empty((M, D)), D
+    else:
+        ldo = _rows(out, "out", x, x.shape)
+    pz, ldz, stats, ps = None, D, None, None
+    if w_pre is None:
+        if z is not None:
             raise ValueError("z needs w_pre")
-        stats = torch.empty((M, 4), dtype=torch.float32, device=x.device) if save else None
-        _check(lib().ccdc_residual_norm_forward(
-            M, D, code, NORMS[kind], eps, x.data_ptr(), ldx, None if y is None else y.data_ptr(), ldy, pw, pp, pg, per,
-            alpha, p, seed, offset, out.data_ptr(), _rows(out, "out", x, x.shape),
-            None if z is None else z.data_ptr(), D if z is None else _rows(z, "z", x, x.shape),
-            stats.data_ptr() if save else None, _handle()), "ccdc_residual_norm_forward")
+    else:
+        if z is None:
+            z = x.new_empty((M, D))
+        else:
+            ldz = _rows(z, "z", x, x.shape)
+        pz = z.data_ptr()
+    if save:
+        import torch
+
+        stats = x.new_empty((M, 4), dtype=torch.float32)
+        ps = stats.data_ptr()
+    status = lib().ccdc_residual_norm_forward(M, D, code, NORMS[kind], eps, x.data_ptr(), ldx,
+                                              None if y is None else y.data_ptr(), ldy, pw, pp, pg, per, alpha, p, seed,
+                                              offset, out.data_ptr(), ldo, pz, ldz, ps, _handle(x))
+    if status:
+        _check(status, "ccdc_residual_norm_forward")
     return (out, z, stats) if save else (out, z)
 
 
@@ -612,51 +635,65 @@ def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, ga
     ``dout`` or ``dz`` may be None (zero).  ``eps`` is accepted for symmetry; the forward's is in ``stats``."""
     import torch
 
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return residual_norm_backward(dout, dz, x, y, stats, w_post=w_post, w_pre=w_pre, gate=gate,
+                                          rows_per_gate=rows_per_gate, alpha=alpha, p=p, seed=seed, offset=offset,
+                                          kind=kind, grad_dtype=grad_dtype, dx=dx, dy=dy, dw_post=dw_post, dw_pre=dw_pre,
+                                          dgate=dgate, workspace=workspace)
     M, D, ldx, ldy, pw, pp, pg, per = _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate)
-    code, like = _block_dtype(x), x
+    code = _block_dtype(x)
     gt = x.dtype if grad_dtype is None else grad_dtype
-    if gt not in (x.dtype, torch.float32):
+    if gt != x.dtype and gt != torch.float32:
         raise TypeError("grad_dtype is the tensors' dtype or float32")
-    if tuple(stats.shape) != (M, 4) or stats.dtype != torch.float32 or not stats.is_contiguous() or stats.device != x.device:
-        raise ValueError("stats: what residual_norm_forward(save=True) returned expected")
-    with _OnStream(x, stream):
-        def empty(t, wanted, shape, dtype, name):
-            if not wanted:
-                if t is not None:
-                    raise ValueError(f"{name}: the forward call has no such input")
-                return None
-            if t is None:
-                return torch.empty(shape, dtype=dtype, device=x.device)
-            if t.device != x.device or t.dtype != dtype or (name[:2] == "dw" or name == "dgate") and (
-                    not t.is_contiguous() or t.numel() != (D if name[:2] == "dw" else gate.numel())):
-                raise ValueError(f"{name}: {tuple(shape)} {dtype} on {x.device} expected")
-            return t
+    ps = _vector(stats, "stats (of residual_norm_forward with save)", x, 4 * M, torch.float32)
 
-        dx = empty(dx, True, (M, D), x.dtype, "dx")
-        dy = empty(dy, y is not None, (M, D), x.dtype, "dy")
-        dw_post = empty(dw_post, w_post is not None, (D,), gt, "dw_post")
-        dw_pre = empty(dw_pre, w_pre is not None, (D,), gt, "dw_pre")
-        dgate = empty(dgate, gate is not None, None if gate is None else gate.shape, gt, "dgate")
-        need = lib().ccdc_residual_norm_workspace_bytes(M, D)
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    def given(t, name):
+        return (None, D) if t is None else (t.data_ptr(), _rows(t, name, x, x.shape))
 
-        def ptr(t):
-            return None if t is None else t.data_ptr()
+    def rows_out(t, name):
+        if t is None:
+            t = x.new_empty((M, D))
+            return t, t.data_ptr(), D
+        return t, t.data_ptr(), _rows(t, name, x, x.shape)
 
-        def ld(t, name):
-            return D if t is None else _rows(t, name, like, like.shape)
+    def param_out(t, of, name):
+        if of is None:
+            if t is not None:
+                raise ValueError(f"{name}: the forward call has no such input")
+            return None, None
+        if t is None:
+            t = x.new_empty(of.shape, dtype=gt)
+            return t, t.data_ptr()
+        return t, _vector(t, name, x, of.numel(), gt)
 
-        _check(lib().ccdc_residual_norm_backward(
-            M, D, code, F32 if gt == torch.float32 else code, NORMS[kind], ptr(dout), ld(dout, "dout"), ptr(dz), ld(dz, "dz"),
-            x.data_ptr(), ldx, ptr(y), ldy, stats.data_ptr(), pw, pp, pg, per, alpha, p, seed, offset,
-            dx.data_ptr(), ld(dx, "dx"), ptr(dy), ld(dy, "dy"), ptr(dw_post), ptr(dw_pre), ptr(dgate),
-            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle()), "ccdc_residual_norm_backward")
+    po, ldo = given(dout, "dout")
+    pz, ldz = given(dz, "dz")
+    dx, pdx, lddx = rows_out(dx, "dx")
+    if y is None:
+        if dy is not None:
+            raise ValueError("dy: the forward call has no such input")
+        pdy, lddy = None, D
+    else:
+        dy, pdy, lddy = rows_out(dy, "dy")
+    dw_post, p1 = param_out(dw_post, w_post, "dw_post")
+    dw_pre, p2 = param_out(dw_pre, w_pre, "dw_pre")
+    dgate, p3 = param_out(dgate, gate, "dgate")
+    L = lib()
+    if workspace is None:
+        workspace = x.new_empty(L.ccdc_residual_norm_workspace_bytes(M, D), dtype=torch.uint8)
+    status = L.ccdc_residual_norm_backward(
+        M, D, code, F32 if gt == torch.float32 else code, NORMS[kind], po, ldo, pz, ldz, x.data_ptr(), ldx,
+        None if y is None else y.data_ptr(), ldy, ps, pw, pp, pg, per, alpha, p, seed, offset, pdx, lddx, pdy, lddy,
+        p1, p2, p3, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle(x))
+    if status:
+        _check(status, "ccdc_residual_norm_backward")
     return dx, dy, dw_post, dw_pre, dgate
 
 
 def _ffn_tensors(x, w_gate, w_up, w_down):
-    M, D = x.shape
+    M, D = x.shape if x.dim() == 2 else (0, 0)
     F = w_gate.shape[0]
     ldx = _rows(x, "x")
     ldw = _rows(w_gate, "w_gate", x, (F, D))
@@ -665,11 +702,13 @@ def _ffn_tensors(x, w_gate, w_up, w_down):
     return M, D, F, ldx, ldw, _rows(w_down, "w_down", x, (D, F))
 
 
-def _ffn_aligned(size, D, F, tensors):
-    """whether every pointer and row stride is a multiple of 16 bytes"""
-    if D * size % 16 or F * size % 16:
-        return 0
-    return int(all(t.data_ptr() % 16 == 0 and (t.shape[0] < 2 or t.stride(0) * size % 16 == 0) for t in tensors))
+def _ffn_aligned(size, *values):
+    """whether these addresses (given in bytes) and lengths (given in elements) are multiples of 16 bytes"""
+    addresses, lengths = 0, 0
+    for address, length in values:
+        addresses |= address
+        lengths |= length
+    return int(addresses % 16 == 0 and lengths * size % 16 == 0)
 
 
 def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved=None, workspace=None, stream=None):
@@ -677,22 +716,33 @@ def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved
     ``saved`` is opaque and goes to ``ffn_backward``."""
     import torch
 
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return ffn_forward(x, w_gate, w_up, w_down, act, save, out, saved, workspace)
     M, D, F, ldx, ldw, ldd = _ffn_tensors(x, w_gate, w_up, w_down)
     code, L = _block_dtype(x), lib()
-    with _OnStream(x, stream):
-        y = torch.empty((M, D), dtype=x.dtype, device=x.device) if out is None else out
-        ldy = _rows(y, "out", x, x.shape)
-        if save and saved is None:
-            saved = torch.empty(L.ccdc_ffn_saved_bytes(M, F, code), dtype=torch.uint8, device=x.device)
-        if workspace is None:
-            aligned = _ffn_aligned(x.element_size(), D, F, (x, w_gate, w_up, w_down, y))
-            workspace = torch.empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 0, aligned), dtype=torch.uint8,
-                                    device=x.device)
-        _check(L.ccdc_ffn_forward(M, D, F, code, ACTS[act], x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), ldw,
-                                  w_down.data_ptr(), ldd, y.data_ptr(), ldy, saved.data_ptr() if save else None,
-                                  workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle()),
-               "ccdc_ffn_forward")
-    return (y, saved) if save else y
+    if out is None:
+        out, ldy = x.new_empty((M, D)), D
+    else:
+        ldy = _rows(out, "out", x, x.shape)
+    ptrs = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), out.data_ptr()
+    psaved = None
+    if save:
+        need = L.ccdc_ffn_saved_bytes(M, F, code)
+        if saved is None:
+            saved = x.new_empty(need, dtype=torch.uint8)
+        elif saved.numel() * saved.element_size() < need or saved.get_device() != x.get_device():
+            raise ValueError(f"saved: {need} bytes on {x.device} expected")
+        psaved = saved.data_ptr()
+    if workspace is None:
+        aligned = _ffn_aligned(x.element_size(), *zip(ptrs, (ldx, ldw, D, ldd, ldy)), (0, F))
+        workspace = x.new_empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 0, aligned), dtype=torch.uint8)
+    status = L.ccdc_ffn_forward(M, D, F, code, ACTS[act], ptrs[0], ldx, ptrs[1], ptrs[2], ldw, ptrs[3], ldd, ptrs[4], ldy,
+                                psaved, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle(x))
+    if status:
+        _check(status, "ccdc_ffn_forward")
+    return (out, saved) if save else out
 
 
 def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None, dx=None, dw_gate=None, dw_up=None,
@@ -701,32 +751,39 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
     a partition row); ``grad_dtype`` float32 keeps the sums' 32 bits."""
     import torch
 
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return ffn_backward(dy, x, w_gate, w_up, w_down, saved, act, grad_dtype, dx, dw_gate, dw_up, dw_down, workspace)
     M, D, F, ldx, ldw, ldd = _ffn_tensors(x, w_gate, w_up, w_down)
     code, L = _block_dtype(x), lib()
     gt = x.dtype if grad_dtype is None else grad_dtype
-    if gt not in (x.dtype, torch.float32):
+    if gt != x.dtype and gt != torch.float32:
         raise TypeError("grad_dtype is the tensors' dtype or float32")
     lddy = _rows(dy, "dy", x, x.shape)
-    if saved.numel() * saved.element_size() < L.ccdc_ffn_saved_bytes(M, F, code) or saved.device != x.device:
+    if saved.numel() * saved.element_size() < L.ccdc_ffn_saved_bytes(M, F, code) or saved.get_device() != x.get_device():
         raise ValueError("saved: what ffn_forward(save=True) returned expected")
-    with _OnStream(x, stream):
-        dx = torch.empty((M, D), dtype=x.dtype, device=x.device) if dx is None else dx
-        grads = []
-        for t, rows, cols, name in ((dw_gate, F, D, "dw_gate"), (dw_up, F, D, "dw_up"), (dw_down, D, F, "dw_down")):
-            if t is None:
-                t = torch.empty((rows, cols), dtype=gt, device=x.device)
-            elif t.numel() != rows * cols or not t.is_contiguous() or t.dtype != gt or t.device != x.device:
-                raise ValueError(f"{name}: {rows}x{cols} contiguous {gt} on {x.device} expected")
-            grads.append(t)
-        if workspace is None:
-            aligned = _ffn_aligned(x.element_size(), D, F, (dy, x, w_gate, w_up, w_down, dx))
-            workspace = torch.empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 1, aligned), dtype=torch.uint8,
-                                    device=x.device)
-        _check(L.ccdc_ffn_backward(
-            M, D, F, code, F32 if gt == torch.float32 else code, ACTS[act], dy.data_ptr(), lddy, x.data_ptr(), ldx,
-            w_gate.data_ptr(), w_up.data_ptr(), ldw, w_down.data_ptr(), ldd, saved.data_ptr(), dx.data_ptr(),
-            _rows(dx, "dx", x, x.shape), *(t.data_ptr() for t in grads), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), _handle()), "ccdc_ffn_backward")
+    if dx is None:
+        dx, lddx = x.new_empty((M, D)), D
+    else:
+        lddx = _rows(dx, "dx", x, x.shape)
+    grads, at = [], []
+    for t, shape, name in ((dw_gate, (F, D), "dw_gate"), (dw_up, (F, D), "dw_up"), (dw_down, (D, F), "dw_down")):
+        if t is None:
+            t = x.new_empty(shape, dtype=gt)
+            at.append(t.data_ptr())
+        else:
+            at.append(_vector(t, name, x, D * F, gt))
+        grads.append(t)
+    ptrs = dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dx.data_ptr()
+    if workspace is None:
+        aligned = _ffn_aligned(x.element_size(), *zip(ptrs, (lddy, ldx, ldw, D, ldd, lddx)), (0, F))
+        workspace = x.new_empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 1, aligned), dtype=torch.uint8)
+    status = L.ccdc_ffn_backward(M, D, F, code, F32 if gt == torch.float32 else code, ACTS[act], ptrs[0], lddy, ptrs[1], ldx,
+                                 ptrs[2], ptrs[3], ldw, ptrs[4], ldd, saved.data_ptr(), ptrs[5], lddx, *at,
+                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle(x))
+    if status:
+        _check(status, "ccdc_ffn_backward")
     return dx, *grads
 
 

@@ -4,6 +4,7 @@
 
 #include "ccdc_ffn.h"
 #include "ccdc_ffn_mma.h"
+#include "ccdc_ffn_rows.h"
 
 namespace {
 
@@ -247,13 +248,26 @@ struct Call {
 
     void forward(const void *x, long long ldx, const void *wg, const void *wu, long long ldw, const void *wd, long long ldd,
                  void *y, long long ldy, char *saved) {
+        float *h = reinterpret_cast<float *>(saved), *u = saved ? reinterpret_cast<float *>(saved + wide_bytes(M, F)) : nullptr;
+        char *kept = saved ? saved + 2 * wide_bytes(M, F) : nullptr;
+        if (M <= ROWS_MOST) {        // few rows: bound by the weights' bytes, not by products
+            const bool wide = dtype == CCDC_F32;
+            void *a = kept && !wide ? kept : space.take((size_t)M * pitch(F) * type_bytes(dtype));
+            if (plan_only || rc != CCDC_OK) return;
+            RowsProduct p = {M, F, D, x, wg, wu, ldx, ldw, a, pitch(F), h, u, wide ? kept : nullptr, act, dtype, false};
+            rc = rows_launch(p, sms, s);
+            if (rc != CCDC_OK) return;
+            RowsProduct q = {M, D, F, a, wd, nullptr, pitch(F), ldd, y, ldy, nullptr, nullptr, nullptr, act, dtype, true};
+            rc = rows_launch(q, sms, s);
+            return;
+        }
         const MmaMatrix X = operand(x, M, D, ldx), G = operand(wg, F, D, ldw), U = operand(wu, F, D, ldw);
         const MmaMatrix W = operand(wd, D, F, ldd);
-        void *a = saved ? saved + 2 * wide_bytes(M, F) : space.take(inner_bytes(M, F, dtype));
+        void *a = kept ? kept : space.take(inner_bytes(M, F, dtype));
         MmaProduct p = {};
         p.M = M, p.N = F, p.K = D, p.terms = 1, p.act = act;
         p.a[0] = {X, false}, p.b[0] = {G, false}, p.b[1] = {U, false};
-        if (saved) p.h = reinterpret_cast<float *>(saved), p.u = reinterpret_cast<float *>(saved + wide_bytes(M, F));
+        p.h = h, p.u = u;
         p.out[0] = inner(a);
         Shape first = {M, F, steps_of(D, 1), 1};
         const MmaTile tile = choose_tiles(&first, 1, MMA_GATE, dtype == CCDC_F32, sms);
@@ -403,6 +417,12 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
     if (count.space.used > workspace_bytes) return CCDC_ESIZE;
     c.backward(dy, lddy, x, ldx, w_gate, w_up, ldw, w_down, ldd, keep, dx, lddx, dw_gate, dw_up, dw_down, grad_dtype);
     return c.rc;
+}
+
+int ccdc_block_status(void) {
+    int failed = 0;
+    const int rc = mma_status(&failed);
+    return rc != CCDC_OK ? rc : failed ? CCDC_ESTATE : CCDC_OK;
 }
 
 }  // extern "C"

@@ -682,9 +682,7 @@ int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int 
                                   : launch_tile<MMA_GATE_BACK>(w, shape, sms, s);
 }
 
-extern "C" int ccdc_block_status(void) {
-    int failed = 0;
-    const cudaError_t e = cudaMemcpyFromSymbol(&failed, g_wait_failed, sizeof(int));
-    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
-    return failed ? CCDC_ESTATE : CCDC_OK;
+int mma_status(int *failed) {
+    const cudaError_t e = cudaMemcpyFromSymbol(failed, g_wait_failed, sizeof(int));
+    return e != cudaSuccess ? ccdc_internal_cuda_fail((int)e) : CCDC_OK;
 }

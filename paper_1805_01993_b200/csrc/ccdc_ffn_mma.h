@@ -51,3 +51,4 @@ inline int mma_tile_columns(MmaTile t) {        // GATE: of h and u together
 // All products of a call go through one launch: `type` CCDC_BF16 or CCDC_F16.  Matrices of three planes take
 // MMA_PLANES, others one of the first three.
 int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int type, MmaTile tile, int sms, cudaStream_t s);
+int mma_status(int *failed);     // *failed: whether a wait ever ran out on the current device
