@@ -103,46 +103,55 @@ __device__ __forceinline__ void store8(T *p, const Eight<T> &r) {
 // Random Numbers: As Easy as 1, 2, 3", 2011).  Key = the two words of the seed; counter = (element / 8, 0),
 // so that eight elements share one call and an element's number depends on (seed, element) alone: every
 // replica of a file draws the same mask wherever and in whatever order it is computed.
-__host__ __device__ __forceinline__ uint4 philox(unsigned long long seed, unsigned long long counter) {
-    uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32), c2 = 0, c3 = 0;
-    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-        const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-        c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
-        c3 = (uint32_t)a;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
-    }
-    return make_uint4(c0, c1, c2, c3);
-}
-// bit i set: element i of the eight that share `counter` is kept, i.e. its 16 bits are at least `cut`
-__device__ __forceinline__ uint32_t keep_bits(unsigned long long seed, unsigned long long counter, uint32_t cut) {
-    const uint4 r = philox(seed, counter);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-    uint32_t bits = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bits |= (uint32_t)((w[i] & 0xFFFFu) >= cut) << (2 * i);
-        bits |= (uint32_t)((w[i] >> 16) >= cut) << (2 * i + 1);
-    }
-    return bits;
-}
 // A probability in 1/65536 steps, and the factor of kept elements: that of the rounded probability, so that the
 // expectation is exact.  p = 1 drops everything.
 struct Dropout {
     unsigned long long seed, offset;
     uint32_t cut;       // 0: no dropout
+    uint32_t below;     // cut * 65536 - 1: 16 bits in the upper half of a word are kept where the word is above this
     float scale;
+    uint32_t key[20];   // the generator's keys, round by round
 };
 inline bool make_dropout(double p, unsigned long long seed, unsigned long long offset, Dropout *d) {
     if (!(p >= 0.0 && p <= 1.0)) return false;
     d->seed = seed, d->offset = offset;
     d->cut = (uint32_t)(p * 65536.0 + 0.5);
+    d->below = d->cut ? (uint32_t)(((unsigned long long)d->cut << 16) - 1) : 0;
     d->scale = d->cut >= 65536u ? 0.0f : (float)(65536.0 / (65536.0 - d->cut));
+    for (uint32_t i = 0; i < 10; ++i) {
+        d->key[2 * i] = (uint32_t)seed + i * 0x9E3779B9u;
+        d->key[2 * i + 1] = (uint32_t)(seed >> 32) + i * 0xBB67AE85u;
+    }
     return true;
+}
+// one call of the generator: 128 bits for the eight elements that share the counter
+__device__ __forceinline__ uint4 drop_words(const Dropout &d, unsigned long long counter) {
+    uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32), c2 = 0, c3 = 0;
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ d.key[2 * i];
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ d.key[2 * i + 1];
+        c3 = (uint32_t)a;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+// v where element `e` of the eight that share `w` is kept, else 0
+__device__ __forceinline__ float kept(const uint4 &w, int e, uint32_t below, float v) {
+    const uint32_t word = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
+    return ((e & 1) ? word : word << 16) > below ? v : 0.0f;
+}
+// the same as bits: bit e is set where element e is kept
+__device__ __forceinline__ uint32_t keep_bits(const Dropout &d, unsigned long long counter) {
+    const uint4 w = drop_words(d, counter);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t word = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
+        bits |= (uint32_t)(((e & 1) ? word : word << 16) > d.below) << e;
+    }
+    return bits;
 }
 
 inline bool is_16bit(int dtype) { return dtype == CCDC_BF16 || dtype == CCDC_F16; }

@@ -96,7 +96,8 @@ def norm_case(rng, M, D, dtype, gate, per, pad=0, shift=0, post=True, pre=True):
 
 
 NORMS = [(1, 1, 1), (1, 8, 1), (2, 5, 2), (3, 64, 1), (7, 129, 3), (300, 40, 7), (333, 1000, 50), (6, 1001, 2), (4, 2056, 4),
-         (2, 4100, 1), (3, 8192, 3), (2, 8200, 1), (2, 9001, 2), (1, 20000, 1), (2, 32768, 2), (600, 16, 600)]
+         (2, 4100, 1), (3, 8192, 3), (2, 8200, 1), (2, 9001, 2), (1, 20000, 1), (2, 32768, 2), (600, 16, 600),
+         (5, 64, 5), (13, 48, 4), (5, 520, 5), (11, 1032, 11), (9, 2064, 4), (700, 256, 90), (1300, 128, 1300), (37, 4096, 10)]
 
 
 @pytest.mark.parametrize("dtype", DT)
