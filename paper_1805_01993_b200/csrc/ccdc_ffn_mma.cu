@@ -107,16 +107,21 @@ __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, 
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
                  ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
 }
-template <int CG>
+// KEEP: 0 the block of A is read for this product alone; 1 it stays in the tensor core for the next one; 2 it is there
+template <int CG, int KEEP = 0>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    if constexpr (CG == 2)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+#define CCDC_MMA(GROUP, COLLECT)                                                                                   \
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::" GROUP ".kind::f16" COLLECT         \
+                 " [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory")
+    if constexpr (CG == 1)
+        CCDC_MMA("1", "");
+    else if constexpr (KEEP == 0)
+        CCDC_MMA("2", "");
+    else if constexpr (KEEP == 1)
+        CCDC_MMA("2", ".collector::a::fill");
     else
-        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+        CCDC_MMA("2", ".collector::a::lastuse");
+#undef CCDC_MMA
 }
 // arrives at the barrier (of both blocks of a pair) when the products issued so far are done
 template <int CG>
@@ -451,9 +456,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                         } else {
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-#pragma unroll
-                                for (int j = 0; j < NB; ++j)
-                                    mma<CG>(d + j * HALF_N, a + k * a_step, b + j * (BLOCK_BYTES >> 4) + k * b_step, idesc, add);
+                                mma<CG, NB == 2 ? 1 : 0>(d, a + k * a_step, b + k * b_step, idesc, add);
+                                if constexpr (NB == 2)
+                                    mma<CG, 2>(d + HALF_N, a + k * a_step, b + (BLOCK_BYTES >> 4) + k * b_step, idesc, add);
                                 add = true;
                             }
                         }

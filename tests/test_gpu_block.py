@@ -398,3 +398,84 @@ def test_on_another_stream_and_in_a_graph(ccdc):
     torch.cuda.synchronize()
     e_out, e_z = ccdc.residual_norm_forward(x, ccdc.ffn_forward(x, wg, wu, wd), w_pre=wd[:, 0].contiguous(), p=0.5, seed=4)
     assert torch.equal(out, e_out) and torch.equal(z, e_z) and torch.equal(d, ccdc.dropout(e_z, 0.5, 5))
+
+
+# ---------------------------------------------------------------- every tile shape of the products
+@pytest.mark.parametrize("M,D,F,dtype", [(600, 520, 4104, "bfloat16"), (1100, 1032, 5000, "float16"), (2304, 1024, 4096, "bfloat16"),
+                                         (300, 776, 1544, "float32"), (17, 2048, 4100, "bfloat16")])
+def test_ffn_large_tiles(ccdc, M, D, F, dtype):
+    """sizes at which the launches take the large tiles, cuts along k and several rounds of tiles, with ragged edges;
+    compared in 64 bits on the device, by norm: a result's rounding, and those of a, dh and du, are independent and
+    each at most U sqrt(1/3) of the values' size in the mean; 3 times their joint size is allowed"""
+    g = torch.Generator(device="cuda").manual_seed(M + D)
+
+    def randn(*shape, std=1.0):
+        return (torch.randn(shape, generator=g, device="cuda") * std).to(DT[dtype])
+
+    x, dy = randn(M, D), randn(M, D)
+    wg, wu, wd = randn(F, D, std=D ** -0.5), randn(F, D, std=D ** -0.5), randn(D, F, std=F ** -0.5)
+    leaves = [t.double().requires_grad_() for t in (x, wg, wu, wd)]
+    h, u = leaves[0] @ leaves[1].t(), leaves[0] @ leaves[2].t()
+    want = (h * torch.sigmoid(h) * u) @ leaves[3].t()
+    grads = torch.autograd.grad(want, leaves, dy.double())
+    y, saved = ccdc.ffn_forward(x, wg, wu, wd, save=True)
+    got = (y, *ccdc.ffn_backward(dy, x, wg, wu, wd, saved))
+    tol = 2.0 ** -19 if dtype == "float32" else 3 * ref.U[dtype] * (4 / 3) ** 0.5
+    for name, a, b in zip(("y", "dx", "dw_gate", "dw_up", "dw_down"), got, (want.detach(), *grads)):
+        err = float((a.double() - b).norm() / b.norm())
+        assert err <= tol, (name, err)
+        # no element is off by more than the sum's size allows: a misplaced tile would be
+        assert float((a.double() - b).abs().max() / b.abs().max()) <= 40 * tol, name
+    ccdc.block_status()
+
+
+# ---------------------------------------------------------------- the operators in a coded gradient job
+def test_block_job(ccdc):
+    """Map, shuffle and Reduce of the sub-block's gradients: replicas bit-identical, the Reduce output the sum over the
+    files, the gradients those of automatic differentiation"""
+    from paper_1805_01993_b200 import block_job
+
+    nodes, load, files, rows, D, F, p, seed = 4, 2, 12, 40, 64, 96, 0.25, 77
+    total, per_file, plan, losses = block_job.run(nodes, load, files, rows, D, F, p, seed, torch.float32)
+    direct, size = per_file.double().sum(0), per_file.double().abs().sum(0)
+    assert bool(((total.double() - direct).abs() <= 1e-5 * size + 1e-30).all())
+    params = block_job.make_parameters(D, F, torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    data = [torch.randn((rows, D), generator=g, device="cuda") for _ in range(files)]
+    for n in (0, 5, 11):
+        leaves = {k: v.double().requires_grad_() for k, v in params.items()}
+
+        def unit(v):
+            return v / (v.square().mean(1, keepdim=True) + 1e-5).sqrt()
+
+        x = data[n].double()
+        z = unit(x) * leaves["w_pre"]
+        h = z @ leaves["w_gate"].t()
+        y = (h * torch.sigmoid(h) * (z @ leaves["w_up"].t())) @ leaves["w_down"].t()
+        keep = torch.from_numpy(ref.keep_factors(rows, D, p, seed, n * rows * D)).cuda()
+        out = x + unit(y) * leaves["w_post"] * leaves["gate"] * keep
+        loss = out.square().mean()
+        grads = torch.autograd.grad(loss, [leaves[k] for k in block_job.PARAMETERS])
+        assert abs(float(losses[n]) - float(loss)) <= 1e-5 * float(loss)
+        at = 0
+        for k, want in zip(block_job.PARAMETERS, grads):
+            got = per_file[n][at:at + want.numel()].double().view(want.shape)
+            at += want.numel()
+            assert float((got - want).norm() / want.norm()) <= 1e-5, (n, k)
+    # the nodes' replicas agree bit by bit
+    again = block_job.run(nodes, load, files, rows, D, F, p, seed, torch.float32)
+    assert torch.equal(again[1], per_file) and torch.equal(again[0], total)
+
+
+def test_block_job_replicas(ccdc):
+    """a file mapped twice, from other addresses, leaves the same bits"""
+    from paper_1805_01993_b200 import block_job
+
+    D, F, rows = 136, 200, 33
+    params = block_job.make_parameters(D, F, torch.bfloat16)
+    x = torch.randn((rows, D), device="cuda").bfloat16()
+    words = block_job.gradient_words(D, F)
+    a, b = torch.zeros(words, device="cuda"), torch.ones(words + 64, device="cuda")[64:]
+    block_job.map_file(x, params, 0.1, 5, 1000, a)
+    block_job.map_file(x.clone(), {k: v.clone() for k, v in params.items()}, 0.1, 5, 1000, b)
+    assert torch.equal(a, b) and bool(a.isfinite().all())
