@@ -148,9 +148,9 @@ struct Space {
 // ------------------------------------------------------------------ tiles and cuts
 // How a launch's products are tiled, and how often each is cut along k.  The estimate, in cycles: a step of 64 k is
 // bounded by the fetch of its blocks (48 KiB for the 256 x 512 tile, 72 KiB for binary32, 32 KiB for the others, at about
-// 39 bytes a cycle);
-// an item costs about 2000 cycles besides, and its epilogue where it is not hidden (256 x 512); a cut product is
-// written and read again in binary32 and needs another launch.
+// 39 bytes a cycle); an item costs 2500 to begin, and its epilogue goes by 32-column pieces (two warps side by side),
+// hidden under the next item's products unless the tile fills tensor memory; a cut product is written and read again in
+// binary32 and needs another launch.
 struct Shape {
     long long M, N, steps;      // steps of 64 k over all terms
     int splits;
@@ -163,20 +163,22 @@ MmaTile choose_tiles(Shape *q, int count, MmaEpilogue e, bool planes, int sms) {
         const MmaTile at = (MmaTile)shape;
         const long long rows = mma_tile_rows(at), cols = mma_tile_columns(at) / (e == MMA_GATE ? 2 : 1);
         const double step = planes ? 1890 : at == MMA_WIDE ? 1260 : 840, units = at == MMA_SINGLE ? sms : sms / 2;
-        const double item = 2000 + (at != MMA_WIDE ? 0 : e == MMA_STORE ? 2000 : e == MMA_GATE ? 4000 : 8000);
+        const double epilogue = cols / 64 * (e == MMA_STORE ? 400.0 : e == MMA_GATE ? 3000.0 : 3500.0);
         for (long long most = e == MMA_STORE ? 8 : 1LL << 40;; most = most >= 256 ? 1LL << 40 : most * 2) {
             double total = 0, longest = 0, items = 0, parts = 0;
             int c[4];
             for (int i = 0; i < count; ++i) {
                 const long long tiles = ((q[i].M + rows - 1) / rows) * ((q[i].N + cols - 1) / cols);
                 c[i] = (int)std::min<long long>(std::max<long long>(1, (q[i].steps + most / 2) / most), 64);
-                const double cost = (double)q[i].steps / c[i] * step + item;
+                const double work = (double)q[i].steps / c[i] * step + 500;
+                const double cost = at == MMA_WIDE ? work + epilogue : std::max(work, epilogue);
                 total += cost * tiles * c[i], items += (double)tiles * c[i];
                 longest = std::max(longest, cost);
                 if (c[i] > 1) parts += 8.0 * c[i] * q[i].M * q[i].N;
             }
             double t = items <= units ? longest : std::max(longest, total / units) + longest / 2;
-            if (parts > 0) t += 4000 + parts / 2000;        // parts mostly stay in L2
+            t += 2500 + (at == MMA_WIDE ? 0 : epilogue);
+            if (parts > 0) t += 5000 + parts / 2000;        // parts mostly stay in L2
             if (t < best) {
                 best = t, tile = at;
                 for (int i = 0; i < count; ++i) cuts[i] = c[i];
