@@ -513,21 +513,23 @@ _BLOCK_TYPES = {}
 
 def _rows(t, name, like=None, shape=None):
     """row stride of a 2-D tensor; raises where it is not what the call takes."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.size(1) > 1):
+    strides, own = t.stride(), t.shape
+    if len(strides) != 2 or (strides[1] != 1 and own[1] > 1):
         raise ValueError(f"{name}: a 2-D tensor with contiguous columns expected")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if shape is not None and own != shape:
+        raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(own)}")
     if like is None:
         if not t.is_cuda:
             raise ValueError(f"{name}: a CUDA tensor expected")
-    elif t.dtype != like.dtype or t.get_device() != like.get_device():
+    elif t.dtype is not like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: {like.dtype} on {like.device} expected, got {t.dtype} on {t.device}")
-    return t.stride(0) if t.size(0) > 1 else t.size(1)
+    return strides[0] if own[0] > 1 else own[1]
 
 
 def _vector(t, name, like, n, dtype=None):
     """address of n contiguous values of like's (or the given) dtype."""
-    if t.numel() != n or not t.is_contiguous() or t.dtype != (dtype or like.dtype) or t.get_device() != like.get_device():
+    if (t.numel() != n or not t.is_contiguous() or t.dtype is not (dtype or like.dtype)
+            or t.get_device() != like.get_device()):
         raise ValueError(f"{name}: {n} contiguous {dtype or like.dtype} on {like.device} expected")
     return t.data_ptr()
 
@@ -552,6 +554,13 @@ def _handle(x):
     return torch._C._cuda_getCurrentRawStream(x.get_device())
 
 
+def _empty_like(x):
+    """a tensor of x's shape, type and device with contiguous rows (the cheapest call of torch's that makes one)."""
+    import torch
+
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 def dropout(x, p, seed, offset=0, out=None, stream=None):
     """``ccdc_dropout``: x with elements dropped by the counter-based mask of (seed, offset + element).
     The backward pass is the same call on the gradient.  ``out`` may be ``x``."""
@@ -563,7 +572,7 @@ def dropout(x, p, seed, offset=0, out=None, stream=None):
     code = _block_dtype(x)
     rows, cols = x.shape
     if out is None:
-        out, ldy = x.new_empty((rows, cols)), cols
+        out, ldy = _empty_like(x), cols
     else:
         ldy = _rows(out, "out", x, x.shape)
     status = lib().ccdc_dropout(rows, cols, code, x.data_ptr(), ldx, out.data_ptr(), ldy, p, seed, offset, _handle(x))
@@ -573,8 +582,8 @@ def dropout(x, p, seed, offset=0, out=None, stream=None):
 
 
 def _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate):
-    M, D = x.shape if x.dim() == 2 else (0, 0)
     ldx = _rows(x, "x")
+    M, D = x.shape
     ldy = D if y is None else _rows(y, "y", x, x.shape)
     pw = None if w_post is None else _vector(w_post, "w_post", x, D)
     pp = None if w_pre is None else _vector(w_pre, "w_pre", x, D)
@@ -592,7 +601,8 @@ def _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate):
 def residual_norm_forward(x, y=None, *, w_post=None, w_pre=None, gate=None, rows_per_gate=None, alpha=1.0, p=0.0, seed=0,
                           offset=0, kind="rms", eps=1e-5, save=False, out=None, z=None, stream=None):
     """``ccdc_residual_norm_forward``: out = alpha*x + drop(gate * norm(y)*w_post), z = norm(out)*w_pre.
-    Returns (out, z), or (out, z, stats) with ``save``; z is None without ``w_pre``."""
+    Returns (out, z), or (out, z, stats) with ``save``; z is None without ``w_pre``.  ``stats`` is opaque and goes to
+    ``residual_norm_backward``."""
     ctx = _elsewhere(x, stream)
     if ctx is not None:
         with ctx:
@@ -602,7 +612,7 @@ def residual_norm_forward(x, y=None, *, w_post=None, w_pre=None, gate=None, rows
     M, D, ldx, ldy, pw, pp, pg, per = _norm_tensors(x, y, w_post, w_pre, gate, rows_per_gate)
     code = _block_dtype(x)
     if out is None:
-        out, ldo = x.new_empty((M, D)), D
+        out, ldo = _empty_like(x), D
     else:
         ldo = _rows(out, "out", x, x.shape)
     pz, ldz, stats, ps = None, D, None, None
@@ -611,14 +621,14 @@ def residual_norm_forward(x, y=None, *, w_post=None, w_pre=None, gate=None, rows
             raise ValueError("z needs w_pre")
     else:
         if z is None:
-            z = x.new_empty((M, D))
+            z = _empty_like(x)
         else:
             ldz = _rows(z, "z", x, x.shape)
         pz = z.data_ptr()
     if save:
         import torch
 
-        stats = x.new_empty((M, 4), dtype=torch.float32)
+        stats = x.new_empty(4 * M, dtype=torch.float32)
         ps = stats.data_ptr()
     status = lib().ccdc_residual_norm_forward(M, D, code, NORMS[kind], eps, x.data_ptr(), ldx,
                                               None if y is None else y.data_ptr(), ldy, pw, pp, pg, per, alpha, p, seed,
@@ -654,7 +664,7 @@ def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, ga
 
     def rows_out(t, name):
         if t is None:
-            t = x.new_empty((M, D))
+            t = _empty_like(x)
             return t, t.data_ptr(), D
         return t, t.data_ptr(), _rows(t, name, x, x.shape)
 
@@ -664,7 +674,7 @@ def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, ga
                 raise ValueError(f"{name}: the forward call has no such input")
             return None, None
         if t is None:
-            t = x.new_empty(of.shape, dtype=gt)
+            t = torch.empty_like(of, dtype=gt)
             return t, t.data_ptr()
         return t, _vector(t, name, x, of.numel(), gt)
 
@@ -723,7 +733,7 @@ def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved
     M, D, F, ldx, ldw, ldd = _ffn_tensors(x, w_gate, w_up, w_down)
     code, L = _block_dtype(x), lib()
     if out is None:
-        out, ldy = x.new_empty((M, D)), D
+        out, ldy = _empty_like(x), D
     else:
         ldy = _rows(out, "out", x, x.shape)
     ptrs = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), out.data_ptr()
@@ -764,7 +774,7 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
     if saved.numel() * saved.element_size() < L.ccdc_ffn_saved_bytes(M, F, code) or saved.get_device() != x.get_device():
         raise ValueError("saved: what ffn_forward(save=True) returned expected")
     if dx is None:
-        dx, lddx = x.new_empty((M, D)), D
+        dx, lddx = _empty_like(x), D
     else:
         lddx = _rows(dx, "dx", x, x.shape)
     grads, at = [], []

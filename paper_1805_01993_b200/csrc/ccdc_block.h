@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "ccdc.h"
@@ -162,6 +163,8 @@ inline size_t round_up(size_t v, size_t n) { return (v + n - 1) / n * n; }
 
 // SM count of the current device; 0 on failure (status in *rc)
 int block_sm_count(int *rc);
+// allows a kernel `bytes` of dynamic shared memory on the current device; `done` remembers the devices it was asked on
+int block_allow_smem(const void *kernel, int bytes, std::atomic<unsigned long long> *done);
 
 inline int block_launch_status() {
     const cudaError_t e = cudaGetLastError();

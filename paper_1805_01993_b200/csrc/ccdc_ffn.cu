@@ -137,7 +137,7 @@ bool readable(const void *p, long long ld, long long rows, int dtype) {
 // the workspace, handed out front to back; a null base only counts
 struct Space {
     char *base;
-    size_t used = 0;
+    size_t size = 0, used = 0;
     void *take(size_t bytes) {
         void *p = base ? base + used : nullptr;
         used += round_up(bytes, 256);
@@ -199,7 +199,7 @@ int check_ffn(long long M, long long D, long long F, int dtype, int act) {
 }
 
 // One call: the operands as the tensor cores read them, the workspace, the launches.  With plan_only set the same
-// steps only count the workspace.
+// steps only count the workspace and run nothing.
 struct Call {
     long long M, D, F;
     int dtype, act, sms;
@@ -219,8 +219,14 @@ struct Call {
         copies.c[copies.count++] = {p, to, rows, cols, ld, pitch(cols)};
         return {to, rows, cols, pitch(cols), planes_of(dtype)};
     }
+    // everything is laid out: does it fit?
+    bool fits() {
+        if (plan_only) return false;
+        if (space.used > space.size) rc = CCDC_ESIZE;
+        return rc == CCDC_OK;
+    }
     void run_copies() {
-        if (plan_only || !copies.count || rc != CCDC_OK) return;
+        if (!copies.count || rc != CCDC_OK) return;
         copies.f32 = dtype == CCDC_F32;
         long long most = 0;
         for (int i = 0; i < copies.count; ++i) most = std::max(most, copies.c[i].rows * copies.c[i].ld_to / 2);
@@ -238,11 +244,11 @@ struct Call {
         joins.j[joins.count++] = {static_cast<const float *>(q.c), c, q.M, q.N, q.ldc, ldc, splits, c_type};
     }
     void run_products(const MmaProduct *q, int count, MmaEpilogue e, MmaTile tile) {
-        if (plan_only || rc != CCDC_OK) return;
+        if (rc != CCDC_OK) return;
         rc = mma_launch(q, count, e, type(), tile, sms, s);
     }
     void run_joins() {
-        if (plan_only || !joins.count || rc != CCDC_OK) return;
+        if (!joins.count || rc != CCDC_OK) return;
         long long most = 0;
         for (int i = 0; i < joins.count; ++i) most = std::max(most, joins.j[i].rows * (joins.j[i].cols / 4 + 1));
         rc = launch_small(k_ffn_join, joins, most, joins.count, sms, s);
@@ -255,7 +261,7 @@ struct Call {
         if (M <= ROWS_MOST) {        // few rows: bound by the weights' bytes, not by products
             const bool wide = dtype == CCDC_F32;
             void *a = kept && !wide ? kept : space.take((size_t)M * pitch(F) * type_bytes(dtype));
-            if (plan_only || rc != CCDC_OK) return;
+            if (!fits()) return;
             RowsProduct p = {M, F, D, x, wg, wu, ldx, ldw, a, pitch(F), h, u, wide ? kept : nullptr, act, dtype, false};
             rc = rows_launch(p, sms, s);
             if (rc != CCDC_OK) return;
@@ -278,6 +284,7 @@ struct Call {
         Shape second = {M, D, steps_of(F, 1), 1};
         const MmaTile tile2 = choose_tiles(&second, 1, MMA_STORE, dtype == CCDC_F32, sms);
         to_output(q, second.splits, y, ldy, dtype);
+        if (!fits()) return;
         run_copies();
         run_products(&p, 1, MMA_GATE, tile);
         run_products(&q, 1, MMA_STORE, tile2);
@@ -326,6 +333,7 @@ struct Call {
             q[wanted++] = q[i];
         }
         n = wanted;
+        if (!fits()) return;
         run_copies();
         run_products(&p, 1, MMA_GATE_BACK, tile);
         run_products(q, n, MMA_STORE, tile2);
@@ -376,13 +384,8 @@ int ccdc_ffn_forward(long long M, long long D, long long F, int dtype, int act, 
     Call c = {M, D, F, dtype, act, 0, false, false};
     c.sms = block_sm_count(&rc);
     if (rc != CCDC_OK) return rc;
-    c.space.base = static_cast<char *>(workspace);
+    c.space.base = static_cast<char *>(workspace), c.space.size = workspace_bytes;
     c.s = static_cast<cudaStream_t>(stream);
-    // what this call takes: the same steps, counted
-    Call count = c;
-    count.rc = -100;
-    count.forward(x, ldx, w_gate, w_up, ldw, w_down, ldd, y, ldy, static_cast<char *>(saved));
-    if (count.space.used > workspace_bytes) return CCDC_ESIZE;
     c.forward(x, ldx, w_gate, w_up, ldw, w_down, ldd, y, ldy, static_cast<char *>(saved));
     return c.rc;
 }
@@ -410,13 +413,9 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
     Call c = {M, D, F, dtype, act, 0, false, false};
     c.sms = block_sm_count(&rc);
     if (rc != CCDC_OK) return rc;
-    c.space.base = static_cast<char *>(workspace);
+    c.space.base = static_cast<char *>(workspace), c.space.size = workspace_bytes;
     c.s = s;
     char *keep = static_cast<char *>(const_cast<void *>(saved));
-    Call count = c;
-    count.rc = -100;
-    count.backward(dy, lddy, x, ldx, w_gate, w_up, ldw, w_down, ldd, keep, dx, lddx, dw_gate, dw_up, dw_down, grad_dtype);
-    if (count.space.used > workspace_bytes) return CCDC_ESIZE;
     c.backward(dy, lddy, x, ldx, w_gate, w_up, ldw, w_down, ldd, keep, dx, lddx, dw_gate, dw_up, dw_down, grad_dtype);
     return c.rc;
 }

@@ -614,8 +614,9 @@ bool encode(CUtensorMap *map, int type, const void *p, long long cols, long long
 template <int CG, int NB, int EPI, bool PLANES>
 int launch(const Work &w, int sms, cudaStream_t s) {
     auto *kernel = k_ffn_mma<CG, NB, EPI, PLANES>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
-    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    static std::atomic<unsigned long long> done;
+    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), SMEM_BYTES, &done);
+    if (rc != CCDC_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min(w.items, std::max(1, sms / CG)) * CG));
     cfg.blockDim = dim3(THREADS);
@@ -628,7 +629,7 @@ int launch(const Work &w, int sms, cudaStream_t s) {
     at[1].val.clusterDim.x = CG, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    e = cudaLaunchKernelEx(&cfg, kernel, w);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, w);
     if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
     ccdc_internal_count_launch();
     return CCDC_OK;

@@ -973,8 +973,9 @@ int launch_team(const NormArgs &a, int shares, cudaStream_t s) {
     constexpr int ITEMS = sizeof(T) == 4 ? 1 : 2, TEAMS = W == 16 ? 1 : 8 / W, THREADS = 32 * W * TEAMS;
     constexpr int SMEM = RowStream<T, ITEMS, W, THREADS, BACK ? 5 : 3, STAGES>::SMEM + (BACK ? ITEMS * 32 * THREADS : 0);
     auto *kernel = BACK ? k_norm_rows_back<T, ITEMS, W, TEAMS> : k_norm_rows<T, ITEMS, W, TEAMS>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    static std::atomic<unsigned long long> done;
+    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), SMEM, &done);
+    if (rc != CCDC_OK) return rc;
     kernel<<<shares / TEAMS, THREADS, SMEM, s>>>(a);
     return block_launch_status();
 }
@@ -1032,15 +1033,31 @@ int check_norm(long long M, long long D, int dtype, int kind, const void *x, lon
 }  // namespace
 
 int block_sm_count(int *rc) {
+    static std::atomic<int> known[64];          // a device's SM count does not change
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) sms = known[dev].load(std::memory_order_relaxed);
+    if (e == cudaSuccess && !sms) {
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e == cudaSuccess && dev < 64) known[dev].store(sms, std::memory_order_relaxed);
+    }
     if (e != cudaSuccess) {
         *rc = ccdc_internal_cuda_fail((int)e);
         return 0;
     }
     *rc = CCDC_OK;
     return sms;
+}
+
+int block_allow_smem(const void *kernel, int bytes, std::atomic<unsigned long long> *done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (e == cudaSuccess && (done->load(std::memory_order_relaxed) & bit)) return CCDC_OK;
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    done->fetch_or(bit, std::memory_order_relaxed);
+    return CCDC_OK;
 }
 
 extern "C" {
