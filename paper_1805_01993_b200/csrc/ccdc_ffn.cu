@@ -258,14 +258,13 @@ struct Call {
                  void *y, long long ldy, char *saved) {
         float *h = reinterpret_cast<float *>(saved), *u = saved ? reinterpret_cast<float *>(saved + wide_bytes(M, F)) : nullptr;
         char *kept = saved ? saved + 2 * wide_bytes(M, F) : nullptr;
-        if (M <= ROWS_MOST) {        // few rows: bound by the weights' bytes, not by products
-            const bool wide = dtype == CCDC_F32;
-            void *a = kept && !wide ? kept : space.take((size_t)M * pitch(F) * type_bytes(dtype));
+        if (M <= rows_most(dtype)) {        // few rows: bound by the weights' bytes, not by products
+            void *a = kept ? kept : space.take((size_t)M * pitch(F) * type_bytes(dtype));
             if (!fits()) return;
-            RowsProduct p = {M, F, D, x, wg, wu, ldx, ldw, a, pitch(F), h, u, wide ? kept : nullptr, act, dtype, false};
+            RowsProduct p = {M, F, D, x, wg, wu, ldx, ldw, a, pitch(F), h, u, act, dtype, false};
             rc = rows_launch(p, sms, s);
             if (rc != CCDC_OK) return;
-            RowsProduct q = {M, D, F, a, wd, nullptr, pitch(F), ldd, y, ldy, nullptr, nullptr, nullptr, act, dtype, true};
+            RowsProduct q = {M, D, F, a, wd, nullptr, pitch(F), ldd, y, ldy, nullptr, nullptr, act, dtype, true};
             rc = rows_launch(q, sms, s);
             return;
         }
@@ -291,9 +290,42 @@ struct Call {
         run_joins();
     }
 
+    // binary32, few rows
+    void few_backward(const void *dy, long long lddy, const void *x, long long ldx, const void *wg, const void *wu,
+                      long long ldw, const void *wd, long long ldd, char *saved, void *dx, long long lddx, void *dwg, void *dwu,
+                      void *dwd) {
+        auto f = [](const void *p) { return static_cast<const float *>(p); };
+        const float *a = f(saved + 2 * wide_bytes(M, F));
+        const long long ld = pitch(F), ldo = pitch(D);
+        float *dh = static_cast<float *>(space.take((size_t)M * ld * 4)), *du = static_cast<float *>(space.take((size_t)M * ld * 4));
+        const int cuts = few_across_splits(M, F, D, 1, sms), cuts_x = few_across_splits(M, D, F, 2, sms);
+        float *da = static_cast<float *>(space.take((size_t)cuts * M * ld * 4));
+        float *parts = static_cast<float *>(space.take((size_t)cuts_x * M * ldo * 4));
+        if (!fits()) return;
+        rc = few_across({M, F, D, 1, cuts, {f(dy), nullptr}, {f(wd), nullptr}, lddy, ldd, ld, da}, s);
+        if (rc == CCDC_OK)
+            rc = few_gate_back({M, F, ld, cuts, act, da, reinterpret_cast<float *>(saved),
+                                reinterpret_cast<float *>(saved + wide_bytes(M, F)), dh, du}, s);
+        if (rc == CCDC_OK && dx) {
+            rc = few_across({M, D, F, 2, cuts_x, {dh, du}, {f(wg), f(wu)}, ld, ldw, ldo, parts}, s);
+            joins.j[joins.count++] = {parts, dx, M, D, ldo, lddx, cuts_x, CCDC_F32};
+            run_joins();
+        }
+        FewOuters o = {};
+        o.M = M;
+        if (dwg) o.o[o.count++] = {dh, f(x), ld, ldx, F, D, static_cast<float *>(dwg)};
+        if (dwu) o.o[o.count++] = {du, f(x), ld, ldx, F, D, static_cast<float *>(dwu)};
+        if (dwd) o.o[o.count++] = {f(dy), a, lddy, ld, D, F, static_cast<float *>(dwd)};
+        if (rc == CCDC_OK && o.count) rc = few_outer(o, s);
+    }
+
     void backward(const void *dy, long long lddy, const void *x, long long ldx, const void *wg, const void *wu, long long ldw,
                   const void *wd, long long ldd, char *saved, void *dx, long long lddx, void *dwg, void *dwu, void *dwd,
                   int grad_dtype) {
+        if (dtype == CCDC_F32 && M <= FEW_MOST) {
+            few_backward(dy, lddy, x, ldx, wg, wu, ldw, wd, ldd, saved, dx, lddx, dwg, dwu, dwd);
+            return;
+        }
         const MmaMatrix DY = operand(dy, M, D, lddy), X = operand(x, M, D, ldx), G = operand(wg, F, D, ldw);
         const MmaMatrix U = operand(wu, F, D, ldw), W = operand(wd, D, F, ldd);
         const MmaMatrix A = inner(saved + 2 * wide_bytes(M, F));

@@ -7,7 +7,7 @@
 //   16-bit types: mma.sync m16n8k16 with the weights as the 16-row side and the rows of x as the other.  A thread
 //     loads 16 bytes (8 k) of two weight rows and of its row of x and uses them as the fragments of two
 //     multiplications: the order of k inside a step is free as long as both sides agree, so no shuffles are needed.
-//   binary32: plain multiply-adds, four weight rows a warp, the lanes along k.
+//   binary32 (up to 32 rows): plain multiply-adds, two or four weight rows a warp, the lanes along k.
 // (Bulk copies of row slices into shared memory were slower: about 33 cycles a copy and SM, whatever its size.)
 // Where there are too few blocks of 16 rows to keep the memory busy, a cluster of up to eight blocks shares the k
 // range and the first block adds their sums, in order, through distributed shared memory.
@@ -23,7 +23,7 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int ROWS = 16, WARPS = 8, THREADS = WARPS * 32, TOKENS = 8;
+constexpr int ROWS = 16, WARPS = 8, THREADS = WARPS * 32;
 
 __device__ __forceinline__ void multiply(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1, bf16) {
@@ -60,14 +60,14 @@ __device__ __forceinline__ uint4 load16(const T *row, long long k, long long K, 
     return v;
 }
 
-// MATS: 1 or 2 matrices; ALIGNED: rows of 16-byte multiples
-template <class T, int MATS, bool ALIGNED>
-__global__ void __launch_bounds__(THREADS, 2) k_ffn_rows(const RowsProduct p) {
+// MATS: 1 or 2 matrices; TOKENS: rows of x (8; binary32 also 32); ALIGNED: rows of 16-byte multiples
+template <class T, int MATS, int TOKENS, bool ALIGNED>
+__global__ void __launch_bounds__(THREADS, TOKENS == 8 ? 2 : 1) k_ffn_rows(const RowsProduct p) {
     constexpr bool WIDE = sizeof(T) == 4;
     constexpr int STEP = WIDE ? 128 : 32;               // k of a step
-    constexpr int SHARES = WIDE ? 2 : WARPS;            // warps (binary32: groups of four) that take steps in turn
     constexpr int UNROLL = (WIDE ? 2 : 4) / MATS;       // steps of a batch
-    constexpr int PER = WIDE ? 4 : 2;                   // weight rows of a thread
+    constexpr int PER = !WIDE ? 2 : TOKENS == 8 ? 4 : 4 / MATS;         // weight rows of a thread
+    constexpr int SHARES = WIDE ? PER * WARPS / ROWS : WARPS;           // warps (binary32: groups of them) that take steps in turn
     constexpr int BATCHES = WIDE ? 1 : 2;
     __shared__ float part[SHARES][MATS][ROWS][TOKENS + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_ffn_rows(const RowsProduct p) {
     const long long n0 = (long long)(blockIdx.x / cluster) * ROWS;
     const long long steps = (p.K + STEP - 1) / STEP;
     const long long s0 = steps * rank / cluster, s1 = steps * (rank + 1) / cluster;
-    const int r0 = WIDE ? (warp & 3) * 4 : g, dr = WIDE ? 1 : 8, share = WIDE ? warp >> 2 : warp;
+    const int r0 = WIDE ? warp % (ROWS / PER) * PER : g, dr = WIDE ? 1 : 8, share = WIDE ? warp / (ROWS / PER) : warp;
     const T *w[MATS][PER], *x = static_cast<const T *>(p.x);
     bool in[PER];
 #pragma unroll
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_ffn_rows(const RowsProduct p) {
 
     const int k_lane = WIDE ? 4 * lane : 8 * t;
     uint4 q[BATCHES][UNROLL][MATS][PER], b[BATCHES][UNROLL];
-    float acc[MATS][WIDE ? 4 : 1][WIDE ? TOKENS : 4] = {};
+    float acc[MATS][WIDE ? PER : 1][WIDE ? TOKENS : 4] = {};
     auto fetch_w = [&](int z, long long s) {
 #pragma unroll
         for (int i = 0; i < UNROLL; ++i)
@@ -126,18 +126,24 @@ __global__ void __launch_bounds__(THREADS, 2) k_ffn_rows(const RowsProduct p) {
                 const long long at = s + i * SHARES;
                 if (at >= s1) break;
 #pragma unroll
-                for (int m = 0; m < TOKENS; ++m) {
-                    if (m >= p.M) break;
-                    const uint4 bv = load16<T, ALIGNED, false>(x + m * p.ldx, at * STEP + k_lane, p.K, true);
-                    const float4 c = *reinterpret_cast<const float4 *>(&bv);
+                for (int m0 = 0; m0 < TOKENS; m0 += 8) {
+                    if (m0 >= p.M) break;
+                    uint4 xv[8];        // eight rows of x asked for together
 #pragma unroll
-                    for (int k = 0; k < MATS; ++k)
+                    for (int m = 0; m < 8; ++m)
+                        xv[m] = load16<T, ALIGNED, false>(x + (m0 + m) * p.ldx, at * STEP + k_lane, p.K, m0 + m < p.M);
 #pragma unroll
-                        for (int r = 0; r < PER; ++r) {
-                            const float4 a = *reinterpret_cast<const float4 *>(&q[z][i][k][r]);
-                            float &sum = acc[k][r][m];
-                            sum = fmaf(a.x, c.x, fmaf(a.y, c.y, fmaf(a.z, c.z, fmaf(a.w, c.w, sum))));
-                        }
+                    for (int m = 0; m < 8; ++m) {
+                        const float4 c = *reinterpret_cast<const float4 *>(&xv[m]);
+#pragma unroll
+                        for (int k = 0; k < MATS; ++k)
+#pragma unroll
+                            for (int r = 0; r < PER; ++r) {
+                                const float4 a = *reinterpret_cast<const float4 *>(&q[z][i][k][r]);
+                                float &sum = acc[k][r][m0 + m];
+                                sum = fmaf(a.x, c.x, fmaf(a.y, c.y, fmaf(a.z, c.z, fmaf(a.w, c.w, sum))));
+                            }
+                    }
                 }
             }
         }
@@ -214,22 +220,11 @@ __global__ void __launch_bounds__(THREADS, 2) k_ffn_rows(const RowsProduct p) {
                 });
             }
             static_cast<T *>(p.out)[m * p.ldo + n] = from_f32<T>(f);
-            if constexpr (WIDE) {
-                if (p.planes) {         // a as the backward pass reads it
-                    bf16 *to = static_cast<bf16 *>(p.planes) + m * p.ldo + n;
-#pragma unroll
-                    for (int z = 0; z < 3; ++z) {
-                        const bf16 hi = from_f32<bf16>(f);
-                        to[z * p.M * p.ldo] = hi;
-                        f = isfinite(to_f32<bf16>(hi)) ? f - to_f32<bf16>(hi) : 0.0f;
-                    }
-                }
-            }
         }
     if (cluster > 1) cg::this_cluster().sync();     // the others' shared memory is read until here
 }
 
-template <class T, int MATS, bool ALIGNED>
+template <class T, int MATS, int TOKENS, bool ALIGNED>
 int launch(const RowsProduct &p, int sms, cudaStream_t s) {
     // enough blocks for two an SM, as long as a warp keeps four steps
     const long long blocks = (p.N + ROWS - 1) / ROWS, step = sizeof(T) == 4 ? 128 * 2 : 32 * WARPS;
@@ -246,24 +241,25 @@ int launch(const RowsProduct &p, int sms, cudaStream_t s) {
     at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_ffn_rows<T, MATS, ALIGNED>, p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_ffn_rows<T, MATS, TOKENS, ALIGNED>, p);
     if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
     ccdc_internal_count_launch();
     return CCDC_OK;
 }
-template <class T, int MATS>
+template <class T, int MATS, int TOKENS>
 int launch_aligned(const RowsProduct &p, int sms, cudaStream_t s) {
     auto rows = [&](const void *q, long long ld, long long n) {
         return !q || (aligned_to(q, 16) && (n < 2 || ld * sizeof(T) % 16 == 0));
     };
     const bool aligned = p.K * sizeof(T) % 16 == 0 && rows(p.x, p.ldx, p.M) && rows(p.w, p.ldw, p.N) && rows(p.w2, p.ldw, p.N);
-    return aligned ? launch<T, MATS, true>(p, sms, s) : launch<T, MATS, false>(p, sms, s);
+    return aligned ? launch<T, MATS, TOKENS, true>(p, sms, s) : launch<T, MATS, TOKENS, false>(p, sms, s);
 }
 
 }  // namespace
 
 int rows_launch(const RowsProduct &p, int sms, cudaStream_t s) {
-    if (p.dtype == CCDC_F32) return p.w2 ? launch_aligned<float, 2>(p, sms, s) : launch_aligned<float, 1>(p, sms, s);
-    if (p.dtype == CCDC_BF16) return p.w2 ? launch_aligned<bf16, 2>(p, sms, s) : launch_aligned<bf16, 1>(p, sms, s);
-    return p.w2 ? launch_aligned<fp16, 2>(p, sms, s) : launch_aligned<fp16, 1>(p, sms, s);
+    if (p.dtype == CCDC_F32 && p.M > 8) return p.w2 ? launch_aligned<float, 2, 32>(p, sms, s) : launch_aligned<float, 1, 32>(p, sms, s);
+    if (p.dtype == CCDC_F32) return p.w2 ? launch_aligned<float, 2, 8>(p, sms, s) : launch_aligned<float, 1, 8>(p, sms, s);
+    if (p.dtype == CCDC_BF16) return p.w2 ? launch_aligned<bf16, 2, 8>(p, sms, s) : launch_aligned<bf16, 1, 8>(p, sms, s);
+    return p.w2 ? launch_aligned<fp16, 2, 8>(p, sms, s) : launch_aligned<fp16, 1, 8>(p, sms, s);
 }
