@@ -179,6 +179,19 @@ __device__ __forceinline__ Tile tile_of(const Work &w, int item) {
     return t;
 }
 
+// What the epilogue needs of a problem, copied into registers once a tile: left in the kernel's parameters, every field
+// is loaded again after every barrier (1 to 3 % of the small and middle sizes).
+struct Output {
+    const CUtensorMap *c0, *c1;
+    void *cp;
+    long long ldc, split_stride;
+    float *h, *u;
+    int M, N, c_f32, c_tma, planes, act, groups;
+    __device__ __forceinline__ explicit Output(const Problem &p)
+        : c0(&p.c[0]), c1(&p.c[1]), cp(p.cp), ldc(p.ldc), split_stride(p.split_stride), h(p.h), u(p.u), M(p.M), N(p.N),
+          c_f32(p.c_f32), c_tma(p.c_tma), planes(p.planes), act(p.act), groups(p.groups) {}
+};
+
 // The epilogue warps' way out: 32 rows of 64 bytes a slot, swizzled so that the row writes meet no bank conflict.
 struct Ring {
     char *base;
@@ -210,7 +223,7 @@ __device__ __forceinline__ void put16(char *slot, int row, const float (&f)[32])
                        pack2<T>(f[8 * c + 4], f[8 * c + 5]), pack2<T>(f[8 * c + 6], f[8 * c + 7]));
 }
 // 32 columns as 16-bit words, or as the planes of binary32 words
-__device__ __forceinline__ void emit(const Problem &p, const CUtensorMap *map, int f16, float (&f)[32], int col, int row0,
+__device__ __forceinline__ void emit(const Output &p, const CUtensorMap *map, int f16, float (&f)[32], int col, int row0,
                                      int lane, Ring &ring) {
     for (int z = 0; z < p.planes; ++z) {
         char *slot = ring.next(lane);
@@ -230,7 +243,7 @@ __device__ __forceinline__ void emit(const Problem &p, const CUtensorMap *map, i
 }
 
 // The values of a tile that leave as they are: 32 columns from `col` on.
-__device__ __forceinline__ void store_columns(const Problem &p, int f16, const float (&f)[32], int col, int row0, int split,
+__device__ __forceinline__ void store_columns(const Output &p, int f16, const float (&f)[32], int col, int row0, int split,
                                               int lane, Ring &ring) {
     const int width = p.c_f32 ? 16 : 32;            // columns of a slot
 #pragma unroll
@@ -250,7 +263,7 @@ __device__ __forceinline__ void store_columns(const Problem &p, int f16, const f
             put16<bf16>(slot, lane, f);
         }
         if (p.c_tma) {
-            out_by_tma(&p.c[0], at, row0, split, slot, lane);
+            out_by_tma(p.c0, at, row0, split, slot, lane);
             continue;
         }
         // rows that TMA cannot address: a row (binary32: two) at a time, neighbouring threads neighbouring words
@@ -269,7 +282,7 @@ __device__ __forceinline__ void store_columns(const Problem &p, int f16, const f
     }
 }
 // h and u of 32 columns of this thread's row
-__device__ __forceinline__ void load_saved(const Problem &p, long long block, int col, int lane, float4 (&h)[8], float4 (&u)[8]) {
+__device__ __forceinline__ void load_saved(const Output &p, long long block, int col, int lane, float4 (&h)[8], float4 (&u)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         h[i] = u[i] = make_float4(0, 0, 0, 0);
@@ -281,7 +294,7 @@ __device__ __forceinline__ void load_saved(const Problem &p, long long block, in
     }
 }
 template <bool EXACT>
-__device__ __forceinline__ void gate_columns(const Problem &p, int f16, float (&h)[32], float (&u)[32], long long block, int col,
+__device__ __forceinline__ void gate_columns(const Output &p, int f16, float (&h)[32], float (&u)[32], long long block, int col,
                                              int row0, int lane, Ring &ring) {
     if (p.h) {
 #pragma unroll
@@ -299,11 +312,11 @@ __device__ __forceinline__ void gate_columns(const Problem &p, int f16, float (&
             u[i] *= act(h[i], &slope);
         }
     });
-    emit(p, &p.c[0], f16, u, col, row0, lane, ring);
+    emit(p, p.c0, f16, u, col, row0, lane, ring);
 }
 // d (da on entry) becomes dh, du the other
 template <bool EXACT>
-__device__ __forceinline__ void gate_back_columns(const Problem &p, float (&d)[32], float (&du)[32], const float4 (&h)[8],
+__device__ __forceinline__ void gate_back_columns(const Output &p, float (&d)[32], float (&du)[32], const float4 (&h)[8],
                                                   const float4 (&u)[8]) {
     act_apply<EXACT>(p.act, [&](auto act) {
 #pragma unroll
@@ -472,6 +485,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
     } else {
         const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
         const int part = (warp - 2) >> 2;           // two warps a quarter: each takes half of the columns
+        const int f16 = w.f16;
         Ring ring = {ring_base + (warp - 2) * RING_SLOT * RING_SLOTS, 0};
         uint32_t sums = 0;
         auto release = [&](uint32_t acc) {
@@ -487,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
         constexpr int COLS = EPI == MMA_GATE ? TILE_N / 2 : TILE_N;     // output columns of a tile
         for (int item = cluster; item < w.items; item += clusters) {
             const Tile t = tile_of(w, item);
-            const Problem &p = w.p[t.problem];
+            const Output p(w.p[t.problem]);
             const int row0 = t.m * TILE_M + 128 * (int)rank + 32 * quarter;
             const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
             const bool rows = row0 < p.M;
@@ -504,19 +518,19 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                     tmem_load(from + c, f);
                     if constexpr (EPI == MMA_STORE) {
                         tmem_wait();
-                        store_columns(p, w.f16, f, col0 + c, row0, t.split, lane, ring);
+                        store_columns(p, f16, f, col0 + c, row0, t.split, lane, ring);
                     } else if constexpr (EPI == MMA_GATE) {
                         float g[32];
                         tmem_load(from + COLS + c, g);
                         tmem_wait();
-                        gate_columns<false>(p, w.f16, f, g, block, col0 + c, row0, lane, ring);
+                        gate_columns<false>(p, f16, f, g, block, col0 + c, row0, lane, ring);
                     } else {
                         tmem_wait();
                         float g[32];
                         gate_back_columns<false>(p, f, g, h, u);
                         if (col0 + c + 32 < col1) load_saved(p, block, col0 + c + 32, lane, h, u);     // on their way during the stores
-                        emit(p, &p.c[0], w.f16, f, col0 + c, row0, lane, ring);
-                        emit(p, &p.c[1], w.f16, g, col0 + c, row0, lane, ring);
+                        emit(p, p.c0, f16, f, col0 + c, row0, lane, ring);
+                        emit(p, p.c1, f16, g, col0 + c, row0, lane, ring);
                     }
                 }
                 release(acc);
@@ -539,20 +553,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                 }
                 if (rows && col0 < col1) {
                     if constexpr (EPI == MMA_GATE) {
-                        gate_columns<true>(p, w.f16, f[0], f[1], block, col0, row0, lane, ring);
+                        gate_columns<true>(p, f16, f[0], f[1], block, col0, row0, lane, ring);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             if (col0 + 32 * j >= col1) break;
                             if constexpr (EPI == MMA_STORE) {
-                                store_columns(p, w.f16, f[j], col0 + 32 * j, row0, t.split, lane, ring);
+                                store_columns(p, f16, f[j], col0 + 32 * j, row0, t.split, lane, ring);
                             } else {
                                 float4 h[8], u[8];
                                 load_saved(p, block, col0 + 32 * j, lane, h, u);
                                 float g[32];
                                 gate_back_columns<true>(p, f[j], g, h, u);
-                                emit(p, &p.c[0], w.f16, f[j], col0 + 32 * j, row0, lane, ring);
-                                emit(p, &p.c[1], w.f16, g, col0 + 32 * j, row0, lane, ring);
+                                emit(p, p.c0, f16, f[j], col0 + 32 * j, row0, lane, ring);
+                                emit(p, p.c1, f16, g, col0 + 32 * j, row0, lane, ring);
                             }
                         }
                     }
