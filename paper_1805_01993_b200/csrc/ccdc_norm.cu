@@ -62,9 +62,13 @@ __device__ __forceinline__ float2 block_sum(float a, float b, float2 (*buf)[THRE
         turn ^= 1;
         if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = make_float2(a, b);
         __syncthreads();
-        a = b = 0.0f;
+        const float2 v = s[threadIdx.x & (THREADS / 32 - 1)];
+        a = v.x, b = v.y;
 #pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) a += s[i].x, b += s[i].y;
+        for (int i = THREADS / 64; i; i >>= 1) {
+            a += __shfl_xor_sync(~0u, a, i);
+            b += __shfl_xor_sync(~0u, b, i);
+        }
     }
     return make_float2(a, b);
 }
@@ -226,15 +230,24 @@ __global__ void __launch_bounds__(THREADS) k_residual_norm_back(const NormArgs a
     const long long first = share(a.M, gridDim.x, blockIdx.x), last = share(a.M, gridDim.x, blockIdx.x + 1);
     const long long first_group = first / a.per;
     for (long long m = first; m < last; ++m, parity ^= 1) {
+        // everything the row needs is asked for before the first barrier
         const float4 st = a.stats[m];
-        float oh[ITEMS][VEC], yh[ITEMS][VEC], cg[ITEMS][VEC], t[ITEMS][VEC];
+        float oh[ITEMS][VEC], yh[ITEMS][VEC], cg[ITEMS][VEC], t[ITEMS][VEC], e[ITEMS][VEC], w_post[ITEMS][VEC], gate[ITEMS][VEC];
         R::load(static_cast<const T *>(a.x) + m * a.ldx, D, oh);
+        if (a.y) R::load(static_cast<const T *>(a.y) + m * a.ldy, D, yh);
+        if (a.w_pre) R::load(static_cast<const T *>(a.dz) + m * a.lddz, D, e);
+        if (a.dout) R::load(static_cast<const T *>(a.dout) + m * a.lddout, D, t);
+        if (a.w_post) R::load(static_cast<const T *>(a.w_post), D, w_post);
+        if (a.gate) R::load(static_cast<const T *>(a.gate) + m / a.per * a.D, D, gate);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) oh[i][v] *= a.alpha, cg[i][v] = 1.0f, yh[i][v] = 0.0f;
+            for (int v = 0; v < VEC; ++v) {
+                oh[i][v] *= a.alpha, cg[i][v] = 1.0f;
+                if (!a.y) yh[i][v] = 0.0f;
+                if (!a.dout) t[i][v] = 0.0f;
+            }
         if (a.y) {
-            R::load(static_cast<const T *>(a.y) + m * a.ldy, D, yh);
             if (a.drop.cut) {
                 uint32_t keep[ITEMS];
                 row_keep<VEC, ITEMS, THREADS>(a, m, keep, bytes[parity]);
@@ -244,11 +257,6 @@ __global__ void __launch_bounds__(THREADS) k_residual_norm_back(const NormArgs a
                     for (int v = 0; v < VEC; ++v) cg[i][v] = (keep[i] >> v & 1) ? a.drop.scale : 0.0f;
             }
         }
-        float w_post[ITEMS][VEC], gate[ITEMS][VEC];
-        if (a.w_post) {
-            R::load(static_cast<const T *>(a.w_post), D, w_post);
-        }
-        if (a.gate) R::load(static_cast<const T *>(a.gate) + m / a.per * a.D, D, gate);
         float s1 = 0.0f, s0 = 0.0f;
         // out again from the forward's inputs: exact, where the stored `out` is rounded
 #pragma unroll
@@ -262,17 +270,8 @@ __global__ void __launch_bounds__(THREADS) k_residual_norm_back(const NormArgs a
                 n = cg[i][v] == 0.0f ? 0.0f : n * cg[i][v];
                 if (a.y) oh[i][v] += n;
             }
-        if (a.dout) {
-            R::load(static_cast<const T *>(a.dout) + m * a.lddout, D, t);
-        } else {
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-                for (int v = 0; v < VEC; ++v) t[i][v] = 0.0f;
-        }
         if (a.w_pre) {
-            float e[ITEMS][VEC], w[ITEMS][VEC];
-            R::load(static_cast<const T *>(a.dz) + m * a.lddz, D, e);
+            float w[ITEMS][VEC];
             R::load(static_cast<const T *>(a.w_pre), D, w);
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
@@ -942,7 +941,7 @@ int by_type(int dtype, F f) {
 bool rows16(const void *p, long long ld, int bytes) { return !p || (aligned_to(p, 16) && ld * bytes % 16 == 0); }
 
 // Shares of the rows in the backward pass.  Teams: W warps of a 256-thread block (one of 16 warps alone), two blocks an
-// SM; blocks: two an SM.  A share costs a row of partial sums for each parameter, so it gets four rows at least.
+// SM; blocks: two an SM, three of up to 1024 columns.  A share costs a row of partial sums for each parameter, so it gets four rows at least.
 int team_warps(long long D, int dtype) {
     const int cols = dtype == CCDC_F32 ? 256 : 512;         // of a warp
     int w = 1;
@@ -951,7 +950,7 @@ int team_warps(long long D, int dtype) {
 }
 int row_shares(long long M, long long D, int dtype, bool teams, int sms) {
     const int w = teams ? team_warps(D, dtype) : 0;
-    const int per_sm = w == 0 ? 2 : w == 16 ? 1 : 2 * (8 / w), block = w == 0 || w == 16 ? 1 : 8 / w;
+    const int per_sm = w == 0 ? (D <= 1024 ? 3 : 2) : w == 16 ? 1 : 2 * (8 / w), block = w == 0 || w == 16 ? 1 : 8 / w;
     const long long most = (M + 3) / 4;
     const long long n = std::min<long long>((long long)per_sm * sms, std::max<long long>(1, most));
     return (int)((n + block - 1) / block * block);
@@ -1001,7 +1000,9 @@ int forward(const NormArgs &a, bool vec, int dtype, int sms, cudaStream_t s) {
         return launch_forward<T, 8, 4, 1024>(a, s);
     }
     if (a.D <= 512) return launch_forward<T, 1, 4, 128>(a, s);
+    if (a.D <= 1024) return launch_forward<T, 1, 8, 128>(a, s);
     if (a.D <= 2048) return launch_forward<T, 1, 8, 256>(a, s);
+    if (a.D <= 4096) return launch_forward<T, 1, 8, 512>(a, s);
     if (a.D <= 8192) return launch_forward<T, 1, 16, 512>(a, s);
     return launch_forward<T, 1, 32, 1024>(a, s);
 }
@@ -1014,7 +1015,9 @@ int backward(const NormArgs &a, bool vec, bool teams, int dtype, int shares, cud
         return launch_back<T, 8, 4, 1024>(a, shares, s);
     }
     if (a.D <= 512) return launch_back<T, 1, 4, 128>(a, shares, s);
+    if (a.D <= 1024) return launch_back<T, 1, 8, 128>(a, shares, s);
     if (a.D <= 2048) return launch_back<T, 1, 8, 256>(a, shares, s);
+    if (a.D <= 4096) return launch_back<T, 1, 8, 512>(a, shares, s);
     if (a.D <= 8192) return launch_back<T, 1, 16, 512>(a, shares, s);
     return launch_back<T, 1, 32, 1024>(a, shares, s);
 }
