@@ -47,7 +47,8 @@ def within(got, want, tol, what):
 @pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("rows,cols,pad,shift,offset", [(1, 1, 0, 0, 0), (1, 8, 0, 0, 0), (3, 7, 0, 0, 0), (5, 16, 8, 0, 16),
                                                         (5, 16, 8, 0, 3), (4, 33, 2, 1, 0), (2, 40, 0, 8, (1 << 34) + 8),
-                                                        (1, 1000, 0, 3, (1 << 35) + 5)])
+                                                        (1, 1000, 0, 3, (1 << 35) + 5),
+                                                        (7, 301, 0, 0, 0), (300, 3, 1, 0, 6), (9, 256, 5, 1, 7), (5, 700, 3, 0, 0)])
 def test_dropout(ccdc, dtype, rows, cols, pad, shift, offset):
     rng = np.random.default_rng(rows * 100 + cols)
     x = tensor(rng, rows, cols, dtype, pad=pad, shift=shift)
