@@ -457,7 +457,7 @@ def test_block_job(ccdc):
         out = x + unit(y) * leaves["w_post"] * leaves["gate"] * keep
         loss = out.square().mean()
         grads = torch.autograd.grad(loss, [leaves[k] for k in block_job.PARAMETERS])
-        assert abs(float(losses[n]) - float(loss)) <= 1e-5 * float(loss)
+        assert abs(float(losses[n]) - float(loss.detach())) <= 1e-5 * float(loss.detach())
         at = 0
         for k, want in zip(block_job.PARAMETERS, grads):
             got = per_file[n][at:at + want.numel()].double().view(want.shape)
@@ -480,3 +480,38 @@ def test_block_job_replicas(ccdc):
     block_job.map_file(x, params, 0.1, 5, 1000, a)
     block_job.map_file(x.clone(), {k: v.clone() for k, v in params.items()}, 0.1, 5, 1000, b)
     assert torch.equal(a, b) and bool(a.isfinite().all())
+
+
+# ---------------------------------------------------------------- offsets beyond 32 bits
+def test_more_than_two_to_the_31_elements(ccdc):
+    """the last rows of tensors of over 2^31 elements against calls on those rows alone"""
+    D = 8192
+    M = (1 << 31) // D + 40
+    x = torch.empty((M, D), dtype=torch.bfloat16, device="cuda")
+    x[-64:].normal_()
+    x[:64].normal_()
+    x[64:-64].zero_()
+    w = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    y = ccdc.dropout(x, 0.5, 3)
+    tail = x[-8:].clone()
+    assert torch.equal(y[-8:], ccdc.dropout(tail, 0.5, 3, (M - 8) * D))
+    gate = torch.randn((2, D), device="cuda").bfloat16()
+    out, z, st = ccdc.residual_norm_forward(x, y, w_post=w, w_pre=w, gate=gate, rows_per_gate=M - 20, p=0.25, seed=4, save=True)
+    how = dict(w_post=w, w_pre=w, gate=gate[1:], rows_per_gate=8, p=0.25, seed=4, offset=(M - 8) * D)
+    o, zz, s = ccdc.residual_norm_forward(tail, y[-8:].clone(), save=True, **how)
+    assert torch.equal(out[-8:], o) and torch.equal(z[-8:], zz)
+    dx, dy, *_ = ccdc.residual_norm_backward(x, z, x, y, st, w_post=w, w_pre=w, gate=gate, rows_per_gate=M - 20, p=0.25, seed=4)
+    tx, ty, *_ = ccdc.residual_norm_backward(tail, zz, tail, y[-8:].clone(), s, **how)
+    assert torch.equal(dx[-8:], tx) and torch.equal(dy[-8:], ty)
+    del out, z, st, dx, dy, y, x
+    torch.cuda.empty_cache()
+    M, D, F = (1 << 31) // 16384 + 300, 64, 16384
+    x = torch.randn((M, D), device="cuda").bfloat16()
+    wg, wu, wd = (torch.randn(s, device="cuda").bfloat16() * 0.1 for s in ((F, D), (F, D), (D, F)))
+    y, saved = ccdc.ffn_forward(x, wg, wu, wd, save=True)
+    small, kept = ccdc.ffn_forward(x[-200:], wg, wu, wd, save=True)
+    dx = ccdc.ffn_backward(y, x, wg, wu, wd, saved)[0]
+    sx = ccdc.ffn_backward(y[-200:], x[-200:], wg, wu, wd, kept)[0]
+    for a, b in ((y[-200:], small), (dx[-200:], sx)):       # other tiles, other orders of the sums
+        assert float((a.double() - b.double()).norm() / b.double().norm()) <= 2.0 ** -8
+    ccdc.block_status()
