@@ -24,9 +24,9 @@ struct Act {
             const float t = EXACT ? tanhf(v) : 1.0f - __fdividef(2.0f, 1.0f + __expf(fminf(2.0f * v, 80.0f)));
             *slope = 0.5f * (1.0f + t) + 0.5f * h * (1.0f - t * t) * k * (1.0f + 3.0f * q * h * h);
             return 0.5f * h * (1.0f + t);
-        } else {
-            *slope = h > 0.0f ? 1.0f : 0.0f;
-            return h > 0.0f ? h : 0.0f;
+        } else {        // NaN stays NaN, in the slope too: a fault upstream must not leave plausible values and gradients
+            *slope = h > 0.0f ? 1.0f : h <= 0.0f ? 0.0f : h;
+            return h <= 0.0f ? 0.0f : h;
         }
     }
 };
