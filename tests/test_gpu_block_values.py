@@ -37,3 +37,58 @@ def test_ffn_nan_in_one_weight(ccdc, dtype, act, M):
         assert g[f].isnan().all(), name
         rest = [i for i in range(96) if i != f]
         assert torch.equal(g[rest], c[rest]), name
+
+
+# ---------------------------------------------------------------- feed-forward: activations
+@pytest.mark.parametrize("M", [7, 30, 200])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", DT)
+def test_activation_tails(ccdc, act, dtype, M):
+    """act(h) and act'(h) one by one, relative to their own size far into the negative tail.
+
+    h, u = 1 and the output weight 1 pass through the products exactly, so y is act(h) rounded and dx is act'(h) rounded
+    (twice, dh and dx).  The exponential's argument t has a few roundings, |t| 2^-22 of it, which is the relative error
+    they leave in the exponential; CUDA's fast exponential adds (2 + 1.2 |t|) 2^-23 and the operations around it less
+    than 16 units of 2^-23.  gelu's erfc has |h / sqrt 2|^2 2^-22 in its argument likewise."""
+    h = np.linspace(-4.6, 4.6, M)
+    x = torch.zeros((M, 8), device="cuda", dtype=DT[dtype])
+    x[:, 0], x[:, 1] = torch.from_numpy(h).to(DT[dtype]).cuda(), 1.0
+    h = f64(x[:, 0])
+    wg, wu, wd, dy = (torch.zeros(s, device="cuda", dtype=DT[dtype]) for s in ((8, 8), (8, 8), (8, 8), (M, 8)))
+    wg[0, 0] = wu[0, 1] = wd[0, 0] = 1.0
+    dy[:, 0] = 1.0
+    y, saved = ccdc.ffn_forward(x, wg, wu, wd, act=act, save=True)
+    dx = ccdc.ffn_backward(dy, x, wg, wu, wd, saved, act=act)[0]
+    f, df, _ = ref.act(act, h)
+    k = np.sqrt(2 / np.pi)
+    t = {"silu": h, "gelu": h * h, "gelu_tanh": 2 * k * (h + 0.044715 * h ** 3), "relu": 0 * h}[act]
+    rel = (np.abs(t) * 2 ** -22 + (18 + 1.2 * np.abs(t)) * 2 ** -23) if act != "relu" else 0 * h
+    if act == "gelu":           # 1 + erf cancels in 64 bits too: the integral again, by erfc
+        import math
+
+        f = np.array([h_ * 0.5 * math.erfc(-h_ / math.sqrt(2)) for h_ in h])
+        df = np.array([0.5 * math.erfc(-h_ / math.sqrt(2)) for h_ in h]) + h * np.exp(-h * h / 2) / math.sqrt(2 * math.pi)
+    if act == "gelu_tanh":      # as does 1 + tanh
+        s = 1 / (1 + np.exp(-t))
+        f, df = h * s, s + 2 * h * s * (1 - s) * k * (1 + 3 * 0.044715 * h * h)
+    U, tiny = ref.U[dtype], ref.SMALLEST[dtype]
+    within(y[:, 0], f, np.abs(f) * (rel + U) + tiny, "act")
+    # the slope's two terms may cancel: relative to their sizes
+    first = np.abs(f / np.where(h == 0, 1, h)) + np.abs(df - f / np.where(h == 0, 1, h)) if act != "relu" else np.abs(df)
+    within(dx[:, 0], df, first * rel * 2 + np.abs(df) * (2 * U + U * U) + 2 * tiny, "slope")
+
+
+@pytest.mark.parametrize("M", [8, 40])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", DT)
+def test_activations_of_huge_values(ccdc, act, dtype, M):
+    """far out act(h) is h or 0 and act'(h) 1 or 0, however large h is"""
+    h = torch.tensor([1e3, -1e3, 6e4, -6e4] if dtype == "float16" else [1e3, -1e3, 1e13, -1e13, 1e20, -1e20, 1e38, -1e38])
+    x = torch.zeros((M, 8), device="cuda", dtype=DT[dtype])
+    x[:, 0], x[:, 1] = h.repeat(M)[:M].to(DT[dtype]).cuda(), 1.0
+    wg, wu, wd, dy = (torch.zeros(s, device="cuda", dtype=DT[dtype]) for s in ((8, 8), (8, 8), (8, 8), (M, 8)))
+    wg[0, 0] = wu[0, 1] = wd[0, 0] = 1.0
+    dy[:, 0] = 1.0
+    y, saved = ccdc.ffn_forward(x, wg, wu, wd, act=act, save=True)
+    dx = ccdc.ffn_backward(dy, x, wg, wu, wd, saved, act=act)[0]
+    assert torch.equal(y[:, 0], x[:, 0].clamp(min=0)) and torch.equal(dx[:, 0], (x[:, 0] > 0).to(x.dtype))
