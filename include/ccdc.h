@@ -491,9 +491,9 @@ int ccdc_decode_reduce_static(ccdc_plan_t *plan, const void *const *part, const 
 
 /* Dropout: y[m][n] = x[m][n] * 65536/(65536-c) where the element is kept, else 0
  * (also where x is not finite); c = round(65536 p).  Element e = offset +
- * m*cols + n takes 16 bits (the e mod 8-th of the 128, least significant first)
- * of Philox 4x32-10 with the seed as key and e / 8 as counter, and is kept
- * where they are at least c.  The mask depends on (seed, e) alone and is never
+ * m*cols + n (modulo 2^64) takes 16 bits (the e mod 8-th of the 128, least
+ * significant first) of Philox 4x32-10 with the seed as key and e / 8 as
+ * counter, and is kept where they are at least c.  The mask depends on (seed, e) alone and is never
  * stored: the backward pass is the same call on the gradient, and a replica
  * draws the same mask at every node.  0 <= p <= 1; y may be x itself (same
  * stride).  CCDC_ESIZE beyond 2^46 elements. */

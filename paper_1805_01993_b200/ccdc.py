@@ -563,7 +563,8 @@ def _empty_like(x):
 
 def dropout(x, p, seed, offset=0, out=None, stream=None):
     """``ccdc_dropout``: x with elements dropped by the counter-based mask of (seed, offset + element).
-    The backward pass is the same call on the gradient.  ``out`` may be ``x``."""
+    The backward pass is the same call on the gradient.  ``out`` may be ``x``.  Elements are numbered modulo 2^64 (an
+    ``offset`` of -8 is 2^64 - 8)."""
     ctx = _elsewhere(x, stream)
     if ctx is not None:
         with ctx:

@@ -103,7 +103,9 @@ __device__ __forceinline__ void store8(T *p, const Eight<T> &r) {
 // The generator of the dropout masks: Philox 4x32 with 10 rounds (Salmon, Moraes, Dror and Shaw, "Parallel
 // Random Numbers: As Easy as 1, 2, 3", 2011).  Key = the two words of the seed; counter = (element / 8, 0),
 // so that eight elements share one call and an element's number depends on (seed, element) alone: every
-// replica of a file draws the same mask wherever and in whatever order it is computed.
+// replica of a file draws the same mask wherever and in whatever order it is computed.  Element numbers are taken modulo
+// 2^64, counters modulo 2^61 (COUNTERS).
+constexpr unsigned long long COUNTERS = ~0ull >> 3;
 // A probability in 1/65536 steps, and the factor of kept elements: that of the rounded probability, so that the
 // expectation is exact.  p = 1 drops everything.
 struct Dropout {

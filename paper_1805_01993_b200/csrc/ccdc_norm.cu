@@ -124,7 +124,7 @@ __device__ __forceinline__ void row_keep(const NormArgs &a, long long m, uint32_
         return;
     }
     const int shift = (int)(e0 & 7), n = (shift + D + 7) >> 3;
-    for (int j = threadIdx.x; j < n; j += THREADS) bytes[j] = (uint8_t)keep_bits(a.drop, (e0 >> 3) + j);
+    for (int j = threadIdx.x; j < n; j += THREADS) bytes[j] = (uint8_t)keep_bits(a.drop, ((e0 >> 3) + j) & COUNTERS);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
@@ -913,14 +913,15 @@ struct DropArgs {
 };
 template <class T, bool FAST>
 __global__ void __launch_bounds__(256) k_dropout(const DropArgs a) {
+    // counters c of the calls, from the first element's on; element numbers and so counters go round at 2^64 elements
     const unsigned long long n = (unsigned long long)a.rows * a.cols;
-    const unsigned long long c0 = a.drop.offset >> 3, c1 = (a.drop.offset + n + 7) >> 3;
+    const unsigned long long c0 = a.drop.offset >> 3, calls = ((a.drop.offset & 7) + n + 7) >> 3;
     const T *x = static_cast<const T *>(a.x);
     T *y = static_cast<T *>(a.y);
     if constexpr (FAST) {
-        for (unsigned long long c = c0 + blockIdx.x * 256ull + threadIdx.x; c < c1; c += gridDim.x * 256ull) {
-            const uint4 w = a.drop.cut ? drop_words(a.drop, c) : make_uint4(~0u, ~0u, ~0u, ~0u);
-            const unsigned long long e = (c - c0) * 8;
+        for (unsigned long long c = blockIdx.x * 256ull + threadIdx.x; c < calls; c += gridDim.x * 256ull) {
+            const uint4 w = a.drop.cut ? drop_words(a.drop, (c0 + c) & COUNTERS) : make_uint4(~0u, ~0u, ~0u, ~0u);
+            const unsigned long long e = c * 8;
             const long long m = a.rows == 1 ? 0 : (long long)(e / a.cols);
             const long long j = (long long)(e - (unsigned long long)m * a.cols);
             if (j + 8 <= a.cols) {
@@ -937,12 +938,12 @@ __global__ void __launch_bounds__(256) k_dropout(const DropArgs a) {
         }
     } else {
         const int lane = threadIdx.x & 31;
-        for (unsigned long long c = c0 + (blockIdx.x * 256ull + threadIdx.x) / 32 * 32; c < c1; c += gridDim.x * 256ull) {
-            const uint32_t bits = a.drop.cut ? keep_bits(a.drop, c + lane) : 0xFFu;
-            const long long first = (long long)(c * 8 - a.drop.offset);         // may lie before the tensor
+        for (unsigned long long c = (blockIdx.x * 256ull + threadIdx.x) / 32 * 32; c < calls; c += gridDim.x * 256ull) {
+            const uint32_t bits = a.drop.cut ? keep_bits(a.drop, (c0 + c + lane) & COUNTERS) : 0xFFu;
+            const long long first = (long long)(c * 8) - (long long)(a.drop.offset & 7);    // may lie before the tensor
             const long long base = first > 0 ? first : 0;
             const long long m0 = base / a.cols, j0 = base - m0 * a.cols;
-T v[8];
+            T v[8];
             long long to[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {           // all loads before the first store

@@ -92,3 +92,24 @@ def test_activations_of_huge_values(ccdc, act, dtype, M):
     y, saved = ccdc.ffn_forward(x, wg, wu, wd, act=act, save=True)
     dx = ccdc.ffn_backward(dy, x, wg, wu, wd, saved, act=act)[0]
     assert torch.equal(y[:, 0], x[:, 0].clamp(min=0)) and torch.equal(dx[:, 0], (x[:, 0] > 0).to(x.dtype))
+
+
+# ---------------------------------------------------------------- dropout: the last element numbers
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,cols,before", [(1, 64, 24), (4, 16, 40), (4, 16, 21), (3, 51, 100), (1, 8, 8), (5, 7, 1), (2, 64, 4)])
+def test_dropout_counts_modulo_64_bits(ccdc, rows, cols, before, dtype):
+    """elements are numbered modulo 2^64: offset = 2^64 - before passes the end inside the tensor"""
+    offset, seed, n = (1 << 64) - before, 0xABCDEF0123456789, rows * cols
+    keep = np.concatenate([ref.keep_factors(1, min(before, n), 0.4, seed, offset)[0],
+                           ref.keep_factors(1, max(0, n - before), 0.4, seed, 0)[0]]).reshape(rows, cols)
+    rng = np.random.default_rng(cols)
+    x = tensor(rng, rows, cols, dtype)
+    want = f64(x) * keep
+    for off in (offset, -before):
+        out = torch.full_like(x, 9.0)
+        ccdc.dropout(x, 0.4, seed, off, out=out)
+        within(out, want, np.abs(want) * (ref.U[dtype] + 3 * 2.0 ** -24) + ref.SMALLEST[dtype], "y")
+        fused, _, stats = ccdc.residual_norm_forward(torch.zeros_like(x), x, p=0.4, seed=seed, offset=off, save=True)
+        assert torch.equal(fused, out)
+        _, dy, *_ = ccdc.residual_norm_backward(x, None, torch.zeros_like(x), x, stats, p=0.4, seed=seed, offset=off)
+        assert torch.equal(dy, out)
