@@ -24,7 +24,7 @@ constexpr long long MAX_D = 32768;      // columns of a row that fit a block's r
 struct NormArgs {
     long long M, D;
     const void *x, *y, *w_post, *w_pre, *gate;
-    long long ldx, ldy, per;            // per: rows that share a gate row
+    long long ldx, ldy, per;            // per: rows that share a gate row, at most M (its multiples stay within 64 bits)
     float alpha, eps;
     int layer;
     Dropout drop;
@@ -1116,7 +1116,7 @@ int ccdc_residual_norm_forward(long long M, long long D, int dtype, int kind, fl
     if (M == 0) return CCDC_OK;
     NormArgs a = {};
     a.M = M, a.D = D, a.x = x, a.y = y, a.w_post = w_post, a.w_pre = w_pre, a.gate = gate;
-    a.ldx = ldx, a.ldy = ldy, a.per = gate ? rows_per_gate : M, a.alpha = alpha, a.eps = eps;
+    a.ldx = ldx, a.ldy = ldy, a.per = gate ? std::min(rows_per_gate, M) : M, a.alpha = alpha, a.eps = eps;
     a.layer = kind == CCDC_NORM_LAYER, a.out = out, a.ldo = ldo, a.z = z, a.ldz = ldz, a.stats = static_cast<float4 *>(stats);
     make_dropout(p, seed, offset, &a.drop);
     const int b = type_bytes(dtype);
@@ -1169,7 +1169,7 @@ int ccdc_residual_norm_backward(long long M, long long D, int dtype, int grad_dt
         return CCDC_EINVAL;
     NormArgs a = {};
     a.M = M, a.D = D, a.x = x, a.y = y, a.w_post = w_post, a.w_pre = w_pre, a.gate = gate;
-    a.ldx = ldx, a.ldy = ldy, a.per = gate ? rows_per_gate : M, a.alpha = alpha;
+    a.ldx = ldx, a.ldy = ldy, a.per = gate ? std::min(rows_per_gate, M) : M, a.alpha = alpha;
     a.layer = kind == CCDC_NORM_LAYER, a.stats = const_cast<float4 *>(static_cast<const float4 *>(stats));
     a.dout = dout, a.lddout = lddout, a.dz = dz, a.lddz = lddz, a.dx = dx, a.lddx = lddx, a.dy = dy, a.lddy = lddy;
     a.dgate = dgate, a.grad_f32 = grad_dtype == CCDC_F32, a.partial = static_cast<float *>(workspace);

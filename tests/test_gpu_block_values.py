@@ -113,3 +113,19 @@ def test_dropout_counts_modulo_64_bits(ccdc, rows, cols, before, dtype):
         assert torch.equal(fused, out)
         _, dy, *_ = ccdc.residual_norm_backward(x, None, torch.zeros_like(x), x, stats, p=0.4, seed=seed, offset=off)
         assert torch.equal(dy, out)
+
+
+# ---------------------------------------------------------------- norms: group sizes beyond the rows
+@pytest.mark.parametrize("M,D", [(1, 64), (300, 64), (300, 51), (1000, 4096)])
+def test_gate_row_for_more_rows_than_there_are(ccdc, M, D):
+    rng = np.random.default_rng(M)
+    x, y, w_post, w_pre, g = norm_case(rng, M, D, "float32", True, M)
+    dout, dz = tensor(rng, M, D, "float32"), tensor(rng, M, D, "float32")
+    res = []
+    for per in (M, M + 1, (1 << 63) - 1):
+        how = dict(w_post=w_post, w_pre=w_pre, gate=g, rows_per_gate=per, p=0.25, seed=3)
+        out, z, st = ccdc.residual_norm_forward(x, y, save=True, **how)
+        into = torch.full_like(g, 9.0)
+        res.append((out, z, *ccdc.residual_norm_backward(dout, dz, x, y, st, dgate=into, **how)))
+    for other in res[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(res[0], other))
