@@ -546,7 +546,9 @@ int ccdc_residual_norm_backward(long long M, long long D, int dtype, int grad_dt
  * dx [M][D], dw_gate and dw_up [F][D], dw_down [D][F] contiguous, each may be NULL.
  * a, dh and du, which enter further products, are kept in the tensors' type; h
  * and u in binary32 (rounding them too would take the gradients' error from 1.4
- * to 1.8 times that of their own rounding).
+ * to 1.8 times that of their own rounding).  Infinities and NaN follow IEEE
+ * arithmetic in every type and for any number of rows, but for one thing: with
+ * more than 32 rows of binary32, an infinity times a value below 2^-126 may be NaN.
  * workspace: ccdc_ffn_workspace_bytes(..., backward, aligned), 16-byte aligned;
  * aligned != 0 promises that every pointer and row stride is a multiple of 16
  * bytes (D and F too), which needs less.  workspace_bytes smaller than the call

@@ -1,7 +1,26 @@
-// Activations of the gated feed-forward block.
+// Activations of the gated feed-forward block, and the planes of binary32 operands.
 #pragma once
 
 #include "ccdc_block.h"
+
+// Binary32 values as three bf16 planes, v = hi + mid + lo, each plane what is left rounded to bf16: 24 bits between them.
+// Takes the next plane off two values and returns it as a word, x's in the low half.
+__device__ __forceinline__ uint32_t next_plane(float &x, float &y) {
+    const uint32_t word = pack2<bf16>(x, y);
+    const float2 f = unpack2<bf16>(word);
+    x -= f.x, y -= f.y;
+    return word;
+}
+// The first plane takes this form unless all values are below FIRST_MOST in size: above it they would round to infinity
+// and are cut off to the largest bf16 instead; infinities and NaN stay in the first plane.  Other values as above.
+constexpr float FIRST_MOST = 0x1.FFp127f;
+__device__ __forceinline__ uint32_t first_plane_of_any(float &x, float &y) {
+    float2 f = unpack2<bf16>(pack2<bf16>(x, y));
+    if (!isfinite(f.x)) f.x = __bfloat162float(__float2bfloat16_rz(x));
+    if (!isfinite(f.y)) f.y = __bfloat162float(__float2bfloat16_rz(y));
+    x = isfinite(f.x) ? x - f.x : 0.0f, y = isfinite(f.y) ? y - f.y : 0.0f;
+    return pack2<bf16>(f.x, f.y);
+}
 
 // act(h); act'(h) through `slope`.  EXACT: the library's full-precision functions, for binary32 blocks; otherwise
 // their fast forms, for results that are rounded to 16 bits.  With t the exponential's argument, act is off by less than

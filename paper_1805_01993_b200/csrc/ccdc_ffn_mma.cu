@@ -22,13 +22,17 @@
 // Binary32 blocks: an operand is three bf16 planes, and a product the six plane products that reach 2^-24.  The tensor
 // cores add to an accumulator with truncation, a bias of about 2^-24 of the running sum for every K = 16 step: 10^-5 at
 // K = 4096, harmless under the rounding of 16-bit results but not here.  So a stage holds all planes of 64 k (each is
-// fetched once for its products), the small products accumulate first, and after every stage the accumulator (one of
-// four) is added to registers with rounding.  Tile 256 x 128 by a pair: the registers' share of it fits.
+// fetched once for its products), and after every stage the accumulator of hi hi (one of three) is added to registers
+// with rounding.  The five small products have an accumulator of their own: 2^-8 of the size, they bear 32 stages of
+// truncation, and where an operand is infinite they mean nothing (infinity times a plane of a finite value, which may be
+// zero or of the other sign) and are left out: hi hi alone has the result of IEEE arithmetic there.  (All six in one
+// accumulator of four took 3 % less time and was off by 6 % more.)  Tile 256 x 128 by a pair: the registers' share of it
+// fits.
 //
 // Measured: 2048 rows, 4096 x 8192, bf16: forward 0.33 ms, 1.26 PFLOP/s; 8192 rows, 4096 x 16384 forward and backward
 // 7.99 ms, 1.24 PFLOP/s (256 x 256 tiles alone: 10.1 ms).  Between epilogues a step of 64 k on the large tile takes about
 // 1056 cycles, 1024 at the tensor cores' rate; the gate's epilogue costs 16 %, its backward pass's 25 % of their launches.
-// 1024 rows, 1024 x 4096 in binary32, forward and backward: 0.57 ms.
+// 1024 rows, 1024 x 4096 in binary32, forward and backward: 0.58 ms.
 //
 // All waits are bounded: one that runs out sets g_wait_failed and the thread goes on without waiting.
 #include <cuda.h>
@@ -46,6 +50,7 @@ constexpr int BLOCK_BYTES = 16384, BOX_BYTES = 8192;    // 128 x 64 of an operan
 constexpr int FETCH_BYTES = 12 * BLOCK_BYTES;           // ring of fetched blocks
 constexpr int BLOCK_K = 64;
 constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
+constexpr int SMALL_STEPS = 32;                         // steps of 64 k between drains of the small plane products
 constexpr int RING_SLOT = 2048, RING_SLOTS = 2;         // 32 rows of 64 bytes
 constexpr int SMEM_BYTES = FETCH_BYTES + EPI_WARPS * RING_SLOT * RING_SLOTS + 1024 + 256;
 constexpr int WAIT_LIMIT = 1 << 20;
@@ -58,7 +63,7 @@ struct alignas(64) Problem {
     long long ldc, split_stride;
     float *h, *u;
     int M, N, tiles_m, tiles_n, splits, first, kblocks, terms;
-    int a_across, b_across, c_f32, c_tma, planes, act, groups;
+    int a_across, b_across, c_f32, c_tma, act, groups;
     uint32_t idesc;
 };
 struct Work {
@@ -191,10 +196,10 @@ struct Output {
     void *cp;
     long long ldc, split_stride;
     float *h, *u;
-    int M, N, c_f32, c_tma, planes, act, groups;
+    int M, N, c_f32, c_tma, act, groups;
     __device__ __forceinline__ explicit Output(const Problem &p)
         : c0(&p.c[0]), c1(&p.c[1]), cp(p.cp), ldc(p.ldc), split_stride(p.split_stride), h(p.h), u(p.u), M(p.M), N(p.N),
-          c_f32(p.c_f32), c_tma(p.c_tma), planes(p.planes), act(p.act), groups(p.groups) {}
+          c_f32(p.c_f32), c_tma(p.c_tma), act(p.act), groups(p.groups) {}
 };
 
 // The epilogue warps' way out: 32 rows of 64 bytes a slot, swizzled so that the row writes meet no bank conflict.
@@ -228,22 +233,34 @@ __device__ __forceinline__ void put16(char *slot, int row, const float (&f)[32])
                        pack2<T>(f[8 * c + 4], f[8 * c + 5]), pack2<T>(f[8 * c + 6], f[8 * c + 7]));
 }
 // 32 columns as 16-bit words, or as the planes of binary32 words
-__device__ __forceinline__ void emit(const Output &p, const CUtensorMap *map, int f16, float (&f)[32], int col, int row0,
-                                     int lane, Ring &ring) {
-    for (int z = 0; z < p.planes; ++z) {
+template <bool PLANES>
+__device__ __forceinline__ void emit(const CUtensorMap *map, int f16, float (&f)[32], int col, int row0, int lane, Ring &ring) {
+    if constexpr (!PLANES) {
         char *slot = ring.next(lane);
         if (f16)
             put16<fp16>(slot, lane, f);
         else
             put16<bf16>(slot, lane, f);
-        out_by_tma(map, col, row0, z, slot, lane);
-        if (z + 1 < p.planes) {
+        out_by_tma(map, col, row0, 0, slot, lane);
+    } else {
+        auto plane = [&](int z, auto next) {
+            char *slot = ring.next(lane);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {     // infinities and NaN stay in the first plane
-                const float hi = to_f32<bf16>(from_f32<bf16>(f[i]));
-                f[i] = isfinite(hi) ? f[i] - hi : 0.0f;
+            for (int c = 0; c < 4; ++c) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = next(f[8 * c + 2 * i], f[8 * c + 2 * i + 1]);
+                *reinterpret_cast<uint4 *>(slot_at(slot, lane, c)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
-        }
+            out_by_tma(map, col, row0, z, slot, lane);
+        };
+        bool plain = true;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) plain = plain && fabsf(f[i]) < FIRST_MOST;
+        int z = 0;
+        if (!__all_sync(~0u, plain)) plane(z++, first_plane_of_any);
+#pragma unroll 1
+        for (; z < 3; ++z) plane(z, next_plane);
     }
 }
 
@@ -317,7 +334,7 @@ __device__ __forceinline__ void gate_columns(const Output &p, int f16, float (&h
             u[i] *= act(h[i], &slope);
         }
     });
-    emit(p, p.c0, f16, u, col, row0, lane, ring);
+    emit<EXACT>(p.c0, f16, u, col, row0, lane, ring);
 }
 // d (da on entry) becomes dh, du the other
 template <bool EXACT>
@@ -343,8 +360,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
     constexpr int STAGE_BYTES = PLANES ? 3 * (BLOCK_BYTES + BOX_BYTES) : (1 + NB) * BLOCK_BYTES;
     constexpr int B_AT = PLANES ? 3 * BLOCK_BYTES : BLOCK_BYTES;    // A's blocks come first
     constexpr int STAGES = FETCH_BYTES / STAGE_BYTES;
-    constexpr int ACCS = PLANES ? 4 : 512 / TILE_N < 2 ? 1 : 2;     // accumulators in tensor memory
-    constexpr uint32_t TMEM_COLUMNS = ACCS * TILE_N;
+    constexpr int ACCS = PLANES ? 3 : 512 / TILE_N < 2 ? 1 : 2;     // accumulators in tensor memory
+    constexpr int SMALL_AT = ACCS * TILE_N;                         // PLANES: the small products' accumulator
+    constexpr uint32_t TMEM_COLUMNS = (ACCS + PLANES) * TILE_N;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank = 0;
     if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -354,10 +372,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
     uint64_t *bars = reinterpret_cast<uint64_t *>(ring_base + EPI_WARPS * RING_SLOT * RING_SLOTS);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 2 * STAGES + 8);
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 32;
+    const uint32_t small_empty = acc_empty + 8 * ACCS;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
         for (int i = 0; i < ACCS; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, EPI_WARPS * CG);
+        if constexpr (PLANES) bar_init(small_empty, EPI_WARPS * CG);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -442,7 +462,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t stage = 0, phase = 0, sums = 0;
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, small_phase = 0;
             for (int item = cluster; item < w.items; item += clusters) {
                 const Tile t = tile_of(w, item);
                 const Problem &p = w.p[t.problem];
@@ -450,10 +470,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                 const uint64_t a0 = operand_desc(smem_u32(smem), p.a_across);
                 const uint64_t b0 = operand_desc(smem_u32(smem) + B_AT, p.b_across);
                 const uint32_t a_step = p.a_across ? 2048 >> 4 : 32 >> 4, b_step = p.b_across ? 2048 >> 4 : 32 >> 4;
-                for (int it = t.it0; it < t.it1; ++sums) {
+                for (int it = t.it0; it < t.it1;) {
                     const int end = PLANES ? it + 1 : t.it1;
-                    const uint32_t acc = sums % ACCS, d = tmem + acc * TILE_N;
-                    bar_wait<CG>(acc_empty + 8 * acc, (sums / ACCS & 1) ^ 1, limit);
+                    const uint32_t d = tmem + acc * TILE_N;
+                    bar_wait<CG>(acc_empty + 8 * acc, acc_phase ^ 1, limit);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     bool add = false;
                     for (; it < end; ++it) {
@@ -461,16 +481,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint64_t a = a0 + stage * (STAGE_BYTES >> 4), b = b0 + stage * (STAGE_BYTES >> 4);
                         if constexpr (PLANES) {
-                            // plane products, the small ones first: lo hi, hi lo, mid mid, mid hi, hi mid, hi hi
+                            const bool first = (it - t.it0) % SMALL_STEPS == 0;
+                            if (first) {
+                                bar_wait<CG>(small_empty, small_phase ^ 1, limit);
+                                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                                small_phase ^= 1;
+                            }
+                            // lo hi, hi lo, mid mid, mid hi, hi mid, and apart from them hi hi
                             constexpr int order[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
 #pragma unroll
                             for (int i = 0; i < 6; ++i)
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    mma<CG>(d, a + order[i][0] * (BLOCK_BYTES >> 4) + k * a_step,
-                                            b + order[i][1] * (BOX_BYTES >> 4) + k * b_step, idesc, add);
-                                    add = true;
-                                }
+                                for (int k = 0; k < 4; ++k)
+                                    mma<CG>(i < 5 ? tmem + SMALL_AT : d, a + order[i][0] * (BLOCK_BYTES >> 4) + k * a_step,
+                                            b + order[i][1] * (BOX_BYTES >> 4) + k * b_step, idesc,
+                                            i < 5 ? !first || i + k > 0 : k > 0);
                         } else {
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
@@ -484,6 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                         if (++stage == STAGES) stage = 0, phase ^= 1;
                     }
                     mma_commit<CG>(acc_full + 8 * acc);
+                    if (++acc == ACCS) acc = 0, acc_phase ^= 1;
                 }
             }
         }
@@ -492,15 +518,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
         const int part = (warp - 2) >> 2;           // two warps a quarter: each takes half of the columns
         const int f16 = w.f16;
         Ring ring = {ring_base + (warp - 2) * RING_SLOT * RING_SLOTS, 0};
-        uint32_t sums = 0;
-        auto release = [&](uint32_t acc) {
+        uint32_t acc = 0, acc_phase = 0;
+        auto release = [&](uint32_t bar) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
                 if constexpr (CG == 2)
-                    bar_arrive_cluster(in_first(acc_empty + 8 * acc));
+                    bar_arrive_cluster(in_first(bar));
                 else
-                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
+                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
             }
         };
         constexpr int COLS = EPI == MMA_GATE ? TILE_N / 2 : TILE_N;     // output columns of a tile
@@ -513,10 +539,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
             const int col0 = t.n * COLS + part * (COLS / 2), col1 = min(p.N, col0 + COLS / 2);
             const long long block = (long long)(row0 >> 5) * p.groups;
             if constexpr (!PLANES) {
-                const uint32_t acc = sums % ACCS, from = tmem + acc * TILE_N + part * (COLS / 2) + lanes;
+                const uint32_t from = tmem + acc * TILE_N + part * (COLS / 2) + lanes;
                 float4 h[8], u[8];
                 if (EPI == MMA_GATE_BACK && rows && col0 < col1) load_saved(p, block, col0, lane, h, u);
-                bar_wait<CG>(acc_full + 8 * acc, sums / ACCS & 1, limit);
+                bar_wait<CG>(acc_full + 8 * acc, acc_phase, limit);
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (int c = 0; rows && col0 + c < col1; c += 32) {
                     float f[32];
@@ -534,27 +560,37 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                         float g[32];
                         gate_back_columns<false>(p, f, g, h, u);
                         if (col0 + c + 32 < col1) load_saved(p, block, col0 + c + 32, lane, h, u);     // on their way during the stores
-                        emit(p, p.c0, f16, f, col0 + c, row0, lane, ring);
-                        emit(p, p.c1, f16, g, col0 + c, row0, lane, ring);
+                        emit<false>(p.c0, f16, f, col0 + c, row0, lane, ring);
+                        emit<false>(p.c1, f16, g, col0 + c, row0, lane, ring);
                     }
                 }
-                release(acc);
-                ++sums;
+                release(acc_empty + 8 * acc);
+                if (++acc == ACCS) acc = 0, acc_phase ^= 1;
             } else {
                 // this warp's 64 columns: GATE 32 of h and the 32 of u that belong to them
                 constexpr int SECOND = EPI == MMA_GATE ? TILE_N / 2 : 32;
                 float f[2][32] = {};
-                for (int it = t.it0; it < t.it1; ++it, ++sums) {
-                    const uint32_t acc = sums % ACCS, from = tmem + acc * TILE_N + part * (COLS / 2) + lanes;
-                    bar_wait<CG>(acc_full + 8 * acc, sums / ACCS & 1, limit);
+                const uint32_t columns = tmem + part * (COLS / 2) + lanes;
+                for (int it = t.it0; it < t.it1; ++it) {
+                    bar_wait<CG>(acc_full + 8 * acc, acc_phase, limit);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     float v[2][32];
-                    tmem_load(from, v[0]);
-                    tmem_load(from + SECOND, v[1]);
+                    tmem_load(columns + acc * TILE_N, v[0]);
+                    tmem_load(columns + acc * TILE_N + SECOND, v[1]);
                     tmem_wait();
-                    release(acc);
+                    release(acc_empty + 8 * acc);
+                    if (++acc == ACCS) acc = 0, acc_phase ^= 1;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) f[0][i] += v[0][i], f[1][i] += v[1][i];
+                    if ((it - t.it0) % SMALL_STEPS != SMALL_STEPS - 1 && it + 1 < t.it1) continue;
+                    tmem_load(columns + SMALL_AT, v[0]);
+                    tmem_load(columns + SMALL_AT + SECOND, v[1]);
+                    tmem_wait();
+                    release(small_empty);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) f[j][i] = isfinite(f[j][i]) ? f[j][i] + v[j][i] : f[j][i];
                 }
                 if (rows && col0 < col1) {
                     if constexpr (EPI == MMA_GATE) {
@@ -570,8 +606,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                                 load_saved(p, block, col0 + 32 * j, lane, h, u);
                                 float g[32];
                                 gate_back_columns<true>(p, f[j], g, h, u);
-                                emit(p, p.c0, f16, f[j], col0 + 32 * j, row0, lane, ring);
-                                emit(p, p.c1, f16, g, col0 + 32 * j, row0, lane, ring);
+                                emit<true>(p.c0, f16, f[j], col0 + 32 * j, row0, lane, ring);
+                                emit<true>(p.c1, f16, g, col0 + 32 * j, row0, lane, ring);
                             }
                         }
                     }
@@ -692,13 +728,12 @@ int mma_launch(const MmaProduct *products, int count, MmaEpilogue epilogue, int 
         for (int t = 0; t < q.terms; ++t) side(&p.a[t], q.a[t], q.a[t].transposed);
         for (int t = 0; t < nb; ++t) side(&p.b[t], q.b[t], q.b[t].transposed || halves);
         if (epilogue == MMA_STORE) {
-            p.cp = q.c, p.ldc = q.ldc, p.split_stride = q.M * q.ldc, p.c_f32 = q.c_type == CCDC_F32, p.planes = 1;
+            p.cp = q.c, p.ldc = q.ldc, p.split_stride = q.M * q.ldc, p.c_f32 = q.c_type == CCDC_F32;
             p.c_tma = aligned_to(q.c, 16) && q.ldc * type_bytes(q.c_type) % 16 == 0;
             if (p.c_tma) ok = ok && encode(&p.c[0], q.c_type, q.c, q.N, q.M, q.ldc, p.splits, p.c_f32 ? 16 : 32, 32);
         } else {
-            p.planes = q.out[0].planes;
             for (int t = 0; t < (epilogue == MMA_GATE ? 1 : 2); ++t)
-                ok = ok && encode(&p.c[t], type, q.out[t].p, q.out[t].cols, q.out[t].rows, q.out[t].ld, p.planes, 32, 32);
+                ok = ok && encode(&p.c[t], type, q.out[t].p, q.out[t].cols, q.out[t].rows, q.out[t].ld, q.out[t].planes, 32, 32);
         }
         if (!ok) return CCDC_ECUDA;
     }

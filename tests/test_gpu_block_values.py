@@ -39,6 +39,74 @@ def test_ffn_nan_in_one_weight(ccdc, dtype, act, M):
         assert torch.equal(g[rest], c[rest]), name
 
 
+# ---------------------------------------------------------------- feed-forward: infinities
+def same_kind(got, want, what):
+    got = f64(got)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    big = np.isinf(want)
+    assert np.array_equal(np.isinf(got), big) and np.array_equal(got[big], want[big]), what
+
+
+@pytest.mark.parametrize("M", [8, 32, 33, 150])
+@pytest.mark.parametrize("act", ["silu", "relu"])
+@pytest.mark.parametrize("dtype", DT)
+def test_ffn_infinities(ccdc, dtype, act, M):
+    """An infinity times a finite value is an infinity, whatever that value's bits (quarters here, which 8 bits hold) and
+    however many rows the call has."""
+    rng = np.random.default_rng(M)
+    D, F = 72, 80
+
+    def quarters(*shape):
+        return torch.from_numpy(rng.integers(1, 4, shape) * rng.choice([-0.25, 0.25], shape)).to(DT[dtype]).cuda()
+
+    x, wg, wu, wd, dy = quarters(M, D), quarters(F, D), quarters(F, D), quarters(D, F), quarters(M, D)
+    wg[:, 3], wu[:, 3] = wg[:, 3].abs(), -wu[:, 3].abs()            # h = inf and u = -inf where x[., 3] is inf
+    wd[::2], wd[1::2] = wd[::2].abs(), -wd[1::2].abs()              # and y an infinity of either sign
+    clean, saved = ccdc.ffn_forward(x, wg, wu, wd, act=act, save=True)
+    dirty = x.clone()
+    dirty[5, 3] = float("inf")
+    y = ccdc.ffn_forward(dirty, wg, wu, wd, act=act)
+    rest = [i for i in range(M) if i != 5]
+    assert torch.equal(y[rest], clean[rest])
+    assert bool((y[5, ::2] == -float("inf")).all() and (y[5, 1::2] == float("inf")).all())
+    # an infinite weight: every row of one inner column
+    bad = wu.clone()
+    bad[9, 7] = float("inf")
+    with np.errstate(all="ignore"):
+        h, u = f64(x) @ f64(wg).T, f64(x) @ f64(bad).T
+        assert np.isinf(u[:, 9]).all() and np.isfinite(np.delete(u, 9, 1)).all()
+        want = (ref.act(act, h)[0] * u) @ f64(wd).T
+    same_kind(ccdc.ffn_forward(x, wg, bad, wd, act=act), want, "y")
+    # an infinite gradient of one output: its row of da, and what that enters
+    dirty = dy.clone()
+    dirty[2, 4] = -float("inf")
+    with np.errstate(all="ignore"):
+        u = f64(x) @ f64(wu).T
+        f, df, _ = ref.act(act, h)
+        da = f64(dirty) @ f64(wd)
+        assert np.isinf(da[2]).all()
+        dh, du = da * u * df, da * f
+        want = {"dx": dh @ f64(wg) + du @ f64(wu), "dw_gate": dh.T @ f64(x), "dw_up": du.T @ f64(x),
+                "dw_down": f64(dirty).T @ (f * u)}
+    for name, g in zip(GRADS, ccdc.ffn_backward(dirty, x, wg, wu, wd, saved, act=act)):
+        same_kind(g, want[name], name)
+
+
+@pytest.mark.parametrize("M", [32, 33, 150])
+def test_ffn_largest_binary32(ccdc, M):
+    """finite values that no 16-bit type holds: above the largest bf16, met by weights at the small end"""
+    rng = np.random.default_rng(M)
+    x, wg, wu, wd, dy = ffn_case(rng, M, 72, 80, "float32", 0, 0)
+    large = float(np.finfo(np.float32).max)
+    x[3, 2], x[4, 2] = large, -0.9999 * large
+    x[:3, 2], x[5:, 2] = 0.0, 0.0
+    wg[:, 2], wu[:, 2] = 2.0 ** -126, -(2.0 ** -126)
+    wg[11, 6], wu[12, 6] = large, -large
+    x[:, 6] = 2.0 ** -126 * (1 + torch.arange(M, device="cuda") % 2)
+    want = ref.ffn(*(f64(t) for t in (x, wg, wu, wd)), "silu", None, "float32")
+    within(ccdc.ffn_forward(x, wg, wu, wd), *want["y"], "y")
+
+
 # ---------------------------------------------------------------- feed-forward: activations
 @pytest.mark.parametrize("M", [7, 30, 200])
 @pytest.mark.parametrize("act", ACTS)
