@@ -202,7 +202,8 @@ struct Output {
           c_f32(p.c_f32), c_tma(p.c_tma), act(p.act), groups(p.groups) {}
 };
 
-// The epilogue warps' way out: 32 rows of 64 bytes a slot, swizzled so that the row writes meet no bank conflict.
+// The epilogue warps' way out: 32 rows of 64 bytes a slot, swizzled so that the row writes meet no bank conflict.  Every use
+// of a slot ends with a group of bulk stores (or an empty one): all but the last group read out means this slot is free.
 struct Ring {
     char *base;
     int slot;
@@ -301,6 +302,8 @@ __device__ __forceinline__ void store_columns(const Output &p, int f16, const fl
                     static_cast<uint16_t *>(p.cp)[to] = *reinterpret_cast<uint16_t *>(slot_at(slot, r, c >> 3) + (c & 7) * 2);
             }
         __syncwarp();
+        // an empty group: next() counts groups, and one of an earlier product may still be read from the other slot
+        if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
 }
 // h and u of 32 columns of this thread's row

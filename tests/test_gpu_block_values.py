@@ -162,6 +162,23 @@ def test_activations_of_huge_values(ccdc, act, dtype, M):
     assert torch.equal(y[:, 0], x[:, 0].clamp(min=0)) and torch.equal(dx[:, 0], (x[:, 0] > 0).to(x.dtype))
 
 
+# ---------------------------------------------------------------- products whose outputs take different ways out
+@pytest.mark.parametrize("M,D,F,dtype", [(700, 512, 1111, "bfloat16"), (390, 264, 777, "float16"), (300, 256, 515, "float32")])
+def test_ffn_mixed_outputs(ccdc, M, D, F, dtype):
+    """one launch whose products leave partly by copies of whole tiles (widths of 16-byte multiples) and partly by plain
+    stores (dw_down, whose rows of F are not), element by element"""
+    rng = np.random.default_rng(M)
+    x, wg, wu, wd, dy = ffn_case(rng, M, D, F, dtype, 0, 0)
+    want = ref.ffn(*(f64(t) for t in (x, wg, wu, wd)), "silu", f64(dy), dtype)
+    y, saved = ccdc.ffn_forward(x, wg, wu, wd, save=True)
+    within(y, *want["y"], "y")
+    first = ccdc.ffn_backward(dy, x, wg, wu, wd, saved)
+    for name, g in zip(GRADS, first):
+        within(g, *want[name], name)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, ccdc.ffn_backward(dy, x, wg, wu, wd, saved)))
+
+
 # ---------------------------------------------------------------- dropout: the last element numbers
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("rows,cols,before", [(1, 64, 24), (4, 16, 40), (4, 16, 21), (3, 51, 100), (1, 8, 8), (5, 7, 1), (2, 64, 4)])
