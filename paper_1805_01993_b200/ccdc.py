@@ -534,6 +534,25 @@ def _vector(t, name, like, n, dtype=None):
     return t.data_ptr()
 
 
+def _buffer(t, name, like, need=0):
+    """(address, bytes) of scratch or saved values that the caller brings: one piece of memory on like's device."""
+    size = t.numel() * t.element_size()
+    if t.get_device() != like.get_device() or not t.is_contiguous() or size < need:
+        raise ValueError(f"{name}: a contiguous tensor{f' of {need} bytes' if need else ''} on {like.device} expected")
+    return t.data_ptr(), size
+
+
+def _scratch(workspace, need, x):
+    """(address, bytes, tensor) of the caller's workspace, or of a new one of need() bytes.  Its size is the C entry's to check."""
+    if workspace is not None:
+        return *_buffer(workspace, "workspace", x), workspace
+    import torch
+
+    size = need()
+    workspace = x.new_empty(size, dtype=torch.uint8)
+    return workspace.data_ptr(), size, workspace
+
+
 def _elsewhere(x, stream):
     """a context that makes the call's stream and device torch's current ones, or None where they already are."""
     import torch
@@ -692,12 +711,11 @@ def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, ga
     dw_pre, p2 = param_out(dw_pre, w_pre, "dw_pre")
     dgate, p3 = param_out(dgate, gate, "dgate")
     L = lib()
-    if workspace is None:
-        workspace = x.new_empty(L.ccdc_residual_norm_workspace_bytes(M, D), dtype=torch.uint8)
+    pws, ws_bytes, workspace = _scratch(workspace, lambda: L.ccdc_residual_norm_workspace_bytes(M, D), x)
     status = L.ccdc_residual_norm_backward(
         M, D, code, F32 if gt == torch.float32 else code, NORMS[kind], po, ldo, pz, ldz, x.data_ptr(), ldx,
         None if y is None else y.data_ptr(), ldy, ps, pw, pp, pg, per, alpha, p, seed, offset, pdx, lddx, pdy, lddy,
-        p1, p2, p3, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle(x))
+        p1, p2, p3, pws, ws_bytes, _handle(x))
     if status:
         _check(status, "ccdc_residual_norm_backward")
     return dx, dy, dw_post, dw_pre, dgate
@@ -743,14 +761,11 @@ def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved
         need = L.ccdc_ffn_saved_bytes(M, F, code)
         if saved is None:
             saved = x.new_empty(need, dtype=torch.uint8)
-        elif saved.numel() * saved.element_size() < need or saved.get_device() != x.get_device():
-            raise ValueError(f"saved: {need} bytes on {x.device} expected")
-        psaved = saved.data_ptr()
-    if workspace is None:
-        aligned = _ffn_aligned(x.element_size(), *zip(ptrs, (ldx, ldw, D, ldd, ldy)), (0, F))
-        workspace = x.new_empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 0, aligned), dtype=torch.uint8)
+        psaved = _buffer(saved, "saved", x, need)[0]
+    pws, ws_bytes, workspace = _scratch(workspace, lambda: L.ccdc_ffn_workspace_bytes(
+        M, D, F, code, 0, _ffn_aligned(x.element_size(), *zip(ptrs, (ldx, ldw, D, ldd, ldy)), (0, F))), x)
     status = L.ccdc_ffn_forward(M, D, F, code, ACTS[act], ptrs[0], ldx, ptrs[1], ptrs[2], ldw, ptrs[3], ldd, ptrs[4], ldy,
-                                psaved, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle(x))
+                                psaved, pws, ws_bytes, _handle(x))
     if status:
         _check(status, "ccdc_ffn_forward")
     return (out, saved) if save else out
@@ -772,8 +787,7 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
     if gt != x.dtype and gt != torch.float32:
         raise TypeError("grad_dtype is the tensors' dtype or float32")
     lddy = _rows(dy, "dy", x, x.shape)
-    if saved.numel() * saved.element_size() < L.ccdc_ffn_saved_bytes(M, F, code) or saved.get_device() != x.get_device():
-        raise ValueError("saved: what ffn_forward(save=True) returned expected")
+    psaved = _buffer(saved, "saved (of ffn_forward with save)", x, L.ccdc_ffn_saved_bytes(M, F, code))[0]
     if dx is None:
         dx, lddx = _empty_like(x), D
     else:
@@ -787,12 +801,11 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
             at.append(_vector(t, name, x, D * F, gt))
         grads.append(t)
     ptrs = dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dx.data_ptr()
-    if workspace is None:
-        aligned = _ffn_aligned(x.element_size(), *zip(ptrs, (lddy, ldx, ldw, D, ldd, lddx)), (0, F))
-        workspace = x.new_empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 1, aligned), dtype=torch.uint8)
+    pws, ws_bytes, workspace = _scratch(workspace, lambda: L.ccdc_ffn_workspace_bytes(
+        M, D, F, code, 1, _ffn_aligned(x.element_size(), *zip(ptrs, (lddy, ldx, ldw, D, ldd, lddx)), (0, F))), x)
     status = L.ccdc_ffn_backward(M, D, F, code, F32 if gt == torch.float32 else code, ACTS[act], ptrs[0], lddy, ptrs[1], ldx,
-                                 ptrs[2], ptrs[3], ldw, ptrs[4], ldd, saved.data_ptr(), ptrs[5], lddx, *at,
-                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _handle(x))
+                                 ptrs[2], ptrs[3], ldw, ptrs[4], ldd, psaved, ptrs[5], lddx, *at,
+                                 pws, ws_bytes, _handle(x))
     if status:
         _check(status, "ccdc_ffn_backward")
     return dx, *grads

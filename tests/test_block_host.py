@@ -123,6 +123,16 @@ def test_python_refusals_need_no_device():
         ccdc.ffn_forward(x, x, x, x.t().contiguous())
 
 
+def test_buffers_are_one_piece_of_the_tensors_device():
+    like = torch.zeros(4)
+    t = torch.empty(64, dtype=torch.int16)
+    assert ccdc._buffer(t, "workspace", like, 128) == (t.data_ptr(), 128)
+    assert ccdc._buffer(torch.empty(0), "workspace", like)[1] == 0
+    for bad in (t[::2], t.view(8, 8).t(), t[:1].expand(64), t[1:]):
+        with pytest.raises(ValueError, match="workspace"):
+            ccdc._buffer(bad, "workspace", like, 128 if bad.is_contiguous() else 0)
+
+
 def test_plans_refuse_the_block_types():
     for dtype in (ccdc.BF16, ccdc.F16):
         h = ctypes.c_void_p()

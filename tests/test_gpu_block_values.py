@@ -214,3 +214,30 @@ def test_gate_row_for_more_rows_than_there_are(ccdc, M, D):
         res.append((out, z, *ccdc.residual_norm_backward(dout, dz, x, y, st, dgate=into, **how)))
     for other in res[1:]:
         assert all(torch.equal(a, b) for a, b in zip(res[0], other))
+
+
+# ---------------------------------------------------------------- buffers a call cannot use
+def test_buffers_that_are_refused(ccdc):
+    """a workspace or saved values on the host, or a view with holes, are refused before anything is launched"""
+    rng = np.random.default_rng(1)
+    x, wg, wu, wd, dy = ffn_case(rng, 40, 64, 96, "bfloat16", 0, 0)
+    y, saved = ccdc.ffn_forward(x, wg, wu, wd, save=True)
+    n = 1 << 22
+    w = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    _, _, st = ccdc.residual_norm_forward(x, w_pre=w, save=True)
+    before = ccdc.num_kernel_launches()
+    for bad in (torch.empty(n, dtype=torch.uint8), torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2],
+                torch.empty(1, dtype=torch.uint8, device="cuda").expand(n)):
+        with pytest.raises(ValueError, match="workspace"):
+            ccdc.ffn_forward(x, wg, wu, wd, workspace=bad)
+        with pytest.raises(ValueError, match="workspace"):
+            ccdc.ffn_backward(dy, x, wg, wu, wd, saved, workspace=bad)
+        with pytest.raises(ValueError, match="workspace"):
+            ccdc.residual_norm_backward(None, dy, x, None, st, w_pre=w, workspace=bad)
+        with pytest.raises(ValueError, match="saved"):
+            ccdc.ffn_forward(x, wg, wu, wd, save=True, saved=bad)
+        with pytest.raises(ValueError, match="saved"):
+            ccdc.ffn_backward(dy, x, wg, wu, wd, bad)
+    assert ccdc.num_kernel_launches() == before
+    own = torch.empty(n, dtype=torch.uint8, device="cuda")
+    assert torch.equal(ccdc.ffn_forward(x, wg, wu, wd, workspace=own), y)
