@@ -34,7 +34,8 @@
 // 1056 cycles, 1024 at the tensor cores' rate; the gate's epilogue costs 16 %, its backward pass's 25 % of their launches.
 // 1024 rows, 1024 x 4096 in binary32, forward and backward: 0.58 ms.
 //
-// All waits are bounded: one that runs out sets g_wait_failed and the thread goes on without waiting.
+// All waits are bounded: one that runs out sets g_wait_failed, and its warp issues nothing more and waits for the block's
+// end, which comes once the other warps' waits have run out too and copies and products in flight had time to land.
 #include <cuda.h>
 
 #include <algorithm>
@@ -53,7 +54,9 @@ constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
 constexpr int SMALL_STEPS = 32;                         // steps of 64 k between drains of the small plane products
 constexpr int RING_SLOT = 2048, RING_SLOTS = 2;         // 32 rows of 64 bytes
 constexpr int SMEM_BYTES = FETCH_BYTES + EPI_WARPS * RING_SLOT * RING_SLOTS + 1024 + 256;
-constexpr int WAIT_LIMIT = 1 << 20;
+#ifndef CCDC_FFN_WAIT_LIMIT
+#define CCDC_FFN_WAIT_LIMIT (1 << 20)       // polls of a barrier (each may sleep) before a wait has failed
+#endif
 
 __device__ int g_wait_failed;
 
@@ -88,8 +91,8 @@ __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 template <int CG>
-__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, int &limit) {
-    for (int i = 0; i < limit; ++i) {
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < CCDC_FFN_WAIT_LIMIT; ++i) {
         uint32_t ok;
         if constexpr (CG == 2)
             asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
@@ -97,10 +100,10 @@ __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, int &lim
         else
             asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
                          "selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return;
+        if (ok) return true;
     }
     atomicExch(&g_wait_failed, 1);
-    limit = 4;
+    return false;
 }
 template <int CG>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
@@ -405,26 +408,26 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int limit = WAIT_LIMIT;
+    bool ok = true;             // no wait of this thread has run out
     if (warp == 0) {
         if (lane == 0) {
             const uint32_t ring = smem_u32(smem), first_full = CG == 2 ? in_first(full) : full;
             uint32_t stage = 0, phase = 0;
-            for (int item = cluster; item < w.items; item += clusters) {
+            for (int item = cluster; ok && item < w.items; item += clusters) {
                 const Tile t = tile_of(w, item);
                 const Problem &p = w.p[t.problem];
                 const int am = t.m * TILE_M + 128 * (int)rank;
                 // The tile's B: halves of HALF_N columns, each half's 128 CG rows shared out over the blocks.  GATE: the
                 // first half of the columns is h's, the second u's; with one half, its blocks (or boxes) are.
                 const bool a_across = p.a_across, b_across = p.b_across;
-                for (int it = t.it0; it < t.it1;) {
+                for (int it = t.it0; ok && it < t.it1;) {
                     const int term = it / p.kblocks, end = min(t.it1, (term + 1) * p.kblocks);
                     const CUtensorMap *ma = &p.a[term];
                     const CUtensorMap *mb = &p.b[EPI != MMA_GATE ? term : NB == 1 && CG == 2 ? (int)rank : 0];
                     const int bn = EPI != MMA_GATE ? t.n * TILE_N + HALF_N / CG * (int)rank
                                                    : t.n * (TILE_N / 2) + (NB == 2 ? 128 * (int)rank : 0);
                     for (int k = (it - term * p.kblocks) * BLOCK_K; it < end; ++it, k += BLOCK_K) {
-                        bar_wait<CG>(empty + 8 * stage, phase ^ 1, limit);
+                        if (ok = bar_wait<CG>(empty + 8 * stage, phase ^ 1); !ok) break;
                         const uint32_t bar = first_full + 8 * stage, dst = ring + stage * STAGE_BYTES;
                         if (rank == 0) bar_expect(full + 8 * stage, CG * STAGE_BYTES);
 #pragma unroll
@@ -466,27 +469,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, small_phase = 0;
-            for (int item = cluster; item < w.items; item += clusters) {
+            for (int item = cluster; ok && item < w.items; item += clusters) {
                 const Tile t = tile_of(w, item);
                 const Problem &p = w.p[t.problem];
                 const uint32_t idesc = p.idesc;
                 const uint64_t a0 = operand_desc(smem_u32(smem), p.a_across);
                 const uint64_t b0 = operand_desc(smem_u32(smem) + B_AT, p.b_across);
                 const uint32_t a_step = p.a_across ? 2048 >> 4 : 32 >> 4, b_step = p.b_across ? 2048 >> 4 : 32 >> 4;
-                for (int it = t.it0; it < t.it1;) {
+                for (int it = t.it0; ok && it < t.it1;) {
                     const int end = PLANES ? it + 1 : t.it1;
                     const uint32_t d = tmem + acc * TILE_N;
-                    bar_wait<CG>(acc_empty + 8 * acc, acc_phase ^ 1, limit);
+                    if (ok = bar_wait<CG>(acc_empty + 8 * acc, acc_phase ^ 1); !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     bool add = false;
                     for (; it < end; ++it) {
-                        bar_wait<CG>(full + 8 * stage, phase, limit);
+                        if (ok = bar_wait<CG>(full + 8 * stage, phase); !ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint64_t a = a0 + stage * (STAGE_BYTES >> 4), b = b0 + stage * (STAGE_BYTES >> 4);
                         if constexpr (PLANES) {
                             const bool first = (it - t.it0) % SMALL_STEPS == 0;
                             if (first) {
-                                bar_wait<CG>(small_empty, small_phase ^ 1, limit);
+                                if (ok = bar_wait<CG>(small_empty, small_phase ^ 1); !ok) break;
                                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                                 small_phase ^= 1;
                             }
@@ -511,6 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                         mma_commit<CG>(empty + 8 * stage);
                         if (++stage == STAGES) stage = 0, phase ^= 1;
                     }
+                    if (!ok) break;
                     mma_commit<CG>(acc_full + 8 * acc);
                     if (++acc == ACCS) acc = 0, acc_phase ^= 1;
                 }
@@ -533,7 +537,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
             }
         };
         constexpr int COLS = EPI == MMA_GATE ? TILE_N / 2 : TILE_N;     // output columns of a tile
-        for (int item = cluster; item < w.items; item += clusters) {
+        for (int item = cluster; ok && item < w.items; item += clusters) {
             const Tile t = tile_of(w, item);
             const Output p(w.p[t.problem]);
             const int row0 = t.m * TILE_M + 128 * (int)rank + 32 * quarter;
@@ -545,7 +549,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                 const uint32_t from = tmem + acc * TILE_N + part * (COLS / 2) + lanes;
                 float4 h[8], u[8];
                 if (EPI == MMA_GATE_BACK && rows && col0 < col1) load_saved(p, block, col0, lane, h, u);
-                bar_wait<CG>(acc_full + 8 * acc, acc_phase, limit);
+                if (ok = __all_sync(~0u, bar_wait<CG>(acc_full + 8 * acc, acc_phase)); !ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (int c = 0; rows && col0 + c < col1; c += 32) {
                     float f[32];
@@ -575,7 +579,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                 float f[2][32] = {};
                 const uint32_t columns = tmem + part * (COLS / 2) + lanes;
                 for (int it = t.it0; it < t.it1; ++it) {
-                    bar_wait<CG>(acc_full + 8 * acc, acc_phase, limit);
+                    if (ok = __all_sync(~0u, bar_wait<CG>(acc_full + 8 * acc, acc_phase)); !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     float v[2][32];
                     tmem_load(columns + acc * TILE_N, v[0]);
@@ -595,7 +599,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
 #pragma unroll
                         for (int i = 0; i < 32; ++i) f[j][i] = isfinite(f[j][i]) ? f[j][i] + v[j][i] : f[j][i];
                 }
-                if (rows && col0 < col1) {
+                if (ok && rows && col0 < col1) {
                     if constexpr (EPI == MMA_GATE) {
                         gate_columns<true>(p, f16, f[0], f[1], block, col0, row0, lane, ring);
                     } else {
@@ -619,7 +623,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
-    if (limit != WAIT_LIMIT) {          // a wait ran out: let copies that are still in flight land before the block ends
+    if (!ok) {          // let copies that are still in flight land before the block ends
         const long long until = clock64() + 2000000;
         while (clock64() < until) {}
     }

@@ -241,3 +241,48 @@ def test_buffers_that_are_refused(ccdc):
     assert ccdc.num_kernel_launches() == before
     own = torch.empty(n, dtype=torch.uint8, device="cuda")
     assert torch.equal(ccdc.ffn_forward(x, wg, wu, wd, workspace=own), y)
+# ---------------------------------------------------------------- waits that run out
+NO_WAITS = r"""
+import sys
+sys.path.insert(0, sys.argv[1])
+from pathlib import Path
+import torch
+from paper_1805_01993_b200 import build, ccdc
+ccdc._LIB_PATH = build.build_variant(Path(sys.argv[2]) / "libccdc_waits.so", ("CCDC_FFN_WAIT_LIMIT=0",))
+
+def block(M, dtype, D=136, F=200):
+    x, w = torch.ones((M, D), device="cuda", dtype=dtype), torch.ones((F, D), device="cuda", dtype=dtype)
+    y, saved = ccdc.ffn_forward(x, w, w, w.t().contiguous(), save=True)
+    ccdc.ffn_backward(x, x, w, w, w.t().contiguous(), saved)
+    torch.cuda.synchronize()
+    return y
+
+block(4, torch.float32)
+ccdc.block_status()                     # no wait so far
+for M, D, F in ((40, 136, 200), (700, 512, 1024), (2304, 1024, 4096)):
+    for dtype in (torch.bfloat16, torch.float32):
+        block(M, dtype, D, F)
+        try:
+            ccdc.block_status()
+        except ccdc.CcdcError as e:
+            assert e.status == ccdc.ESTATE
+        else:
+            raise AssertionError("a wait ran out and the status is good")
+# the context is as good as before
+assert bool((block(4, torch.float32)[0] == block(4, torch.float32)[3]).all())
+x = torch.ones((40, 64), device="cuda")
+assert torch.equal(ccdc.residual_norm_forward(x, x)[0], x + x)
+print("bounded waits ok")
+"""
+
+
+def test_waits_that_run_out_are_reported(tmp_path):
+    """The feed-forward kernels built with waits that run out at their first poll: every warp stops before it issues a copy
+    or a product, the call ends, the status says so, and the process goes on."""
+    import subprocess
+    import sys
+
+    from paper_1805_01993_b200.build import ROOT
+
+    r = subprocess.run([sys.executable, "-c", NO_WAITS, str(ROOT), str(tmp_path)], capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0 and "bounded waits ok" in r.stdout, r.stdout + r.stderr
