@@ -159,7 +159,19 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, float (&f)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for this thread's loads.  Their registers go through it: otherwise the compiler could move plain arithmetic on them
+// ahead of the wait, which it does not know to write them.
+__device__ __forceinline__ void arrived(float (&f)[32]) {
+    asm volatile("" : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]),
+                   "+f"(f[8]), "+f"(f[9]), "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15]),
+                   "+f"(f[16]), "+f"(f[17]), "+f"(f[18]), "+f"(f[19]), "+f"(f[20]), "+f"(f[21]), "+f"(f[22]), "+f"(f[23]),
+                   "+f"(f[24]), "+f"(f[25]), "+f"(f[26]), "+f"(f[27]), "+f"(f[28]), "+f"(f[29]), "+f"(f[30]), "+f"(f[31]));
+}
+template <class... F>
+__device__ __forceinline__ void tmem_wait(F &...f) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    (arrived(f), ...);
+}
 
 // Shared-memory descriptor of a 128-byte-swizzled operand.  Along k: rows of 128 bytes, eight to a 1 KiB group
 // (stride 1 KiB between groups).  Across k: a row of 128 bytes is 64 indices at one k; eight k to a 1 KiB group, and
@@ -555,15 +567,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                     float f[32];
                     tmem_load(from + c, f);
                     if constexpr (EPI == MMA_STORE) {
-                        tmem_wait();
+                        tmem_wait(f);
                         store_columns(p, f16, f, col0 + c, row0, t.split, lane, ring);
                     } else if constexpr (EPI == MMA_GATE) {
                         float g[32];
                         tmem_load(from + COLS + c, g);
-                        tmem_wait();
+                        tmem_wait(f, g);
                         gate_columns<false>(p, f16, f, g, block, col0 + c, row0, lane, ring);
                     } else {
-                        tmem_wait();
+                        tmem_wait(f);
                         float g[32];
                         gate_back_columns<false>(p, f, g, h, u);
                         if (col0 + c + 32 < col1) load_saved(p, block, col0 + c + 32, lane, h, u);     // on their way during the stores
@@ -584,7 +596,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                     float v[2][32];
                     tmem_load(columns + acc * TILE_N, v[0]);
                     tmem_load(columns + acc * TILE_N + SECOND, v[1]);
-                    tmem_wait();
+                    tmem_wait(v[0], v[1]);
                     release(acc_empty + 8 * acc);
                     if (++acc == ACCS) acc = 0, acc_phase ^= 1;
 #pragma unroll
@@ -592,7 +604,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_ffn_mma(const __grid_constant__ 
                     if ((it - t.it0) % SMALL_STEPS != SMALL_STEPS - 1 && it + 1 < t.it1) continue;
                     tmem_load(columns + SMALL_AT, v[0]);
                     tmem_load(columns + SMALL_AT + SECOND, v[1]);
-                    tmem_wait();
+                    tmem_wait(v[0], v[1]);
                     release(small_empty);
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
