@@ -542,17 +542,6 @@ def _buffer(t, name, like, need=0):
     return t.data_ptr(), size
 
 
-def _scratch(workspace, need, x):
-    """(address, bytes, tensor) of the caller's workspace, or of a new one of need() bytes.  Its size is the C entry's to check."""
-    if workspace is not None:
-        return *_buffer(workspace, "workspace", x), workspace
-    import torch
-
-    size = need()
-    workspace = x.new_empty(size, dtype=torch.uint8)
-    return workspace.data_ptr(), size, workspace
-
-
 def _elsewhere(x, stream):
     """a context that makes the call's stream and device torch's current ones, or None where they already are."""
     import torch
@@ -711,7 +700,12 @@ def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, ga
     dw_pre, p2 = param_out(dw_pre, w_pre, "dw_pre")
     dgate, p3 = param_out(dgate, gate, "dgate")
     L = lib()
-    pws, ws_bytes, workspace = _scratch(workspace, lambda: L.ccdc_residual_norm_workspace_bytes(M, D), x)
+    if workspace is None:
+        ws_bytes = L.ccdc_residual_norm_workspace_bytes(M, D)
+        workspace = x.new_empty(ws_bytes, dtype=torch.uint8)
+        pws = workspace.data_ptr()
+    else:
+        pws, ws_bytes = _buffer(workspace, "workspace", x)
     status = L.ccdc_residual_norm_backward(
         M, D, code, F32 if gt == torch.float32 else code, NORMS[kind], po, ldo, pz, ldz, x.data_ptr(), ldx,
         None if y is None else y.data_ptr(), ldy, ps, pw, pp, pg, per, alpha, p, seed, offset, pdx, lddx, pdy, lddy,
@@ -762,8 +756,13 @@ def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved
         if saved is None:
             saved = x.new_empty(need, dtype=torch.uint8)
         psaved = _buffer(saved, "saved", x, need)[0]
-    pws, ws_bytes, workspace = _scratch(workspace, lambda: L.ccdc_ffn_workspace_bytes(
-        M, D, F, code, 0, _ffn_aligned(x.element_size(), *zip(ptrs, (ldx, ldw, D, ldd, ldy)), (0, F))), x)
+    if workspace is None:
+        aligned = _ffn_aligned(x.element_size(), *zip(ptrs, (ldx, ldw, D, ldd, ldy)), (0, F))
+        ws_bytes = L.ccdc_ffn_workspace_bytes(M, D, F, code, 0, aligned)
+        workspace = x.new_empty(ws_bytes, dtype=torch.uint8)
+        pws = workspace.data_ptr()
+    else:
+        pws, ws_bytes = _buffer(workspace, "workspace", x)
     status = L.ccdc_ffn_forward(M, D, F, code, ACTS[act], ptrs[0], ldx, ptrs[1], ptrs[2], ldw, ptrs[3], ldd, ptrs[4], ldy,
                                 psaved, pws, ws_bytes, _handle(x))
     if status:
@@ -801,8 +800,13 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
             at.append(_vector(t, name, x, D * F, gt))
         grads.append(t)
     ptrs = dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), dx.data_ptr()
-    pws, ws_bytes, workspace = _scratch(workspace, lambda: L.ccdc_ffn_workspace_bytes(
-        M, D, F, code, 1, _ffn_aligned(x.element_size(), *zip(ptrs, (lddy, ldx, ldw, D, ldd, lddx)), (0, F))), x)
+    if workspace is None:
+        aligned = _ffn_aligned(x.element_size(), *zip(ptrs, (lddy, ldx, ldw, D, ldd, lddx)), (0, F))
+        ws_bytes = L.ccdc_ffn_workspace_bytes(M, D, F, code, 1, aligned)
+        workspace = x.new_empty(ws_bytes, dtype=torch.uint8)
+        pws = workspace.data_ptr()
+    else:
+        pws, ws_bytes = _buffer(workspace, "workspace", x)
     status = L.ccdc_ffn_backward(M, D, F, code, F32 if gt == torch.float32 else code, ACTS[act], ptrs[0], lddy, ptrs[1], ldx,
                                  ptrs[2], ptrs[3], ldw, ptrs[4], ldd, psaved, ptrs[5], lddx, *at,
                                  pws, ws_bytes, _handle(x))

@@ -216,6 +216,56 @@ def test_gate_row_for_more_rows_than_there_are(ccdc, M, D):
         assert all(torch.equal(a, b) for a, b in zip(res[0], other))
 
 
+# ---------------------------------------------------------------- outputs that are left out
+@pytest.mark.parametrize("M,D,F,dtype", [(5, 64, 96, "bfloat16"), (300, 136, 200, "bfloat16"), (300, 136, 201, "float16"),
+                                         (20, 64, 96, "float32"), (130, 72, 100, "float32")])
+def test_ffn_outputs_left_out(ccdc, M, D, F, dtype):
+    """every output may be NULL, and leaving some out changes no other output's bits"""
+    rng = np.random.default_rng(M)
+    x, wg, wu, wd, dy = ffn_case(rng, M, D, F, dtype, 0, 0)
+    code, L = ccdc._block_dtype(x), ccdc.lib()
+    _, saved = ccdc.ffn_forward(x, wg, wu, wd, save=True)
+    want = ccdc.ffn_backward(dy, x, wg, wu, wd, saved)
+    ws = torch.empty(L.ccdc_ffn_workspace_bytes(M, D, F, code, 1, 0), dtype=torch.uint8, device="cuda")
+    for mask in range(16):
+        out = [torch.full_like(w, 3.0) if mask >> i & 1 else None for i, w in enumerate(want)]
+        ptr = [None if t is None else t.data_ptr() for t in out]
+        status = L.ccdc_ffn_backward(M, D, F, code, code, 0, dy.data_ptr(), D, x.data_ptr(), D, wg.data_ptr(), wu.data_ptr(), D,
+                                     wd.data_ptr(), F, saved.data_ptr(), ptr[0], D, *ptr[1:], ws.data_ptr(), ws.numel(), 0)
+        assert status == ccdc.OK
+        assert all(t is None or torch.equal(t, w) for t, w in zip(out, want)), mask
+    ccdc.block_status()
+
+
+@pytest.mark.parametrize("M,D", [(9, 64), (300, 51), (2, 8200)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_residual_norm_outputs_left_out(ccdc, M, D, dtype):
+    rng = np.random.default_rng(M)
+    per = 4
+    x, y, w_post, w_pre, g = norm_case(rng, M, D, dtype, True, per)
+    dout, dz = tensor(rng, M, D, dtype), tensor(rng, M, D, dtype)
+    how = dict(w_post=w_post, w_pre=w_pre, gate=g, rows_per_gate=per, p=0.25, seed=3)
+    out, z, st = ccdc.residual_norm_forward(x, y, save=True, **how)
+    want = ccdc.residual_norm_backward(dout, dz, x, y, st, **how)
+    code, L = ccdc._block_dtype(x), ccdc.lib()
+    ws = torch.empty(L.ccdc_residual_norm_workspace_bytes(M, D), dtype=torch.uint8, device="cuda")
+    for mask in range(32):
+        res = [torch.full_like(w, 3.0) if mask >> i & 1 else None for i, w in enumerate(want)]
+        ptr = [None if t is None else t.data_ptr() for t in res]
+        status = L.ccdc_residual_norm_backward(
+            M, D, code, code, 0, dout.data_ptr(), D, dz.data_ptr(), D, x.data_ptr(), D, y.data_ptr(), D, st.data_ptr(),
+            w_post.data_ptr(), w_pre.data_ptr(), g.data_ptr(), per, 1.0, 0.25, 3, 0, ptr[0], D, ptr[1], D, *ptr[2:],
+            ws.data_ptr(), ws.numel(), 0)
+        assert status == ccdc.OK
+        assert all(t is None or torch.equal(t, w) for t, w in zip(res, want)), mask
+    # z alone
+    alone = torch.full_like(z, 3.0)
+    status = L.ccdc_residual_norm_forward(M, D, code, 0, 1e-5, x.data_ptr(), D, y.data_ptr(), D, w_post.data_ptr(),
+                                          w_pre.data_ptr(), g.data_ptr(), per, 1.0, 0.25, 3, 0, None, D, alone.data_ptr(), D,
+                                          None, 0)
+    assert status == ccdc.OK and torch.equal(alone, z)
+
+
 # ---------------------------------------------------------------- buffers a call cannot use
 def test_buffers_that_are_refused(ccdc):
     """a workspace or saved values on the host, or a view with holes, are refused before anything is launched"""
@@ -241,6 +291,35 @@ def test_buffers_that_are_refused(ccdc):
     assert ccdc.num_kernel_launches() == before
     own = torch.empty(n, dtype=torch.uint8, device="cuda")
     assert torch.equal(ccdc.ffn_forward(x, wg, wu, wd, workspace=own), y)
+# ---------------------------------------------------------------- feed-forward: what the backward pass keeps
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("M", [8, 40, 136])
+def test_inner_gradients_are_rounded_once(ccdc, dtype, M):
+    """h and u are kept in binary32: dh = da u act'(h) and du = da act(h) are off by their own rounding alone.
+
+    x is two unit matrices side by side, so h and u are sums of two weights (more bits than the type has), and the
+    weights' gradients are dh and du themselves.  Beside the rounding: the product da, within (D + 8) 2^-23 of its terms'
+    size, and the elementwise work, 2^-17 of it."""
+    rng = np.random.default_rng(M)
+    F, D = 96, 2 * M
+    eye = torch.eye(M, device="cuda", dtype=DT[dtype])
+    x = torch.cat([eye, eye], 1)
+    wg, wu = (tensor(rng, F, D, dtype, 1.0) for _ in range(2))
+    wd, dy = tensor(rng, D, F, dtype, D ** -0.5), tensor(rng, M, D, dtype)
+    _, saved = ccdc.ffn_forward(x, wg, wu, wd, save=True)
+    _, dwg, dwu, _ = ccdc.ffn_backward(dy, x, wg, wu, wd, saved, grad_dtype=torch.float32)
+    h, u = f64(x) @ f64(wg).T, f64(x) @ f64(wu).T
+    f, df, _ = ref.act("silu", h)
+    da = f64(dy) @ f64(wd)
+    size = np.abs(f64(dy)) @ np.abs(f64(wd))
+    for got, want, terms in ((dwg, da * u * df, size * np.abs(u)), (dwu, da * f, size * np.abs(f))):
+        # rounding to the type: half a unit in the last place of the binade
+        half = ref.U[dtype] * 2.0 ** np.floor(np.log2(np.maximum(np.abs(want), 1e-30)))
+        slack = 1.2 * terms * ((D + 8) * 2.0 ** -23 + 2.0 ** -17)
+        for at in (got[:, :M], got[:, M:]):
+            within(at, want.T, (half * (1 + 2.0 ** -8) + slack + ref.SMALLEST[dtype]).T, "inner gradient")
+
+
 # ---------------------------------------------------------------- waits that run out
 NO_WAITS = r"""
 import sys
