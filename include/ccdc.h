@@ -544,9 +544,12 @@ int ccdc_residual_norm_backward(long long M, long long D, int dtype, int grad_dt
  *     da = dy w_down,  dh = da * u * act'(h),  du = da * act(h),
  *     dx = dh w_gate + du w_up,  dw_gate = dh^T x,  dw_up = du^T x,  dw_down = dy^T a;
  * dx [M][D], dw_gate and dw_up [F][D], dw_down [D][F] contiguous, each may be NULL.
- * a, dh and du, which enter further products, are kept in the tensors' type; h
- * and u in binary32 (rounding them too would take the gradients' error from 1.4
- * to 1.8 times that of their own rounding).  Infinities and NaN follow IEEE
+ * a, dh and du, which enter further products, are kept in the tensors' type: in
+ * CCDC_F16 a overflows beyond 65504, and dh and du lose bits below 2^-14.  h and u
+ * are kept in binary32 (rounding them too would take the gradients' error from 1.4
+ * to 1.8 times that of their own rounding).  16-bit products are summed with the
+ * tensor cores' truncation, about 2^-28 of the terms' size for each of the K; so
+ * far around zero the slope of CCDC_ACT_RELU may fall on either side.  Infinities and NaN follow IEEE
  * arithmetic in every type and for any number of rows, but for one thing: with
  * more than 32 rows of binary32, an infinity times a value below 2^-126 may be NaN.
  * workspace: ccdc_ffn_workspace_bytes(..., backward, aligned), 16-byte aligned;

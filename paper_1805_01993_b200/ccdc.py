@@ -651,7 +651,7 @@ def residual_norm_backward(dout, dz, x, y, stats, *, w_post=None, w_pre=None, ga
                            p=0.0, seed=0, offset=0, kind="rms", eps=None, grad_dtype=None, dx=None, dy=None,
                            dw_post=None, dw_pre=None, dgate=None, workspace=None, stream=None):
     """``ccdc_residual_norm_backward``: (dx, dy, dw_post, dw_pre, dgate), None for what the forward call lacked.
-    ``dout`` or ``dz`` may be None (zero).  ``eps`` is accepted for symmetry; the forward's is in ``stats``."""
+    ``dz`` comes with ``w_pre``, and only then; ``dout`` may be None (zero) beside it.  ``eps`` is accepted for symmetry; the forward's is in ``stats``."""
     import torch
 
     ctx = _elsewhere(x, stream)
@@ -773,7 +773,8 @@ def ffn_forward(x, w_gate, w_up, w_down, act="silu", save=False, out=None, saved
 def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None, dx=None, dw_gate=None, dw_up=None,
                  dw_down=None, workspace=None, stream=None):
     """``ccdc_ffn_backward``: (dx, dw_gate, dw_up, dw_down).  Gradients may be passed in (contiguous, e.g. slices of
-    a partition row); ``grad_dtype`` float32 keeps the sums' 32 bits."""
+    a partition row); with ``grad_dtype`` float32 the sums are not rounded to the tensors' type, as their factors a, dh
+    and du are."""
     import torch
 
     ctx = _elsewhere(x, stream)

@@ -30,7 +30,7 @@
 // fits.
 //
 // Measured: 2048 rows, 4096 x 8192, bf16: forward 0.33 ms, 1.26 PFLOP/s; 8192 rows, 4096 x 16384 forward and backward
-// 7.99 ms, 1.24 PFLOP/s (256 x 256 tiles alone: 10.1 ms).  Between epilogues a step of 64 k on the large tile takes about
+// 8.0 ms, 1.24 PFLOP/s (256 x 256 tiles alone: 10.1 ms).  Between epilogues a step of 64 k on the large tile takes about
 // 1056 cycles, 1024 at the tensor cores' rate; the gate's epilogue costs 16 %, its backward pass's 25 % of their launches.
 // 1024 rows, 1024 x 4096 in binary32, forward and backward: 0.58 ms.
 //

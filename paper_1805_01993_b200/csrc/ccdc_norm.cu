@@ -19,7 +19,7 @@
 
 namespace {
 
-constexpr long long MAX_D = 32768;      // columns of a row that fit a block's registers
+constexpr long long MAX_D = 32768;      // the most columns of a row: 32 for each thread of the largest block
 
 struct NormArgs {
     long long M, D;
@@ -48,8 +48,12 @@ __host__ __device__ __forceinline__ long long share(long long M, int blocks, int
 
 // ------------------------------------------------------------------ rows by blocks
 // The form for any alignment and up to MAX_D columns: a block owns a row and loads it straight into registers, all of it
-// before the first barrier.  Measured at 16384 x 1001, binary32: forward 57 us, 4.6 TB/s; backward 127 us, 3.1 TB/s (it was
-// 321 us with the loads spread between the barriers).  16-bit rows go by 2-byte accesses: 0.8 to 1.4 TB/s.
+// before the first barrier.  Measured with gate and dropout at 16384 x 1001, binary32: forward 64 us, 4.1 TB/s; backward
+// 134 us, 2.9 TB/s (the loads spread between the barriers: 2.5 times that).  16-bit rows that vectors cannot address go by
+// 2-byte accesses: at 1001 and 4095 columns forward 2.0 TB/s, backward 1.0 to 1.1.
+// A thread's columns fit its registers up to 4096 (forward 8192); the backward pass spills 0.3 to 0.5 KB a thread up to 8192
+// and 3.6 to 4.5 KB beyond (forward 0.3 to 2 KB), at 16384 columns some 35 GB through L1 and L2 for 0.8 GB of tensors:
+// 4096 x 16384 bf16 forward 0.35 ms, backward 3.6 ms (0.23 TB/s), binary32 0.45 and 4.3 ms.
 
 // sums of two values over the block; one barrier, buffers used in turn
 template <int THREADS>
@@ -357,8 +361,9 @@ __global__ void __launch_bounds__(THREADS) k_residual_norm_back(const NormArgs a
 // row's sums are formed.
 // Rows asked for ahead: two; three take the L1 share that w_pre and the factors are read through (16384 x 4096 bf16,
 // backward: 224 us with two, 249 with three).
-// Measured at 16384 x 4096, bf16, rms, with dropout: forward 108 us, 5.0 TB/s; backward 217 us, 3.7 TB/s.  What bounds them
-// is instructions as much as bytes: 34 and 61 an element, of which the generator takes about 6.
+// Measured at 16384 x 4096, bf16, rms, with dropout: forward 108 us, 5.0 TB/s; backward 217 us, 3.7 TB/s.  Neither issue
+// slots (52 to 55 % used; 34 and 61 instructions an element, of which the generator takes about 6) nor DRAM (42 to 45 %)
+// are at their limit: 16 warps an SM at 112 to 128 registers do not hide the latency of a row's two meetings.
 constexpr int STAGES = 2;
 
 template <int W>
