@@ -555,7 +555,8 @@ int ccdc_residual_norm_backward(long long M, long long D, int dtype, int grad_dt
  * workspace: ccdc_ffn_workspace_bytes(..., backward, aligned), 16-byte aligned;
  * aligned != 0 promises that every pointer and row stride is a multiple of 16
  * bytes (D and F too), which needs less.  workspace_bytes smaller than the call
- * needs gives CCDC_ESIZE.  saved must be 16-byte aligned. */
+ * needs gives CCDC_ESIZE, as do M > 2^21 and D or F > 2^20.  saved must be
+ * 16-byte aligned. */
 typedef enum { CCDC_ACT_SILU = 0, CCDC_ACT_GELU = 1, CCDC_ACT_GELU_TANH = 2, CCDC_ACT_RELU = 3 } ccdc_act_t;
 size_t ccdc_ffn_saved_bytes(long long M, long long F, int dtype);
 size_t ccdc_ffn_workspace_bytes(long long M, long long D, long long F, int dtype, int backward, int aligned);
