@@ -574,6 +574,98 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
  * Synchronous; copies one word back. */
 int ccdc_block_status(void);
 
+/* ------------------------------------------- experts, distillation, 8 bits
+ * What a distillation job of an expert block needs next to the block operators:
+ * tokens sorted by expert and back, the loss from a teacher's top logits, and
+ * the 8-bit products of a teacher that is not trained.  The conventions of the
+ * block operators hold (row strides, types, sums in binary32 or more, one
+ * rounding, one order, no atomics, no allocation, capturable); these calls need
+ * no workspace.
+ *
+ * Tokens sorted by expert.  ids [M][k] contiguous (id_bytes 4 or 8: signed
+ * integers): slot s = m*k + j goes to expert ids[m][j]; a slot whose expert is
+ * not in [0, experts) is dropped.  Sort: offsets[experts + 1], offsets[e] =
+ * slots of experts below e; places[M][k] = the slot's position in the stable
+ * order by expert, -1 where dropped; slots[M*k] = the slot at each position, -1
+ * behind offsets[experts].  CCDC_ESIZE beyond 2^31 - 1 slots or 4096 experts.
+ *
+ * Dispatch: xs[places[m][j]] = x[m]; the rows of xs [M*k][D] behind
+ * offsets[experts] are set to zero.  Its backward pass is combine without
+ * weights.
+ *
+ * Combine: y[m] = sum_j weights[m][j] * ys[places[m][j]], j ascending; dropped
+ * slots are left out, whatever the rows hold, and a token without slots gets 0.
+ * weights [M][k] contiguous in dtype or CCDC_F32 (weight_dtype), or NULL: 1.
+ * Backward: dys[places[m][j]] = weights[m][j] * dy[m], the rows behind
+ * offsets[experts] zero; dweights[m][j] = <dy[m], ys[places[m][j]]> in
+ * weight_dtype, 0 where dropped.  dys or dweights may be NULL (ys too without
+ * dweights).
+ * slots and places are those of one ccdc_expert_sort of the same M and k;
+ * places outside [0, M*k) count as dropped.  D <= 2^20 (CCDC_ESIZE). */
+int ccdc_expert_sort(long long M, int k, int experts, int id_bytes, const void *ids, int *offsets, int *slots, int *places,
+                     void *stream);
+int ccdc_expert_dispatch(long long M, int k, long long D, int dtype, const void *x, long long ldx, const int *slots,
+                         const int *places, void *xs, long long ldxs, void *stream);
+int ccdc_expert_combine(long long M, int k, long long D, int dtype, const void *ys, long long ldys, const int *places,
+                        const void *weights, int weight_dtype, void *y, long long ldy, void *stream);
+int ccdc_expert_combine_backward(long long M, int k, long long D, int dtype, const void *dy, long long lddy, const void *ys,
+                                 long long ldys, const int *slots, const int *places, const void *weights, int weight_dtype,
+                                 void *dys, long long lddys, void *dweights, void *stream);
+
+/* Distillation from a teacher's top logits.  Row m has the student's logits
+ * z[V] (row stride ldz) and k slots (ids[m][j], values[m][j]), contiguous, ids
+ * of id_bytes 4 or 8, values in dtype or CCDC_F32 (value_dtype).  A slot counts
+ * where its id is in [0, V) and its value is not -infinity.  With T = temperature:
+ *     t_j  = softmax over the row's slots of values / T      (teacher_lse NULL)
+ *            exp(values_j / T - teacher_lse[m])              (the log of the
+ *            whole teacher's sum of exponentials at T: its mass outside the
+ *            slots is left out)
+ *     loss = sum_j t_j * (log t_j - log s[ids_j]),   s = softmax(z / T)
+ *     dz   = dloss[m] / T * (P * s - t),   P = sum_j t_j
+ * Slots of one id add up.  A row without slots, or with P = 0, has loss 0 and
+ * gradient 0, whatever its logits.  Logits of -infinity or of the type's lowest
+ * value have s = 0 (loss +infinity where t > 0).
+ *   loss alone             dlogits NULL; stats NULL, or [M][2] binary32 (8-byte
+ *                          aligned) for the gradient later
+ *   gradient from stats    loss NULL, dloss [M] binary32, dlogits (row stride
+ *                          lddz), the stats of the same inputs
+ *   both in one pass       loss, dloss and dlogits; stats may be NULL
+ * dlogits may be the logits themselves (same stride).  1e-6 <= T <= 1e6;
+ * k <= 1024, V < 2^31 (CCDC_ESIZE). */
+int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits, long long ldz, int id_bytes, const void *ids,
+                 int value_dtype, const void *values, const float *teacher_lse, float temperature, const float *dloss, float *loss,
+                 void *stats, void *dlogits, long long lddz, void *stream);
+
+/* 8-bit products with a scale for each block of 128.  A tensor is e4m3 values
+ * (sign, 4 bits of exponent with bias 7, 3 of mantissa; largest 448) and a
+ * binary32 scale for each 128 elements of a row (block_rows 1) or each 128 x 128
+ * (block_rows 128); the last blocks may be smaller.  8-bit rows start at
+ * multiples of 16 bytes (pointer and strides).
+ *
+ * Quantisation of `groups` matrices x [M][K] (x_group elements apart; 1 with
+ * block_rows 1): scale = the least 2^e, e >= -126, with 448 * 2^e >= the block's
+ * largest magnitude; q = x / scale (exact) rounded to nearest, ties to even.  A
+ * block that holds an infinity or a NaN becomes NaN throughout.  scales:
+ * element (group, row block, column block) at their three strides.
+ *
+ * Product: y[m][n] = sum_b xs[m][b] * ws[n / 128][b] * sum_{k in b} x[m][k] w[n][k].
+ * x [M][K] with scales at x_scales[m*x_scale_row + b*x_scale_col]; w [experts][N][K]
+ * (w_expert bytes apart, row stride ldw) with scales [experts][ceil(N/128)][ceil(K/128)]
+ * contiguous; any binary32 scales whose products are finite.  y [M][N] in y_dtype.
+ * offsets NULL: one weight.  Else [experts + 1] on the device: rows offsets[e]
+ * up to offsets[e + 1] take weight e (offsets[0] is taken as 0, entries beyond
+ * M as M); rows behind the last are set to zero.
+ * The 128 products of a block are summed by the tensor cores, blocks in
+ * binary32 in ascending order.  The gradient with respect to x is the same call
+ * with the transposed weight, whose blocks are the transposed blocks.
+ * CCDC_ESIZE: M > 2^30, N > 2^22, K > 2^23, experts > 1024, groups > 65535. */
+int ccdc_quantize_fp8(long long groups, long long M, long long K, int block_rows, int dtype, const void *x, long long x_group,
+                      long long ldx, void *q, long long q_group, long long ldq, float *scales, long long scale_group,
+                      long long scale_row, long long scale_col, void *stream);
+int ccdc_matmul_fp8(long long M, long long N, long long K, int experts, const void *x, long long ldx, const float *x_scales,
+                    long long x_scale_row, long long x_scale_col, const void *w, long long w_expert, long long ldw,
+                    const float *w_scales, const int *offsets, void *y, int y_dtype, long long ldy, void *stream);
+
 /* ------------------------------------------------------------- diagnostics */
 const char *ccdc_strerror(int status);
 int ccdc_last_cuda_error(void);          /* cudaError_t of the last CCDC_ECUDA on this thread */

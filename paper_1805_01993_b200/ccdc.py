@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 from pathlib import Path
+from typing import NamedTuple
 
 _LIB_PATH = Path(__file__).resolve().parent / "libccdc.so"
 _lib = None
@@ -103,6 +104,13 @@ SIGNATURES = {
     "ccdc_ffn_backward": (_I, [_LL, _LL, _LL, _I, _I, _I, _P, _LL, _P, _LL, _P, _P, _LL, _P, _LL, _P, _P, _LL, _P, _P,
                                _P, _P, _SZ, _P]),
     "ccdc_block_status": (_I, []),
+    "ccdc_expert_sort": (_I, [_LL, _I, _I, _I, _P, _P, _P, _P, _P]),
+    "ccdc_expert_dispatch": (_I, [_LL, _I, _LL, _I, _P, _LL, _P, _P, _P, _LL, _P]),
+    "ccdc_expert_combine": (_I, [_LL, _I, _LL, _I, _P, _LL, _P, _P, _I, _P, _LL, _P]),
+    "ccdc_expert_combine_backward": (_I, [_LL, _I, _LL, _I, _P, _LL, _P, _LL, _P, _P, _P, _I, _P, _LL, _P, _P]),
+    "ccdc_distill": (_I, [_LL, _LL, _I, _I, _P, _LL, _I, _P, _I, _P, _P, _FL, _P, _P, _P, _P, _LL, _P]),
+    "ccdc_quantize_fp8": (_I, [_LL, _LL, _LL, _I, _I, _P, _LL, _LL, _P, _LL, _LL, _P, _LL, _LL, _LL, _P]),
+    "ccdc_matmul_fp8": (_I, [_LL, _LL, _LL, _I, _P, _LL, _P, _LL, _LL, _P, _LL, _LL, _P, _P, _P, _I, _LL, _P]),
     "ccdc_strerror": (ctypes.c_char_p, [_I]),
     "ccdc_last_cuda_error": (_I, []),
     "ccdc_num_kernel_launches": (_I, []),
@@ -814,6 +822,329 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
     if status:
         _check(status, "ccdc_ffn_backward")
     return dx, *grads
+
+
+# ---- experts, distillation, 8 bits ----------------------------------------
+# The same conventions; ids, places and offsets are integers on the tensors' device.
+
+
+class ExpertOrder(NamedTuple):
+    """What ``expert_sort`` returns: ``offsets`` [experts + 1], ``slots`` [M*k] and ``places`` [M][k], all int32."""
+    offsets: object
+    slots: object
+    places: object
+
+
+def _ids(t, name, like=None):
+    """bytes of an id; raises unless t is [rows][k] contiguous int32 or int64 (on like's device)."""
+    size = t.element_size()
+    if t.dim() != 2 or not t.is_contiguous() or t.shape[1] < 1 or t.is_floating_point() or t.is_complex() or not (
+            size == 4 or size == 8) or not t.dtype.is_signed:
+        raise ValueError(f"{name}: contiguous int32 or int64 [rows][k] expected")
+    if not t.is_cuda if like is None else t.get_device() != like.get_device():
+        raise ValueError(f"{name}: a tensor on {'a CUDA device' if like is None else like.device} expected")
+    return size
+
+
+def _order(order, like, rows=None):
+    """(slots, places, M, k, addresses) of an order for tensors on like's device."""
+    import torch
+
+    slots, places = order.slots, order.places
+    M, k = places.shape
+    ps, pp = _vector(slots, "order.slots", like, M * k, torch.int32), _vector(places, "order.places", like, M * k, torch.int32)
+    if rows is not None and rows != M:
+        raise ValueError(f"the order is of {M} tokens, the tensor has {rows} rows")
+    return M, k, ps, pp
+
+
+def expert_sort(ids, n_experts, offsets=None, slots=None, places=None, stream=None):
+    """``ccdc_expert_sort``: the stable order of the slots of ``ids`` [M][k] by expert, an ``ExpertOrder``.
+    Slots whose expert is not in [0, n_experts) are dropped."""
+    import torch
+
+    ctx = _elsewhere(ids, stream)
+    if ctx is not None:
+        with ctx:
+            return expert_sort(ids, n_experts, offsets, slots, places)
+    size = _ids(ids, "ids")
+    M, k = ids.shape
+    i32 = torch.int32
+    offsets = ids.new_empty(n_experts + 1, dtype=i32) if offsets is None else offsets
+    slots = ids.new_empty(M * k, dtype=i32) if slots is None else slots
+    places = ids.new_empty((M, k), dtype=i32) if places is None else places
+    status = lib().ccdc_expert_sort(M, k, n_experts, size, ids.data_ptr(), _vector(offsets, "offsets", ids, n_experts + 1, i32),
+                                    _vector(slots, "slots", ids, M * k, i32), _vector(places, "places", ids, M * k, i32),
+                                    _handle(ids))
+    if status:
+        _check(status, "ccdc_expert_sort")
+    return ExpertOrder(offsets, slots, places)
+
+
+def expert_dispatch(x, order, out=None, stream=None):
+    """``ccdc_expert_dispatch``: the rows of x [M][D] sorted by expert, [M*k][D]; rows behind the last expert's are zero."""
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return expert_dispatch(x, order, out)
+    ldx, code = _rows(x, "x"), _block_dtype(x)
+    M, k, ps, pp = _order(order, x, x.shape[0])
+    D = x.shape[1]
+    if out is None:
+        out, ldo = x.new_empty((M * k, D)), D
+    else:
+        ldo = _rows(out, "out", x, (M * k, D))
+    status = lib().ccdc_expert_dispatch(M, k, D, code, x.data_ptr(), ldx, ps, pp, out.data_ptr(), ldo, _handle(x))
+    if status:
+        _check(status, "ccdc_expert_dispatch")
+    return out
+
+
+def _weights(weights, like, M, k):
+    import torch
+
+    dtype = weights.dtype
+    if dtype is not torch.float32 and dtype is not like.dtype:
+        raise TypeError(f"weights: float32 or {like.dtype} expected, got {dtype}")
+    if weights.shape != (M, k):
+        raise ValueError(f"weights: shape {(M, k)} expected, got {tuple(weights.shape)}")
+    return _vector(weights, "weights", like, M * k, dtype), F32 if dtype is torch.float32 else _block_dtype(like)
+
+
+def expert_combine(ys, order, weights=None, out=None, stream=None):
+    """``ccdc_expert_combine``: y[m] = sum_j weights[m][j] * (the row of ys [M*k][D] that slot (m, j) has in the order);
+    without ``weights`` their plain sum.  Dropped slots are left out."""
+    ctx = _elsewhere(ys, stream)
+    if ctx is not None:
+        with ctx:
+            return expert_combine(ys, order, weights, out)
+    ldys, code = _rows(ys, "ys"), _block_dtype(ys)
+    M, k, _, pp = _order(order, ys)
+    D = ys.shape[1]
+    if ys.shape[0] != M * k:
+        raise ValueError(f"ys: {M * k} rows expected, got {ys.shape[0]}")
+    pw, wt = (None, code) if weights is None else _weights(weights, ys, M, k)
+    if out is None:
+        out, ldo = ys.new_empty((M, D)), D
+    else:
+        ldo = _rows(out, "out", ys, (M, D))
+    status = lib().ccdc_expert_combine(M, k, D, code, ys.data_ptr(), ldys, pp, pw, wt, out.data_ptr(), ldo, _handle(ys))
+    if status:
+        _check(status, "ccdc_expert_combine")
+    return out
+
+
+def expert_combine_backward(dy, ys, order, weights, dys=None, dweights=None, stream=None):
+    """``ccdc_expert_combine_backward``: (dys, dweights) of ``expert_combine(ys, order, weights)``.  Without ``weights``
+    dweights is None and ``ys`` is not read."""
+    ctx = _elsewhere(dy, stream)
+    if ctx is not None:
+        with ctx:
+            return expert_combine_backward(dy, ys, order, weights, dys, dweights)
+    lddy, code = _rows(dy, "dy"), _block_dtype(dy)
+    M, k, ps, pp = _order(order, dy, dy.shape[0])
+    D = dy.shape[1]
+    pys, ldys, pw, wt, pdw = None, D, None, code, None
+    if weights is not None:
+        pw, wt = _weights(weights, dy, M, k)
+        pys, ldys = ys.data_ptr(), _rows(ys, "ys", dy, (M * k, D))
+        if dweights is None:
+            dweights = weights.new_empty((M, k))
+        pdw = _vector(dweights, "dweights", dy, M * k, weights.dtype)
+    elif dweights is not None:
+        raise ValueError("dweights needs weights")
+    if dys is None:
+        dys, lddys = dy.new_empty((M * k, D)), D
+    else:
+        lddys = _rows(dys, "dys", dy, (M * k, D))
+    status = lib().ccdc_expert_combine_backward(M, k, D, code, dy.data_ptr(), lddy, pys, ldys, ps, pp, pw, wt, dys.data_ptr(),
+                                                lddys, pdw, _handle(dy))
+    if status:
+        _check(status, "ccdc_expert_combine_backward")
+    return dys, dweights
+
+
+def expert_dispatch_backward(dxs, order, out=None, stream=None):
+    """Gradient of ``expert_dispatch``: the sum of a token's rows, ``expert_combine`` without weights."""
+    return expert_combine(dxs, order, None, out, stream)
+
+
+def _distill(logits, ids, values, temperature, teacher_lse, dloss, loss, stats, dlogits):
+    import torch
+
+    ldz, code = _rows(logits, "logits"), _block_dtype(logits)
+    M, V = logits.shape
+    size = _ids(ids, "ids", logits)
+    k = ids.shape[1]
+    f32 = torch.float32
+    if ids.shape[0] != M or values.shape != ids.shape:
+        raise ValueError(f"ids and values: [{M}][k] expected, got {tuple(ids.shape)} and {tuple(values.shape)}")
+    if values.dtype is not f32 and values.dtype is not logits.dtype:
+        raise TypeError(f"values: float32 or {logits.dtype} expected, got {values.dtype}")
+    pv = _vector(values, "values", logits, M * k, values.dtype)
+    pt = None if teacher_lse is None else _vector(teacher_lse, "teacher_lse", logits, M, f32)
+    pd = None if dloss is None else _vector(dloss, "dloss", logits, M, f32)
+    pl = None if loss is None else _vector(loss, "loss", logits, M, f32)
+    ps = None if stats is None else _vector(stats, "stats (of distill_forward with save)", logits, 2 * M, f32)
+    pz, lddz = (None, V) if dlogits is None else (dlogits.data_ptr(), _rows(dlogits, "dlogits", logits, logits.shape))
+    status = lib().ccdc_distill(M, V, k, code, logits.data_ptr(), ldz, size, ids.data_ptr(),
+                                F32 if values.dtype is f32 else code, pv, pt, temperature, pd, pl, ps, pz, lddz, _handle(logits))
+    if status:
+        _check(status, "ccdc_distill")
+
+
+def distill_forward(logits, ids, values, *, temperature=1.0, teacher_lse=None, save=False, loss=None, stream=None):
+    """``ccdc_distill``: the loss [M] (float32) of each row of logits [M][V] against the teacher's top logits (``ids``,
+    ``values``: [M][k]; slots with ids outside [0, V) are not there).  The teacher's probabilities are the softmax over its
+    slots, or exp(values / T - teacher_lse) where the whole teacher's logsumexp at T is given.  Returns loss, or
+    (loss, stats) with ``save``; ``stats`` is opaque and goes to ``distill_backward``."""
+    import torch
+
+    ctx = _elsewhere(logits, stream)
+    if ctx is not None:
+        with ctx:
+            return distill_forward(logits, ids, values, temperature=temperature, teacher_lse=teacher_lse, save=save, loss=loss)
+    M = logits.shape[0]
+    loss = logits.new_empty(M, dtype=torch.float32) if loss is None else loss
+    stats = logits.new_empty(2 * M, dtype=torch.float32) if save else None
+    _distill(logits, ids, values, temperature, teacher_lse, None, loss, stats, None)
+    return (loss, stats) if save else loss
+
+
+def distill_backward(dloss, logits, ids, values, stats, *, temperature=1.0, teacher_lse=None, dlogits=None, stream=None):
+    """``ccdc_distill``: the gradient of the logits from ``dloss`` [M] (float32) and the forward call's inputs and
+    ``stats``.  ``dlogits`` may be ``logits``."""
+    ctx = _elsewhere(logits, stream)
+    if ctx is not None:
+        with ctx:
+            return distill_backward(dloss, logits, ids, values, stats, temperature=temperature, teacher_lse=teacher_lse,
+                                    dlogits=dlogits)
+    dlogits = _empty_like(logits) if dlogits is None else dlogits
+    _distill(logits, ids, values, temperature, teacher_lse, dloss, None, stats, dlogits)
+    return dlogits
+
+
+def distill(dloss, logits, ids, values, *, temperature=1.0, teacher_lse=None, loss=None, dlogits=None, stream=None):
+    """``ccdc_distill``: (loss, dlogits) in one pass over the logits, where the loss's gradient ``dloss`` [M] (float32;
+    a mean over rows: 1/M) is known beforehand.  ``dlogits`` may be ``logits``."""
+    import torch
+
+    ctx = _elsewhere(logits, stream)
+    if ctx is not None:
+        with ctx:
+            return distill(dloss, logits, ids, values, temperature=temperature, teacher_lse=teacher_lse, loss=loss,
+                           dlogits=dlogits)
+    loss = logits.new_empty(logits.shape[0], dtype=torch.float32) if loss is None else loss
+    dlogits = _empty_like(logits) if dlogits is None else dlogits
+    _distill(logits, ids, values, temperature, teacher_lse, dloss, loss, None, dlogits)
+    return loss, dlogits
+
+
+FP8_BLOCK = 128
+
+
+def _bytes_rows(t, name, like=None):
+    """row stride of an e4m3 matrix whose rows start at multiples of 16 bytes"""
+    import torch
+
+    if t.dtype is not torch.float8_e4m3fn or t.dim() not in (2, 3) or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{name}: float8_e4m3fn with contiguous columns expected")
+    if not t.is_cuda if like is None else t.get_device() != like.get_device():
+        raise ValueError(f"{name}: a tensor on {'a CUDA device' if like is None else like.device} expected")
+    ld = t.stride(-2) if t.shape[-2] > 1 else -(-t.shape[-1] // 16) * 16
+    if t.data_ptr() % 16 or ld % 16:
+        raise ValueError(f"{name}: rows must start at multiples of 16 bytes")
+    return ld
+
+
+def quantize_fp8(x, block_rows=1, out=None, scales=None, stream=None):
+    """``ccdc_quantize_fp8``: (q, scales), x as e4m3 values with a float32 scale for each 128 elements of a row
+    (``block_rows`` 1: scales [M][K/128], stored by column) or each 128 x 128 (``block_rows`` 128: [M/128][K/128]; x may then be
+    a stack of matrices).  q's rows are padded to multiples of 16 bytes."""
+    import torch
+
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return quantize_fp8(x, block_rows, out, scales)
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError("block_rows is 1 or 128")
+    if x.dim() == 3 and block_rows == FP8_BLOCK:
+        first = x[0] if x.shape[0] else x.new_empty(x.shape[1:])
+        groups, group, ldx = x.shape[0], x.stride(0), _rows(first, "x")
+    else:
+        groups, group, ldx = 1, 0, _rows(x, "x")
+    code = _block_dtype(x)
+    M, K = x.shape[-2:]
+    kb = -(-K // FP8_BLOCK)
+    if out is None:
+        ldq = -(-K // 16) * 16
+        out = x.new_empty((*x.shape[:-1], ldq), dtype=torch.float8_e4m3fn)
+        if ldq != K:
+            out = out[..., :K]
+    else:
+        if out.shape != x.shape:
+            raise ValueError(f"out: shape {tuple(x.shape)} expected, got {tuple(out.shape)}")
+        ldq = _bytes_rows(out, "out", x)
+    if block_rows == 1:
+        shape = M, kb
+        if scales is None:
+            scales = x.new_empty((kb, M), dtype=torch.float32).t()
+    else:
+        shape = *x.shape[:-2], -(-M // FP8_BLOCK), kb
+        if scales is None:
+            scales = x.new_empty(shape, dtype=torch.float32)
+    if scales.shape != shape or scales.dtype is not torch.float32 or scales.get_device() != x.get_device():
+        raise ValueError(f"scales: float32 {shape} on {x.device} expected")
+    strides = scales.stride() if scales.dim() == 3 else (0, *scales.stride())
+    status = lib().ccdc_quantize_fp8(groups, M, K, block_rows, code, x.data_ptr(), group, ldx, out.data_ptr(),
+                                     out.stride(0) if x.dim() == 3 else 0, ldq, scales.data_ptr(), *strides, _handle(x))
+    if status:
+        _check(status, "ccdc_quantize_fp8")
+    return out, scales
+
+
+def matmul_fp8(x, x_scales, w, w_scales, *, offsets=None, out_dtype=None, out=None, stream=None):
+    """``ccdc_matmul_fp8``: y = (x * x_scales) (w * w_scales)^T for e4m3 x [M][K] and w [N][K] with the scales of
+    ``quantize_fp8`` (x by rows, w by blocks).  With ``offsets`` [E + 1] (int32, as of ``expert_sort``) w is [E][N][K] and
+    the rows of x from offsets[e] on take weight e; rows behind the last are zero.  Type of y: bfloat16 unless given."""
+    import torch
+
+    ctx = _elsewhere(x, stream)
+    if ctx is not None:
+        with ctx:
+            return matmul_fp8(x, x_scales, w, w_scales, offsets=offsets, out_dtype=out_dtype, out=out)
+    ldx, ldw = _bytes_rows(x, "x"), _bytes_rows(w, "w", x)
+    f32, experts = torch.float32, 1
+    if x.dim() != 2 or w.dim() != (2 if offsets is None else 3) or w.shape[-1] != x.shape[1]:
+        raise ValueError(f"x [M][K] and w [N][K] (with offsets [E][N][K]) expected, got {tuple(x.shape)} and {tuple(w.shape)}")
+    M, K = x.shape
+    N, kb = w.shape[-2], -(-K // FP8_BLOCK)
+    po, expert = None, 0
+    if offsets is not None:
+        experts, expert = w.shape[0], w.stride(0)
+        po = _vector(offsets, "offsets", x, experts + 1, torch.int32)
+        if experts > 1 and expert % 16:
+            raise ValueError("w: matrices must start at multiples of 16 bytes")
+    if x_scales.shape != (M, kb) or x_scales.dtype is not f32 or x_scales.get_device() != x.get_device():
+        raise ValueError(f"x_scales: float32 {(M, kb)} on {x.device} expected")
+    shape = (*w.shape[:-2], -(-N // FP8_BLOCK), kb)
+    if w_scales.shape != shape:
+        raise ValueError(f"w_scales: shape {shape} expected, got {tuple(w_scales.shape)}")
+    pws = _vector(w_scales, "w_scales", x, w_scales.numel(), f32)
+    if out is None:
+        out, ldo = x.new_empty((M, N), dtype=torch.bfloat16 if out_dtype is None else out_dtype), N
+    else:
+        if out_dtype is not None and out.dtype is not out_dtype:
+            raise TypeError(f"out: {out_dtype} expected, got {out.dtype}")
+        ldo = _rows(out, "out")
+        if out.shape != (M, N) or out.get_device() != x.get_device():
+            raise ValueError(f"out: {(M, N)} on {x.device} expected")
+    status = lib().ccdc_matmul_fp8(M, N, K, experts, x.data_ptr(), ldx, x_scales.data_ptr(), *x_scales.stride(), w.data_ptr(),
+                                   expert, ldw, pws, po, out.data_ptr(), _block_dtype(out), ldo, _handle(x))
+    if status:
+        _check(status, "ccdc_matmul_fp8")
+    return out
 
 
 def block_status():

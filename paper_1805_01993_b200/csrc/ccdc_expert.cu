@@ -1,0 +1,402 @@
+// Tokens sorted by expert and back, with weights applied, and the gradients.
+//
+// Slot s = m k + j is token m's j-th expert.  The sort is a stable counting sort: offsets[e] = slots of experts before e, the
+// place of a slot = offsets[e] + slots of the same expert before it.  Everything has one order and there are no atomics, so
+// replicas of a file agree bit by bit.  A slot whose expert lies outside [0, E) is dropped: place -1.
+#include "ccdc_block.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr int MAX_EXPERTS = 4096;
+constexpr int SORT_CLUSTER = 8;             // blocks of a sort of many slots
+constexpr int SORT_ONE_BLOCK = 4096;        // slots that one block sorts alone
+
+struct SortArgs {
+    long long slots;
+    int experts;
+    const void *ids;
+    int *offsets, *slot_at, *place_of;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// a word of another block's shared memory
+__device__ __forceinline__ int remote(const int *p, uint32_t rank) {
+    uint32_t at;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// One launch of one block, or of one cluster of blocks.  Each warp owns a run of consecutive slots and counts its experts in
+// shared memory (lanes with the same expert find one another by a match and the first adds for all); the counts become
+// starting positions by prefix sums over warps, over the cluster's blocks (read from one another's shared memory) and over
+// experts; the same walk again then places every slot.
+template <class I>
+__global__ void __launch_bounds__(1024) k_expert_sort(SortArgs a) {
+    extern __shared__ int smem[];
+    const int E = a.experts, warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int *count = smem, *total = count + warps * E, *base = total + E, *sums = base + E;     // [warps][E], [E], [E], [33]
+    const int blocks = gridDim.x, rank = blocks > 1 ? (int)cluster_rank() : 0;
+    for (int i = threadIdx.x; i < warps * E; i += blockDim.x) count[i] = 0;
+    __syncthreads();
+    const long long run = ((a.slots + (long long)blocks * warps - 1) / ((long long)blocks * warps) + 31) / 32 * 32;
+    const long long from = min(a.slots, run * ((long long)rank * warps + warp)), to = min(a.slots, from + run);
+    const I *ids = static_cast<const I *>(a.ids);
+    int *mine = count + warp * E;
+    const auto expert_of = [&](long long s) {
+        if (s >= to) return -1;
+        const I e = ids[s];
+        return e >= 0 && e < (I)E ? (int)e : -1;
+    };
+    for (long long s = from; s < to; s += 32) {
+        const int e = expert_of(s + lane);
+        const uint32_t same = __match_any_sync(~0u, e);
+        if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        int sum = 0;
+        for (int w = 0; w < warps; ++w) {
+            const int c = count[w * E + e];
+            count[w * E + e] = sum;
+            sum += c;
+        }
+        total[e] = sum;
+    }
+    if (blocks > 1)
+        cluster_sync();
+    else
+        __syncthreads();
+    // base[e]: slots of experts before e, and of e in the cluster's earlier blocks
+    int carry = 0;
+    for (int first = 0; first < E; first += blockDim.x) {
+        const int e = first + threadIdx.x;
+        int all = 0, before = 0;
+        if (e < E)
+            for (int b = 0; b < blocks; ++b) {
+                const int v = blocks > 1 ? remote(total + e, b) : total[e];
+                before += b < rank ? v : 0;
+                all += v;
+            }
+        int scan = all;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int v = __shfl_up_sync(~0u, scan, d);
+            if (lane >= d) scan += v;
+        }
+        if (lane == 31) sums[warp] = scan;
+        __syncthreads();
+        if (warp == 0) {
+            int v = lane < warps ? sums[lane] : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int u = __shfl_up_sync(~0u, v, d);
+                if (lane >= d) v += u;
+            }
+            sums[lane] = v;
+        }
+        __syncthreads();
+        const int start = carry + (warp ? sums[warp - 1] : 0) + scan - all;
+        if (e < E) {
+            base[e] = start + before;
+            if (rank == 0) a.offsets[e] = start;
+        }
+        carry += sums[31];
+        __syncthreads();
+    }
+    if (rank == 0 && threadIdx.x == 0) a.offsets[E] = carry;
+    for (int i = threadIdx.x; i < warps * E; i += blockDim.x) count[i] += base[i % E];
+    __syncthreads();
+    for (long long s = from; s < to; s += 32) {
+        const int e = expert_of(s + lane);
+        const uint32_t same = __match_any_sync(~0u, e);
+        int place = -1;
+        if (e >= 0) {
+            place = mine[e] + __popc(same & ((1u << lane) - 1));
+            a.slot_at[place] = (int)(s + lane);
+        }
+        __syncwarp();
+        if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+        __syncwarp();
+        if (s + lane < to) a.place_of[s + lane] = place;
+    }
+    // positions behind the last expert's hold nothing
+    for (long long i = carry + (long long)rank * blockDim.x + threadIdx.x; i < a.slots; i += (long long)blocks * blockDim.x)
+        a.slot_at[i] = -1;
+    if (blocks > 1) cluster_sync();         // no block leaves while another reads its totals
+}
+
+// ------------------------------------------------------------- rows there and back
+template <class T, int N>
+struct alignas(sizeof(T) * N) Pack {
+    T v[N];
+};
+struct RowArgs {
+    long long M, rows;          // tokens, slots
+    int k, D, weights_f32;
+    const void *x;              // what is read by token (dispatch: x; backward of combine: dy)
+    const void *ys;             // what is read by place
+    void *out;                  // xs, y or dys
+    long long ldx, ldys, ldo;
+    const int *slots, *places;
+    const void *weights;
+    void *dweights;
+};
+template <class T>
+__device__ __forceinline__ float weight_of(const RowArgs &a, long long slot) {
+    if (!a.weights) return 1.0f;
+    return a.weights_f32 ? static_cast<const float *>(a.weights)[slot] : to_f32<T>(static_cast<const T *>(a.weights)[slot]);
+}
+
+// xs[place] = x[m] for the token's places, and zeros in as many of the rows behind the last expert's.  A token's row is read
+// once.  blockDim.x threads to a row, blockDim.y tokens to a block, ITEMS accesses of N elements to a thread.
+template <class T, int N, int ITEMS>
+__global__ void __launch_bounds__(256) k_expert_dispatch(RowArgs a) {
+    const long long m = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    if (m >= a.M) return;
+    using P = Pack<T, N>;
+    const int c0 = (blockIdx.y * ITEMS * blockDim.x + threadIdx.x) * N, step = blockDim.x * N;
+    const T *x = static_cast<const T *>(a.x) + m * a.ldx;
+    P v[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+        if (c0 + i * step < a.D) v[i] = *reinterpret_cast<const P *>(x + c0 + i * step);
+    for (int j = 0; j < a.k; ++j) {
+        const long long s = m * a.k + j;
+        const int place = a.places[s];
+        if (place >= 0 && place < a.rows) {
+            T *out = static_cast<T *>(a.out) + place * a.ldo;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (c0 + i * step < a.D) *reinterpret_cast<P *>(out + c0 + i * step) = v[i];
+        }
+        if (a.slots[s] < 0) {
+            T *out = static_cast<T *>(a.out) + s * a.ldo;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (c0 + i * step < a.D) *reinterpret_cast<P *>(out + c0 + i * step) = P{};
+        }
+    }
+}
+
+// y[m] = sum over j of w[m][j] ys[place], j ascending, dropped slots left out; 0 for a token without slots.
+template <class T, int N, int ITEMS>
+__global__ void __launch_bounds__(256) k_expert_combine(RowArgs a) {
+    const long long m = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    if (m >= a.M) return;
+    using P = Pack<T, N>;
+    const int c0 = (blockIdx.y * ITEMS * blockDim.x + threadIdx.x) * N, step = blockDim.x * N;
+    constexpr int AHEAD = ITEMS * N >= 8 ? 4 : 8;       // rows whose loads are in flight together
+    float sum[ITEMS * N] = {};
+    for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
+        P v[AHEAD][ITEMS];
+        float w[AHEAD];
+        bool there[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const long long s = m * a.k + j0 + u;
+            const int place = j0 + u < a.k ? a.places[s] : -1;
+            there[u] = place >= 0 && place < a.rows;
+            w[u] = there[u] ? weight_of<T>(a, s) : 0.0f;
+            const T *ys = static_cast<const T *>(a.ys) + place * a.ldys;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (there[u] && c0 + i * step < a.D) v[u][i] = *reinterpret_cast<const P *>(ys + c0 + i * step);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (there[u])
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) sum[i * N + n] = fmaf(w[u], to_f32<T>(v[u][i].v[n]), sum[i * N + n]);
+    }
+    T *out = static_cast<T *>(a.out) + m * a.ldo;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+        if (c0 + i * step < a.D) {
+            P r;
+#pragma unroll
+            for (int n = 0; n < N; ++n) r.v[n] = from_f32<T>(sum[i * N + n]);
+            *reinterpret_cast<P *>(out + c0 + i * step) = r;
+        }
+}
+
+// dys[place] = w dy[m] and dw = <dy[m], ys[place]>: a warp to a slot, so that the product is summed within the warp.  The k
+// warps of a token read its dy at about the same time, from L1 or L2.
+template <class T, int N, int ITEMS>
+__global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a) {
+    const long long s = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5;
+    const int lane = threadIdx.x & 31;
+    if (s >= a.rows) return;
+    using P = Pack<T, N>;
+    const long long m = s / a.k;
+    if (a.out && a.slots[s] < 0) {
+        T *out = static_cast<T *>(a.out) + s * a.ldo;
+        for (int c = lane * N; c < a.D; c += 32 * N) *reinterpret_cast<P *>(out + c) = P{};
+    }
+    const int place = a.places[s];
+    const bool there = place >= 0 && place < a.rows;
+    float dot = 0.0f;
+    if (there) {
+        const float w = weight_of<T>(a, s);
+        const T *dy = static_cast<const T *>(a.x) + m * a.ldx, *ys = static_cast<const T *>(a.ys) + place * a.ldys;
+        T *out = static_cast<T *>(a.out) + place * a.ldo;
+        for (int c0 = lane * N; c0 < a.D; c0 += 32 * N * ITEMS) {
+            P g[ITEMS], v[ITEMS];
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int c = c0 + 32 * N * i;
+                if (c < a.D) {
+                    g[i] = *reinterpret_cast<const P *>(dy + c);
+                    if (a.dweights) v[i] = *reinterpret_cast<const P *>(ys + c);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int c = c0 + 32 * N * i;
+                if (c >= a.D) continue;
+                P r;
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const float d = to_f32<T>(g[i].v[n]);
+                    if (a.dweights) dot = fmaf(d, to_f32<T>(v[i].v[n]), dot);
+                    r.v[n] = from_f32<T>(w * d);
+                }
+                if (a.out) *reinterpret_cast<P *>(out + c) = r;
+            }
+        }
+    }
+    if (!a.dweights) return;
+#pragma unroll
+    for (int d = 16; d; d /= 2) dot += __shfl_xor_sync(~0u, dot, d);
+    if (lane == 0) {
+        if (a.weights_f32)
+            static_cast<float *>(a.dweights)[s] = dot;
+        else
+            static_cast<T *>(a.dweights)[s] = from_f32<T>(dot);
+    }
+}
+
+enum Which { DISPATCH, COMBINE, COMBINE_BACK };
+
+template <class T, int N, int ITEMS>
+int launch_rows(Which which, const RowArgs &a, cudaStream_t s) {
+    if (which == COMBINE_BACK) {
+        k_expert_combine_back<T, N, ITEMS><<<(unsigned)((a.rows + 7) / 8), 256, 0, s>>>(a);
+        return block_launch_status();
+    }
+    const int packs = (a.D + N - 1) / N;
+    int x = 8;
+    while (x < 256 && x * ITEMS < packs) x *= 2;
+    const dim3 block(x, 256 / x), grid((unsigned)((a.M + block.y - 1) / block.y), (unsigned)((packs + x * ITEMS - 1) / (x * ITEMS)));
+    if (which == DISPATCH)
+        k_expert_dispatch<T, N, ITEMS><<<grid, block, 0, s>>>(a);
+    else
+        k_expert_combine<T, N, ITEMS><<<grid, block, 0, s>>>(a);
+    return block_launch_status();
+}
+template <class T>
+int launch_type(Which which, const RowArgs &a, bool vec, cudaStream_t s) {
+    constexpr int N = 16 / sizeof(T);
+    return vec ? launch_rows<T, N, 1>(which, a, s) : launch_rows<T, 1, 4>(which, a, s);
+}
+int launch(Which which, RowArgs &a, int dtype, cudaStream_t s) {
+    const int b = type_bytes(dtype);
+    const auto rows16 = [&](const void *p, long long ld) { return aligned_to(p, 16) && (!p || ld * b % 16 == 0); };
+    const bool vec = a.D * b % 16 == 0 && rows16(a.x, a.ldx) && rows16(a.ys, a.ldys) && rows16(a.out, a.ldo);
+    return dtype == CCDC_F32    ? launch_type<float>(which, a, vec, s)
+           : dtype == CCDC_BF16 ? launch_type<bf16>(which, a, vec, s) : launch_type<fp16>(which, a, vec, s);
+}
+int check(long long M, int k, long long D, int dtype, int weight_dtype) {
+    if (M < 0 || k < 1 || D < 1 || !is_float_type(dtype) || (weight_dtype != dtype && weight_dtype != CCDC_F32))
+        return CCDC_EINVAL;
+    return M > 0x7FFFFFFF / k || D > (1 << 20) ? CCDC_ESIZE : CCDC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ccdc_expert_sort(long long M, int k, int experts, int id_bytes, const void *ids, int *offsets, int *slots, int *places,
+                     void *stream) {
+    if (M < 0 || k < 1 || experts < 1 || (id_bytes != 4 && id_bytes != 8) || !offsets || !aligned_to(ids, id_bytes) ||
+        !aligned_to(offsets, 4) || !aligned_to(slots, 4) || !aligned_to(places, 4))
+        return CCDC_EINVAL;
+    if (M > 0 && (!ids || !slots || !places)) return CCDC_EINVAL;
+    if (M > 0x7FFFFFFF / k || experts > MAX_EXPERTS) return CCDC_ESIZE;
+    SortArgs a = {M * k, experts, ids, offsets, slots, places};
+    const int warps = experts <= 1024 ? 32 : 8;             // the counts of all warps fit the shared memory
+    const int smem = (warps * experts + 2 * experts + 33) * (int)sizeof(int);
+    static std::atomic<unsigned long long> done[2];
+    constexpr int MOST = (32 * 1024 + 2 * MAX_EXPERTS + 33) * (int)sizeof(int);
+    const void *kernel = id_bytes == 4 ? (const void *)k_expert_sort<int> : (const void *)k_expert_sort<long long>;
+    const int rc = block_allow_smem(kernel, MOST, &done[id_bytes / 8]);
+    if (rc != CCDC_OK) return rc;
+    const int blocks = a.slots <= SORT_ONE_BLOCK ? 1 : SORT_CLUSTER;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks), cfg.blockDim = dim3(32 * warps), cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = blocks, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = 1;
+    const cudaError_t e = id_bytes == 4 ? cudaLaunchKernelEx(&cfg, k_expert_sort<int>, a)
+                                        : cudaLaunchKernelEx(&cfg, k_expert_sort<long long>, a);
+    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    return block_launch_status();
+}
+
+int ccdc_expert_dispatch(long long M, int k, long long D, int dtype, const void *x, long long ldx, const int *slots,
+                         const int *places, void *xs, long long ldxs, void *stream) {
+    const int rc = check(M, k, D, dtype, dtype);
+    if (rc != CCDC_OK) return rc;
+    if (M == 0) return CCDC_OK;
+    if (!x || !slots || !places || !xs || ldx < D || ldxs < D) return CCDC_EINVAL;
+    RowArgs a = {};
+    a.M = M, a.rows = M * k, a.k = k, a.D = (int)D, a.x = x, a.ldx = ldx, a.slots = slots, a.places = places;
+    a.out = xs, a.ldo = ldxs;
+    return launch(DISPATCH, a, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int ccdc_expert_combine(long long M, int k, long long D, int dtype, const void *ys, long long ldys, const int *places,
+                        const void *weights, int weight_dtype, void *y, long long ldy, void *stream) {
+    const int rc = check(M, k, D, dtype, weights ? weight_dtype : dtype);
+    if (rc != CCDC_OK) return rc;
+    if (M == 0) return CCDC_OK;
+    if (!ys || !places || !y || ldys < D || ldy < D) return CCDC_EINVAL;
+    RowArgs a = {};
+    a.M = M, a.rows = M * k, a.k = k, a.D = (int)D, a.ys = ys, a.ldys = ldys, a.places = places, a.weights = weights;
+    a.weights_f32 = weight_dtype == CCDC_F32, a.out = y, a.ldo = ldy;
+    return launch(COMBINE, a, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int ccdc_expert_combine_backward(long long M, int k, long long D, int dtype, const void *dy, long long lddy, const void *ys,
+                                 long long ldys, const int *slots, const int *places, const void *weights, int weight_dtype,
+                                 void *dys, long long lddys, void *dweights, void *stream) {
+    const int rc = check(M, k, D, dtype, weight_dtype);
+    if (rc != CCDC_OK) return rc;
+    if (M == 0) return CCDC_OK;
+    if (!dy || !slots || !places || lddy < D || (!dys && !dweights) || (dys && lddys < D) ||
+        (dweights && (!ys || ldys < D)))
+        return CCDC_EINVAL;
+    RowArgs a = {};
+    a.M = M, a.rows = M * k, a.k = k, a.D = (int)D, a.x = dy, a.ldx = lddy, a.ys = ys, a.ldys = ldys, a.slots = slots;
+    a.places = places, a.weights = weights, a.weights_f32 = weight_dtype == CCDC_F32, a.out = dys, a.ldo = lddys;
+    a.dweights = dweights;
+    return launch(COMBINE_BACK, a, dtype, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
