@@ -568,7 +568,7 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
                       const void *w_down, long long ldd, const void *saved, void *dx, long long lddx, void *dw_gate,
                       void *dw_up, void *dw_down, void *workspace, size_t workspace_bytes, void *stream);
 
-/* The feed-forward kernels wait for copies and products through bounded polls.
+/* The feed-forward and 8-bit kernels wait for copies and products through bounded polls.
  * After the stream was synchronised: CCDC_OK, or CCDC_ESTATE if a wait of any
  * call on the current device ever ran out (outputs since then are not valid).
  * Synchronous; copies one word back. */
@@ -658,7 +658,9 @@ int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits,
  * The 128 products of a block are summed by the tensor cores, blocks in
  * binary32 in ascending order.  The gradient with respect to x is the same call
  * with the transposed weight, whose blocks are the transposed blocks.
- * CCDC_ESIZE: M > 2^30, N > 2^22, K > 2^23, experts > 1024, groups > 65535. */
+ * CCDC_ESIZE: M > 2^30, N > 2^22, K > 2^23, experts > 1024, groups > 65535, or
+ * more than 2^31 - 1 tiles of 16 rows by 128 columns.  Waits inside the product
+ * are bounded as those of the feed-forward block (ccdc_block_status). */
 int ccdc_quantize_fp8(long long groups, long long M, long long K, int block_rows, int dtype, const void *x, long long x_group,
                       long long ldx, void *q, long long q_group, long long ldq, float *scales, long long scale_group,
                       long long scale_row, long long scale_col, void *stream);

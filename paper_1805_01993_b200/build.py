@@ -12,7 +12,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libccdc.so"
 SOURCES = ["ccdc_plan.cpp", "ccdc_kernels.cu", "ccdc_map.cu", "ccdc_map_cluster.cu", "ccdc_multi.cu", "ccdc_stream.cu",
            "ccdc_norm.cu", "ccdc_ffn.cu", "ccdc_ffn_mma.cu", "ccdc_ffn_rows.cu", "ccdc_ffn_few.cu", "ccdc_expert.cu",
-           "ccdc_distill.cu", "ccdc_fp8.cu"]
+           "ccdc_distill.cu", "ccdc_fp8.cu", "ccdc_fp8_mma.cu"]
 
 
 def nvcc_command(out: Path, verbose: bool = False, defines: tuple[str, ...] = ()) -> list[str]:

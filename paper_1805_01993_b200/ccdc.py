@@ -1148,7 +1148,7 @@ def matmul_fp8(x, x_scales, w, w_scales, *, offsets=None, out_dtype=None, out=No
 
 
 def block_status():
-    """after a synchronise: raises if a bounded wait inside a feed-forward kernel ever ran out on this device."""
+    """after a synchronise: raises if a bounded wait inside a feed-forward or 8-bit kernel ever ran out on this device."""
     _check(lib().ccdc_block_status(), "ccdc_block_status")
 
 

@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "ccdc_ffn.h"
+#include "ccdc_fp8.h"
 #include "ccdc_ffn_mma.h"
 #include "ccdc_ffn_rows.h"
 
@@ -449,7 +450,8 @@ int ccdc_ffn_backward(long long M, long long D, long long F, int dtype, int grad
 
 int ccdc_block_status(void) {
     int failed = 0;
-    const int rc = mma_status(&failed);
+    int rc = mma_status(&failed);
+    if (rc == CCDC_OK && !failed) rc = fp8_mma_status(&failed);
     return rc != CCDC_OK ? rc : failed ? CCDC_ESTATE : CCDC_OK;
 }
 

@@ -5,6 +5,7 @@
 // most.  Quotients by it are exact, so every q has one value whichever way it is computed; a finer scale would gain nothing,
 // since a floating-point q has the same relative error everywhere in its range.
 #include "ccdc_block.h"
+#include "ccdc_fp8.h"
 
 #include <cuda_fp8.h>
 
@@ -137,47 +138,6 @@ int launch_quantize(const QuantArgs &a, long long groups, int block_rows, bool v
     return vec ? launch_quantize<T, true>(a, groups, block_rows, s) : launch_quantize<T, false>(a, groups, block_rows, s);
 }
 
-struct ProductArgs {
-    long long M, N, K;
-    int experts;
-    const uint8_t *x, *w;
-    long long ldx, ldw, w_expert;
-    const float *xs, *ws;
-    long long xs_row, xs_col;
-    const int *offsets;
-    void *y;
-    int y_type;
-    long long ldy;
-};
-
-__device__ __forceinline__ float e4m3(uint8_t q) { return __half2float(__nv_cvt_fp8_to_halfraw(q, __NV_E4M3)); }
-
-// one output a thread
-__global__ void __launch_bounds__(256) k_product(ProductArgs a) {
-    const long long n = (long long)blockIdx.x * 32 + (threadIdx.x & 31), m = (long long)blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (n >= a.N || m >= a.M) return;
-    int e = 0;
-    if (a.offsets)
-        while (e < a.experts && m >= a.offsets[e + 1]) ++e;
-    float sum = 0.0f;
-    if (e < a.experts) {
-        const uint8_t *x = a.x + m * a.ldx, *w = a.w + e * a.w_expert + n * a.ldw;
-        const long long kb = (a.K + BLOCK - 1) / BLOCK, nb = (a.N + BLOCK - 1) / BLOCK;
-        for (long long b = 0; b < kb; ++b) {
-            float s = 0.0f;
-            for (long long k = b * BLOCK; k < min(a.K, (b + 1) * BLOCK); ++k) s = fmaf(e4m3(x[k]), e4m3(w[k]), s);
-            sum = fmaf(s, a.xs[m * a.xs_row + b * a.xs_col] * a.ws[(e * nb + n / BLOCK) * kb + b], sum);
-        }
-    }
-    const long long at = m * a.ldy + n;
-    if (a.y_type == CCDC_F32)
-        static_cast<float *>(a.y)[at] = sum;
-    else if (a.y_type == CCDC_BF16)
-        static_cast<bf16 *>(a.y)[at] = from_f32<bf16>(sum);
-    else
-        static_cast<fp16 *>(a.y)[at] = from_f32<fp16>(sum);
-}
-
 }  // namespace
 
 extern "C" {
@@ -209,10 +169,12 @@ int ccdc_matmul_fp8(long long M, long long N, long long K, int experts, const vo
     if (!x || !x_scales || !w || !w_scales || !y || ldx < K || ldw < K || ldy < N || !aligned_to(x, 16) || !aligned_to(w, 16) ||
         ldx % 16 || ldw % 16 || (experts > 1 && (w_expert % 16 || w_expert < 0)))
         return CCDC_EINVAL;
-    ProductArgs a = {M, N, K, experts, static_cast<const uint8_t *>(x), static_cast<const uint8_t *>(w), ldx, ldw, w_expert,
-                     x_scales, w_scales, x_scale_row, x_scale_col, offsets, y, y_dtype, ldy};
-    k_product<<<dim3((unsigned)((N + 31) / 32), (unsigned)((M + 7) / 8)), 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return block_launch_status();
+    int rc;
+    const int sms = block_sm_count(&rc);
+    if (rc != CCDC_OK) return rc;
+    const Fp8Product p = {M, N, K, experts, static_cast<const uint8_t *>(x), static_cast<const uint8_t *>(w), ldx, ldw, w_expert, x_scales,
+                          w_scales, x_scale_row, x_scale_col, offsets, y, y_dtype, ldy};
+    return fp8_mma_launch(p, sms, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

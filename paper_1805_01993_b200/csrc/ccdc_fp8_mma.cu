@@ -1,0 +1,478 @@
+// The 8-bit product y[m][n] = sum_b xs[m][b] ws[n / 128][b] sum_{k in b} x[m][k] w[n][k] on tcgen05 tensor cores.
+//
+// Weights lie along the tensor core's rows and tokens along its columns: a tile has 128 rows of a weight (a pair of SMs 256)
+// and NT tokens, so that few tokens cost few columns, a warp's stores are 32 neighbouring outputs of a token, and the weight's
+// scale is one number for an SM's tile and block.  A block's 128 products are summed in tensor memory, read out, and added to
+// registers with the product of scales, because the scales change from block to block; accumulators alternate, so that the
+// tensor core works on the next blocks meanwhile.  Warps have roles, as in the feed-forward products:
+//   0      fetches 128 rows x 128 bytes of w and NT x 128 bytes of x (a pair: 128 of 256) by TMA into a ring of stages
+//   1      issues tcgen05.mma (kind::f8f6f4), one thread, four K = 32 steps a stage
+//   2..9   add blocks: 32 rows and half of the tokens a warp
+// One persistent block per SM walks the tiles.  With offsets, each expert's rows are cut into tiles by themselves; the list of
+// tiles comes from the offsets in every block's shared memory, so that nothing waits for the host.  With few tiles, k is cut
+// over the blocks of a cluster, whose sums meet in shared memory in the order of k.
+//
+// All waits are bounded: one that runs out sets g_wait_failed, and its warp issues nothing more and waits for the block's end.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "ccdc_block.h"
+#include "ccdc_fp8.h"
+
+namespace {
+
+constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
+constexpr int RING_BYTES = 192 * 1024;
+constexpr int MAX_SPLIT = 8;
+#ifndef CCDC_FP8_WAIT_LIMIT
+#define CCDC_FP8_WAIT_LIMIT (1 << 20)       // polls of a barrier (each may sleep) before a wait has failed
+#endif
+
+__device__ int g_wait_failed;
+
+struct alignas(64) Args {
+    CUtensorMap x, w;
+    const float *xs, *ws;
+    long long xs_row, xs_col, ldy;
+    const int *offsets;
+    void *y;
+    int M, N, kb, nb, experts, y_type, splits, tiles_n;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// the same address in the cluster's block `rank`
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+template <int CG>
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < CCDC_FP8_WAIT_LIMIT; ++i) {
+        uint32_t ok;
+        if constexpr (CG == 2)
+            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                         "selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        else
+            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+                         "selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    atomicExch(&g_wait_failed, 1);
+    return false;
+}
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2"
+                     " [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+                     " [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    if constexpr (CG == 2)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// arrives at the barrier (of both blocks of a pair) when the products issued so far are done
+template <int CG>
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// 8, 16 or 32 columns of this thread's row
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr));
+}
+// Waits for this thread's loads.  Their registers go through the wait, so that no arithmetic on them moves ahead of it.
+template <int W>
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[W]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < W; i += 8)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]),
+                     "+r"(r[i + 7]));
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// shared-memory descriptor of rows of 128 bytes with the 128-byte swizzle, eight to a 1 KiB group
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+struct Tile {
+    int expert, n, row0, rows;          // expert == experts: rows behind the last, to be set to zero
+};
+// Where tile `item` lies.  ends[e] = end of expert e's rows, first[e] = its first tile; `e` only moves forward.  An expert's
+// tiles go in bands of eight weight tiles, token tile by token tile: neighbours in time share both in L2.
+template <int NT>
+__device__ __forceinline__ Tile tile_of(const Args &a, const int *ends, const int *first, int item, int &e) {
+    while (item >= first[e + 1]) ++e;
+    const int start = e ? ends[e - 1] : 0, rows = ends[e] - start, tokens = (rows + NT - 1) / NT;
+    int i = item - first[e];
+    const int band = i / (8 * tokens), width = min(8, a.tiles_n - 8 * band);
+    i -= band * 8 * tokens;
+    const int t = i / width;
+    return {e, 8 * band + i - t * width, start + t * NT, min(NT, rows - t * NT)};
+}
+__device__ __forceinline__ void put(const Args &a, int token, int n, float v) {
+    const long long at = token * a.ldy + n;
+    if (a.y_type == CCDC_F32)
+        static_cast<float *>(a.y)[at] = v;
+    else if (a.y_type == CCDC_BF16)
+        static_cast<bf16 *>(a.y)[at] = from_f32<bf16>(v);
+    else
+        static_cast<fp16 *>(a.y)[at] = from_f32<fp16>(v);
+}
+
+template <int CG, int NT>
+struct Shape {
+    static constexpr int STAGE_BYTES = 128 * 128 + NT / CG * 128;
+    static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+    static constexpr int COLS = NT / 2;                     // tokens of an adding warp
+    static constexpr int ACCS = NT <= 128 ? 4 : 2;
+    static constexpr int SCALE_BYTES = EPI_WARPS * 2 * COLS * 4;
+    static constexpr int FIXED = STAGES * STAGE_BYTES + SCALE_BYTES + 256 + 1024;
+    static constexpr int smem(int experts) { return FIXED + 2 * 4 * (experts + 3); }
+};
+
+// CG SMs to a tile of 128 CG weight rows and NT tokens
+template <int CG, int NT>
+__global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args a) {
+    using S = Shape<CG, NT>;
+    constexpr int W = S::COLS < 32 ? S::COLS : 32;          // columns of one load from tensor memory
+    constexpr uint32_t TMEM_COLUMNS = S::ACCS * NT;
+    extern __shared__ char smem_raw[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int splits = CG == 2 ? 1 : a.splits, per = CG == 2 ? 2 : splits;
+    const int cluster = blockIdx.x / per, clusters = gridDim.x / per;
+    char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    float *scale_base = reinterpret_cast<float *>(smem + S::STAGES * S::STAGE_BYTES);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(reinterpret_cast<char *>(scale_base) + S::SCALE_BYTES);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 31);
+    int *ends = reinterpret_cast<int *>(bars + 32), *first = ends + a.experts + 1;      // [experts + 1], [experts + 2]
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 8 * S::ACCS;
+    static_assert(2 * S::STAGES + 2 * S::ACCS <= 31, "barriers");
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::STAGES; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+        for (int i = 0; i < S::ACCS; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, EPI_WARPS * CG);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                         ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLUMNS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                         ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLUMNS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // the list of tiles: running maximum of the offsets, then running sums of tiles
+    if (warp == 2) {
+        int end = 0, tiles = 0;
+        for (int e0 = 0; e0 <= a.experts; e0 += 32) {
+            const int e = e0 + lane;
+            int v = e < a.experts && a.offsets ? a.offsets[e + 1] : a.M;
+            v = max(0, min(v, a.M));
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int u = __shfl_up_sync(~0u, v, d);
+                if (lane >= d) v = max(v, u);
+            }
+            v = max(v, end);
+            const int before = __shfl_up_sync(~0u, v, 1);
+            int sum = (v - (lane ? before : end) + NT - 1) / NT * a.tiles_n;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int u = __shfl_up_sync(~0u, sum, d);
+                if (lane >= d) sum += u;
+            }
+            if (e <= a.experts) ends[e] = v, first[e + 1] = tiles + sum;
+            end = __shfl_sync(~0u, v, 31);
+            tiles += __shfl_sync(~0u, sum, 31);
+        }
+        if (lane == 0) first[0] = 0;
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (per > 1) cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_slot;
+    const int items = first[a.experts + 1];
+    // this block's part of k
+    const int b0 = CG == 2 ? 0 : (int)((long long)a.kb * rank / splits), b1 = CG == 2 ? a.kb : (int)((long long)a.kb * (rank + 1) / splits);
+
+    bool ok = true;             // no wait of this thread has run out
+    int expert = 0;
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t ring = smem_u32(smem), first_full = CG == 2 ? in_block(full, 0) : full;
+            uint32_t stage = 0, phase = 0;
+            for (int item = cluster; ok && item < items; item += clusters) {
+                const Tile t = tile_of<NT>(a, ends, first, item, expert);
+                if (t.expert == a.experts) break;           // what follows is set to zero
+                const int n = 128 * (CG * t.n + (CG == 2 ? (int)rank : 0)), row = t.row0 + (CG == 2 ? NT / 2 * (int)rank : 0);
+                for (int b = b0; b < b1; ++b) {
+                    if (ok = bar_wait<CG>(empty + 8 * stage, phase ^ 1); !ok) break;
+                    const uint32_t bar = first_full + 8 * stage, dst = ring + stage * S::STAGE_BYTES;
+                    if (CG == 1 || rank == 0) bar_expect(full + 8 * stage, CG * S::STAGE_BYTES);
+                    tma_load<CG>(dst, &a.w, 128 * b, n, t.expert, bar);
+                    tma_load<CG>(dst + 128 * 128, &a.x, 128 * b, row, 0, bar);
+                    if (++stage == S::STAGES) stage = 0, phase ^= 1;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && (CG == 1 || rank == 0)) {
+            // D binary32, A and B e4m3, both along k
+            constexpr uint32_t idesc = 1u << 4 | (uint32_t)(NT >> 3) << 17 | (uint32_t)(128 * CG >> 4) << 24;
+            const uint64_t w0 = operand_desc(smem_u32(smem)), x0 = operand_desc(smem_u32(smem) + 128 * 128);
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            for (int item = cluster; ok && item < items; item += clusters) {
+                if (tile_of<NT>(a, ends, first, item, expert).expert == a.experts) break;
+                for (int b = b0; b < b1; ++b) {
+                    if (ok = bar_wait<CG>(acc_empty + 8 * acc, acc_phase ^ 1); !ok) break;
+                    if (ok = bar_wait<CG>(full + 8 * stage, phase); !ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t w = w0 + stage * (S::STAGE_BYTES >> 4), x = x0 + stage * (S::STAGE_BYTES >> 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma<CG>(tmem + acc * NT, w + 2 * k, x + 2 * k, idesc, k > 0);
+                    mma_commit<CG>(empty + 8 * stage);
+                    mma_commit<CG>(acc_full + 8 * acc);
+                    if (++stage == S::STAGES) stage = 0, phase ^= 1;
+                    if (++acc == S::ACCS) acc = 0, acc_phase ^= 1;
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
+        const int part = (warp - 2) >> 2;           // two warps a quarter: each takes half of the tokens
+        float *scales = scale_base + (warp - 2) * 2 * S::COLS;
+        uint32_t acc = 0, acc_phase = 0, buffer = 0;
+        for (int item = cluster; ok && item < items; item += clusters) {
+            const Tile t = tile_of<NT>(a, ends, first, item, expert);
+            const int nt = CG * t.n + (CG == 2 ? (int)rank : 0), n = 128 * nt + 32 * quarter + lane;
+            const int token0 = t.row0 + part * S::COLS, tokens = min(S::COLS, t.rows - part * S::COLS);
+            float sum[S::COLS] = {};
+            if (t.expert < a.experts) {
+                const float *ws = a.ws + ((long long)t.expert * a.nb + nt) * a.kb;
+                constexpr int PER = (S::COLS + 31) / 32;    // scales a lane fetches
+                float next[PER];
+                const auto fetch = [&](int b) {
+                    const float sw = b < b1 && nt < a.nb ? ws[b] : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const int token = token0 + 32 * i + lane;
+                        next[i] = b < b1 && 32 * i + lane < S::COLS && token < a.M ? sw * a.xs[token * a.xs_row + b * a.xs_col] : 0.0f;
+                    }
+                };
+                fetch(b0);
+                for (int b = b0; b < b1; ++b) {
+                    float *s = scales + buffer * S::COLS;
+                    buffer ^= 1;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i)
+                        if (32 * i + lane < S::COLS) s[32 * i + lane] = next[i];
+                    fetch(b + 1);                           // on its way during this block
+                    __syncwarp();
+                    if (ok = __all_sync(~0u, bar_wait<CG>(acc_full + 8 * acc, acc_phase)); !ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t from = tmem + acc * NT + part * S::COLS + ((uint32_t)(32 * quarter) << 16);
+#pragma unroll
+                    for (int c = 0; c < S::COLS; c += W) {
+                        uint32_t r[W];
+                        tmem_load(from + c, r);
+                        tmem_wait(r);
+                        if (c + W == S::COLS) {             // read out: the tensor core may have it back
+                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) {
+                                if constexpr (CG == 2)
+                                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];"
+                                                 ::"r"(in_block(acc_empty + 8 * acc, 0)) : "memory");
+                                else
+                                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < W; i += 4) {
+                            const float4 v = *reinterpret_cast<const float4 *>(s + c + i);
+                            sum[c + i] = fmaf(__uint_as_float(r[i]), v.x, sum[c + i]);
+                            sum[c + i + 1] = fmaf(__uint_as_float(r[i + 1]), v.y, sum[c + i + 1]);
+                            sum[c + i + 2] = fmaf(__uint_as_float(r[i + 2]), v.z, sum[c + i + 2]);
+                            sum[c + i + 3] = fmaf(__uint_as_float(r[i + 3]), v.w, sum[c + i + 3]);
+                        }
+                    }
+                    if (++acc == S::ACCS) acc = 0, acc_phase ^= 1;
+                }
+            }
+            if (CG == 1 && splits > 1) {        // to be joined below; the ring is not needed any more
+                float *mine = reinterpret_cast<float *>(smem) + part * S::COLS * 128 + 32 * quarter + lane;
+#pragma unroll
+                for (int i = 0; i < S::COLS; ++i) mine[i * 128] = sum[i];
+            } else if (ok && n < a.N) {
+#pragma unroll
+                for (int i = 0; i < S::COLS; ++i)
+                    if (i < tokens) put(a, token0 + i, n, sum[i]);
+            }
+        }
+    }
+    if (!ok) {          // let copies that are still in flight land before the block ends
+        const long long until = clock64() + 2000000;
+        while (clock64() < until) {}
+    }
+    __syncwarp();
+    if (CG == 1 && splits > 1) {
+        // one tile a cluster at most: each block adds its share of the tokens over the blocks, in the order of k
+        cluster_sync();
+        if (cluster < items && warp >= 2) {
+            int e = 0;
+            const Tile t = tile_of<NT>(a, ends, first, cluster, e);
+            const int i = threadIdx.x - 64, lane_n = i & 127, n = 128 * t.n + lane_n;
+            for (int c = NT / splits * (int)rank + (i >> 7); c < NT / splits * ((int)rank + 1); c += 2) {
+                float sum = 0.0f;
+                for (int r = 0; r < splits; ++r) {
+                    float v;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];"
+                                 : "=f"(v) : "r"(in_block(smem_u32(smem) + (c * 128 + lane_n) * 4, r)) : "memory");
+                    sum += v;
+                }
+                if (c < t.rows && n < a.N) put(a, t.row0 + c, n, sum);
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (per > 1) cluster_sync();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if constexpr (CG == 2)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLUMNS));
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLUMNS));
+    }
+}
+
+// ------------------------------------------------------------------ host
+using encode_fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                               const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+encode_fn encoder() {
+    static encode_fn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<encode_fn>(p);
+    }();
+    return fn;
+}
+// bytes [planes][rows][cols], read in boxes of box_rows x 128; what lies outside reads as zero
+bool encode(CUtensorMap *map, const uint8_t *p, long long cols, long long rows, long long ld, long long planes, long long plane, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)(planes > 1 ? plane : ld)};
+    const cuuint32_t box[3] = {128, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t *>(p), dims, strides, box, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int CG, int NT>
+int launch(const Fp8Product &p, int splits, long long most_tiles, int sms, cudaStream_t s) {
+    using S = Shape<CG, NT>;
+    static std::atomic<unsigned long long> done;
+    const void *kernel = reinterpret_cast<const void *>(k_fp8<CG, NT>);
+    const int rc = block_allow_smem(kernel, S::smem(1024), &done);
+    if (rc != CCDC_OK) return rc;
+    Args a;
+    if (!encode(&a.x, p.x, p.K, p.M, p.ldx, 1, 0, NT / CG) || !encode(&a.w, p.w, p.K, p.N, p.ldw, p.experts, p.w_expert, 128)) return CCDC_ECUDA;
+    a.xs = p.xs, a.ws = p.ws, a.xs_row = p.xs_row, a.xs_col = p.xs_col, a.ldy = p.ldy, a.offsets = p.offsets, a.y = p.y;
+    a.M = (int)p.M, a.N = (int)p.N, a.kb = (int)((p.K + 127) / 128), a.nb = (int)((p.N + 127) / 128), a.experts = p.experts;
+    a.y_type = p.y_type, a.splits = splits, a.tiles_n = (a.nb + CG - 1) / CG;
+    const int per = CG == 2 ? 2 : splits;
+    cudaLaunchConfig_t cfg = {};
+    // a cluster that cuts k takes one tile
+    cfg.gridDim = dim3((unsigned)((per == 1 || CG == 2 ? std::min<long long>(most_tiles, std::max(1, sms / per)) : most_tiles) * per));
+    cfg.blockDim = dim3(THREADS), cfg.dynamicSmemBytes = S::smem(p.experts), cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = per, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_fp8<CG, NT>, a);
+    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    ccdc_internal_count_launch();
+    return CCDC_OK;
+}
+
+}  // namespace
+
+int fp8_mma_launch(const Fp8Product &p, int sms, cudaStream_t s) {
+    if (!encoder()) return CCDC_ECUDA;
+    const long long nb = (p.N + 127) / 128, kb = (p.K + 127) / 128, each = (p.M + p.experts - 1) / p.experts;
+    // no more tiles than these, the ones of rows behind the last expert's among them
+    const auto most = [&](long long nt, long long rows_n) {
+        return (p.offsets ? p.M / nt + std::min<long long>(p.experts + 1, p.M) : (p.M + nt - 1) / nt) * rows_n;
+    };
+    if (most(16, nb) > 0x7FFFFFFF) return CCDC_ESIZE;
+    if (each > 128) return launch<2, 256>(p, 1, most(256, (nb + 1) / 2), sms, s);
+    const int nt = each <= 8 ? 16 : each <= 16 ? 32 : each <= 32 ? 64 : 128;
+    int splits = 1;
+    while (splits < MAX_SPLIT && most(nt, nb) * splits * 2 <= sms && 2 * splits <= kb) splits *= 2;
+    return nt == 16   ? launch<1, 16>(p, splits, most(16, nb), sms, s)
+           : nt == 32 ? launch<1, 32>(p, splits, most(32, nb), sms, s)
+           : nt == 64 ? launch<1, 64>(p, splits, most(64, nb), sms, s) : launch<1, 128>(p, splits, most(128, nb), sms, s);
+}
+
+int fp8_mma_status(int *failed) {
+    const cudaError_t e = cudaMemcpyFromSymbol(failed, g_wait_failed, sizeof(int));
+    return e != cudaSuccess ? ccdc_internal_cuda_fail((int)e) : CCDC_OK;
+}

@@ -298,9 +298,12 @@ def test_more_than_two_to_the_31_elements(ccdc):
     ws = torch.rand((E, N // 128, K // 128), device="cuda")
     x, xs = ccdc.quantize_fp8(torch.randn((40, K), device="cuda"))
     offsets = torch.tensor([0] * E + [40], dtype=torch.int32, device="cuda")
-    y = ccdc.matmul_fp8(x, xs, w, ws, offsets=offsets)
-    assert torch.equal(y, ccdc.matmul_fp8(x, xs, last, ws[E - 1].contiguous()))
-    del w, y
+    # another launch may cut k elsewhere: the 64 blocks are joined in another order, with scales below 1
+    y = ccdc.matmul_fp8(x, xs, w, ws, offsets=offsets, out_dtype=torch.float32)
+    z = ccdc.matmul_fp8(x, xs, last, ws[E - 1].contiguous(), out_dtype=torch.float32)
+    size = (x.float() * xs.repeat_interleave(128, 1)).abs() @ last.float().abs().t()
+    assert bool(((y - z).abs() <= 2 * 64 * 2.0 ** -24 * size).all())
+    del w, y, z, size
     M, K, N = (1 << 31) // 8192 + 100, 8192, 128
     x = torch.zeros((M, K), dtype=torch.uint8, device="cuda").view(E4M3)
     x[-64:] = torch.randn((64, K), device="cuda").to(E4M3)
