@@ -1,13 +1,15 @@
 // The 8-bit product y[m][n] = sum_b xs[m][b] ws[n / 128][b] sum_{k in b} x[m][k] w[n][k] on tcgen05 tensor cores.
 //
-// Weights lie along the tensor core's rows and tokens along its columns: a tile has 128 rows of a weight (a pair of SMs 256)
-// and NT tokens, so that few tokens cost few columns, a warp's stores are 32 neighbouring outputs of a token, and the weight's
-// scale is one number for an SM's tile and block.  A block's 128 products are summed in tensor memory, read out, and added to
+// Few tokens: weights lie along the tensor core's rows and tokens along its columns.  A tile has 128 rows of a weight and NT
+// tokens, so that few tokens cost few columns, and a warp's stores are 32 neighbouring outputs of a token.  Many tokens: a pair
+// of SMs has 256 tokens along its rows and 256 rows of the weight along its columns, so that a thread's scales are one number a
+// block (its token's times the weight's).  A block's 128 products are summed in tensor memory, read out, and added to
 // registers with the product of scales, because the scales change from block to block; accumulators alternate, so that the
 // tensor core works on the next blocks meanwhile.  Warps have roles, as in the feed-forward products:
-//   0      fetches 128 rows x 128 bytes of w and NT x 128 bytes of x (a pair: 128 of 256) by TMA into a ring of stages
+//   0      fetches 128 rows x 128 bytes of w and NT x 128 bytes of x (a pair: 128 each) by TMA into a ring of stages
 //   1      issues tcgen05.mma (kind::f8f6f4), one thread, four K = 32 steps a stage
-//   2..9   add blocks: 32 rows and half of the tokens a warp
+//   4..11  add blocks: 32 rows and half of the columns a warp.  A pair's need 128 registers for their sums alone, which
+//          the other four warps give up.
 // One persistent block per SM walks the tiles.  With offsets, each expert's rows are cut into tiles by themselves; the list of
 // tiles comes from the offsets in every block's shared memory, so that nothing waits for the host.  With few tiles, k is cut
 // over the blocks of a cluster, whose sums meet in shared memory in the order of k.
@@ -22,7 +24,7 @@
 
 namespace {
 
-constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
+constexpr int EPI_WARPS = 8, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 constexpr int RING_BYTES = 192 * 1024;
 constexpr int MAX_SPLIT = 8;
 #ifndef CCDC_FP8_WAIT_LIMIT
@@ -53,16 +55,13 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-template <int CG>
+// No barrier here guards memory that threads write: copies and tensor-core products order what they touch themselves.  So the
+// waits and arrivals ask for no order across the cluster, which would cost them an invalidation of the L1 cache each.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
     for (int i = 0; i < CCDC_FP8_WAIT_LIMIT; ++i) {
         uint32_t ok;
-        if constexpr (CG == 2)
-            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-                         "selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        else
-            asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-                         "selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+                     "selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
     }
     atomicExch(&g_wait_failed, 1);
@@ -122,12 +121,16 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
 }
 // Waits for this thread's loads.  Their registers go through the wait, so that no arithmetic on them moves ahead of it.
 template <int W>
-__device__ __forceinline__ void tmem_wait(uint32_t (&r)[W]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+__device__ __forceinline__ void arrived(uint32_t (&r)[W]) {
 #pragma unroll
     for (int i = 0; i < W; i += 8)
         asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]),
                      "+r"(r[i + 7]));
+}
+template <class... R>
+__device__ __forceinline__ void tmem_wait(R &...r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    (arrived(r), ...);
 }
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -164,18 +167,59 @@ __device__ __forceinline__ void put(const Args &a, int token, int n, float v) {
         static_cast<fp16 *>(a.y)[at] = from_f32<fp16>(v);
 }
 
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+// 128 neighbouring outputs of a token: whole sectors of 32 bytes where the row allows it
+template <class T>
+__device__ __forceinline__ void put_row_as(const Args &a, int token, int n0, const float2 (&sum)[64]) {
+    T *row = static_cast<T *>(a.y) + token * a.ldy + n0;
+    constexpr int N = 32 / sizeof(T);
+    const bool whole = (reinterpret_cast<uintptr_t>(row) & 31) == 0;
+#pragma unroll
+    for (int c = 0; c < 128; c += N) {
+        if (whole && n0 + c + N <= a.N) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if constexpr (sizeof(T) == 4)
+                    w[i] = __float_as_uint(i & 1 ? sum[(c + i) / 2].y : sum[(c + i) / 2].x);
+                else
+                    w[i] = pack2<T>(sum[c / 2 + i].x, sum[c / 2 + i].y);
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"(row + c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (n0 + c + i < a.N) row[c + i] = from_f32<T>(i & 1 ? sum[(c + i) / 2].y : sum[(c + i) / 2].x);
+        }
+    }
+}
+__device__ __forceinline__ void put_row(const Args &a, int token, int n0, const float2 (&sum)[64]) {
+    if (a.y_type == CCDC_F32)
+        put_row_as<float>(a, token, n0, sum);
+    else if (a.y_type == CCDC_BF16)
+        put_row_as<bf16>(a, token, n0, sum);
+    else
+        put_row_as<fp16>(a, token, n0, sum);
+}
+
 template <int CG, int NT>
 struct Shape {
     static constexpr int STAGE_BYTES = 128 * 128 + NT / CG * 128;
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
-    static constexpr int COLS = NT / 2;                     // tokens of an adding warp
+    static constexpr int COLS = NT / 2;                     // columns of an adding warp
     static constexpr int ACCS = NT <= 128 ? 4 : 2;
-    static constexpr int SCALE_BYTES = EPI_WARPS * 2 * COLS * 4;
+    static constexpr int SCALE_BYTES = CG == 2 ? 0 : EPI_WARPS * 2 * COLS * 4;
     static constexpr int FIXED = STAGES * STAGE_BYTES + SCALE_BYTES + 256 + 1024;
     static constexpr int smem(int experts) { return FIXED + 2 * 4 * (experts + 3); }
 };
 
-// CG SMs to a tile of 128 CG weight rows and NT tokens
+// CG 1: one SM to a tile of 128 weight rows and NT tokens; CG 2: a pair to 256 tokens and 256 weight rows
 template <int CG, int NT>
 __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args a) {
     using S = Shape<CG, NT>;
@@ -250,6 +294,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
 
     bool ok = true;             // no wait of this thread has run out
     int expert = 0;
+    if constexpr (CG == 2) {
+        // 128 x 56 + 256 x 224 registers: what 384 threads were launched with at 168
+        if (warp < FIRST_EPI) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    }
     if (warp == 0) {
         if (lane == 0) {
             const uint32_t ring = smem_u32(smem), first_full = CG == 2 ? in_block(full, 0) : full;
@@ -257,13 +305,15 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
             for (int item = cluster; ok && item < items; item += clusters) {
                 const Tile t = tile_of<NT>(a, ends, first, item, expert);
                 if (t.expert == a.experts) break;           // what follows is set to zero
-                const int n = 128 * (CG * t.n + (CG == 2 ? (int)rank : 0)), row = t.row0 + (CG == 2 ? NT / 2 * (int)rank : 0);
+                // 128 rows of the tensor core's: of w, of a pair's x; and what lies along its columns
+                const int own = CG == 2 ? 128 * (int)rank : 0, n = 128 * CG * t.n + own, row = t.row0 + own;
+                constexpr int W_AT = CG == 2 ? 128 * 128 : 0, X_AT = CG == 2 ? 0 : 128 * 128;
                 for (int b = b0; b < b1; ++b) {
-                    if (ok = bar_wait<CG>(empty + 8 * stage, phase ^ 1); !ok) break;
+                    if (ok = bar_wait(empty + 8 * stage, phase ^ 1); !ok) break;
                     const uint32_t bar = first_full + 8 * stage, dst = ring + stage * S::STAGE_BYTES;
                     if (CG == 1 || rank == 0) bar_expect(full + 8 * stage, CG * S::STAGE_BYTES);
-                    tma_load<CG>(dst, &a.w, 128 * b, n, t.expert, bar);
-                    tma_load<CG>(dst + 128 * 128, &a.x, 128 * b, row, 0, bar);
+                    tma_load<CG>(dst + W_AT, &a.w, 128 * b, n, t.expert, bar);
+                    tma_load<CG>(dst + X_AT, &a.x, 128 * b, row, 0, bar);
                     if (++stage == S::STAGES) stage = 0, phase ^= 1;
                 }
             }
@@ -272,17 +322,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
         if (lane == 0 && (CG == 1 || rank == 0)) {
             // D binary32, A and B e4m3, both along k
             constexpr uint32_t idesc = 1u << 4 | (uint32_t)(NT >> 3) << 17 | (uint32_t)(128 * CG >> 4) << 24;
-            const uint64_t w0 = operand_desc(smem_u32(smem)), x0 = operand_desc(smem_u32(smem) + 128 * 128);
+            const uint64_t rows0 = operand_desc(smem_u32(smem)), columns0 = operand_desc(smem_u32(smem) + 128 * 128);
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
             for (int item = cluster; ok && item < items; item += clusters) {
                 if (tile_of<NT>(a, ends, first, item, expert).expert == a.experts) break;
                 for (int b = b0; b < b1; ++b) {
-                    if (ok = bar_wait<CG>(acc_empty + 8 * acc, acc_phase ^ 1); !ok) break;
-                    if (ok = bar_wait<CG>(full + 8 * stage, phase); !ok) break;
+                    if (ok = bar_wait(acc_empty + 8 * acc, acc_phase ^ 1); !ok) break;
+                    if (ok = bar_wait(full + 8 * stage, phase); !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t w = w0 + stage * (S::STAGE_BYTES >> 4), x = x0 + stage * (S::STAGE_BYTES >> 4);
+                    const uint64_t rows = rows0 + stage * (S::STAGE_BYTES >> 4), columns = columns0 + stage * (S::STAGE_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma<CG>(tmem + acc * NT, w + 2 * k, x + 2 * k, idesc, k > 0);
+                    for (int k = 0; k < 4; ++k) mma<CG>(tmem + acc * NT, rows + 2 * k, columns + 2 * k, idesc, k > 0);
                     mma_commit<CG>(empty + 8 * stage);
                     mma_commit<CG>(acc_full + 8 * acc);
                     if (++stage == S::STAGES) stage = 0, phase ^= 1;
@@ -290,76 +340,98 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
                 }
             }
         }
-    } else {
+    } else if (warp >= FIRST_EPI) {
+        if constexpr (CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
-        const int part = (warp - 2) >> 2;           // two warps a quarter: each takes half of the tokens
-        float *scales = scale_base + (warp - 2) * 2 * S::COLS;
+        const int part = (warp - FIRST_EPI) >> 2;   // two warps a quarter: each takes half of the columns
+        float *scales = scale_base + (warp - FIRST_EPI) * 2 * S::COLS;
         uint32_t acc = 0, acc_phase = 0, buffer = 0;
         for (int item = cluster; ok && item < items; item += clusters) {
             const Tile t = tile_of<NT>(a, ends, first, item, expert);
-            const int nt = CG * t.n + (CG == 2 ? (int)rank : 0), n = 128 * nt + 32 * quarter + lane;
-            const int token0 = t.row0 + part * S::COLS, tokens = min(S::COLS, t.rows - part * S::COLS);
-            float sum[S::COLS] = {};
+            const int row = 32 * quarter + lane, column0 = part * S::COLS;      // this thread's row of the SM's, its first column
+            const int nb = CG == 2 ? 2 * t.n + part : t.n;                      // the weight's block of 128 rows
+            float2 sum[S::COLS / 2] = {};
             if (t.expert < a.experts) {
-                const float *ws = a.ws + ((long long)t.expert * a.nb + nt) * a.kb;
-                constexpr int PER = (S::COLS + 31) / 32;    // scales a lane fetches
-                float next[PER];
+                const float *ws = a.ws + ((long long)t.expert * a.nb + nb) * a.kb;
+                constexpr int PER = CG == 2 ? 1 : (S::COLS + 31) / 32;          // tokens' scales that a lane fetches
+                float next_x[PER], next_w;
                 const auto fetch = [&](int b) {
-                    const float sw = b < b1 && nt < a.nb ? ws[b] : 0.0f;
+                    next_w = b < b1 && nb < a.nb ? ws[b] : 0.0f;
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        const int token = token0 + 32 * i + lane;
-                        next[i] = b < b1 && 32 * i + lane < S::COLS && token < a.M ? sw * a.xs[token * a.xs_row + b * a.xs_col] : 0.0f;
+                        const int token = t.row0 + (CG == 2 ? 128 * (int)rank + row : column0 + 32 * i + lane);
+                        next_x[i] = b < b1 && token < a.M ? a.xs[token * a.xs_row + b * a.xs_col] : 0.0f;
                     }
                 };
                 fetch(b0);
                 for (int b = b0; b < b1; ++b) {
                     float *s = scales + buffer * S::COLS;
                     buffer ^= 1;
+                    const float2 own = make_float2(next_w * next_x[0], next_w * next_x[0]);
+                    if constexpr (CG == 1) {
 #pragma unroll
-                    for (int i = 0; i < PER; ++i)
-                        if (32 * i + lane < S::COLS) s[32 * i + lane] = next[i];
+                        for (int i = 0; i < PER; ++i)
+                            if (32 * i + lane < S::COLS) s[32 * i + lane] = next_w * next_x[i];
+                    }
                     fetch(b + 1);                           // on its way during this block
                     __syncwarp();
-                    if (ok = __all_sync(~0u, bar_wait<CG>(acc_full + 8 * acc, acc_phase)); !ok) break;
+                    if (ok = __all_sync(~0u, bar_wait(acc_full + 8 * acc, acc_phase)); !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t from = tmem + acc * NT + part * S::COLS + ((uint32_t)(32 * quarter) << 16);
-#pragma unroll
-                    for (int c = 0; c < S::COLS; c += W) {
-                        uint32_t r[W];
-                        tmem_load(from + c, r);
-                        tmem_wait(r);
-                        if (c + W == S::COLS) {             // read out: the tensor core may have it back
-                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0) {
-                                if constexpr (CG == 2)
-                                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];"
-                                                 ::"r"(in_block(acc_empty + 8 * acc, 0)) : "memory");
-                                else
-                                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
-                            }
+                    const uint32_t from = tmem + acc * NT + column0 + ((uint32_t)(32 * quarter) << 16);
+                    const auto give_back = [&] {            // read out: the tensor core may have it back
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if constexpr (CG == 2)
+                                asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_block(acc_empty + 8 * acc, 0)) : "memory");
+                            else
+                                asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(acc_empty + 8 * acc) : "memory");
                         }
+                    };
+                    const auto add = [&](const uint32_t (&r)[W], int c) {
 #pragma unroll
                         for (int i = 0; i < W; i += 4) {
-                            const float4 v = *reinterpret_cast<const float4 *>(s + c + i);
-                            sum[c + i] = fmaf(__uint_as_float(r[i]), v.x, sum[c + i]);
-                            sum[c + i + 1] = fmaf(__uint_as_float(r[i + 1]), v.y, sum[c + i + 1]);
-                            sum[c + i + 2] = fmaf(__uint_as_float(r[i + 2]), v.z, sum[c + i + 2]);
-                            sum[c + i + 3] = fmaf(__uint_as_float(r[i + 3]), v.w, sum[c + i + 3]);
+                            float4 v = make_float4(own.x, own.y, own.x, own.y);
+                            if constexpr (CG == 1) v = *reinterpret_cast<const float4 *>(s + c + i);
+                            float2 &lo = sum[(c + i) / 2], &hi = sum[(c + i) / 2 + 1];
+                            lo = fma2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), make_float2(v.x, v.y), lo);
+                            hi = fma2(make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), make_float2(v.z, v.w), hi);
+                        }
+                    };
+                    if constexpr (S::COLS == W) {
+                        uint32_t r[W];
+                        tmem_load(from, r);
+                        tmem_wait(r);
+                        give_back();
+                        add(r, 0);
+                    } else {                                // two loads under way at a time
+                        uint32_t r[2][W];
+                        tmem_load(from, r[0]);
+                        tmem_load(from + W, r[1]);
+#pragma unroll
+                        for (int c = 0; c < S::COLS; c += 2 * W) {
+                            tmem_wait(r[0], r[1]);
+                            if (c + 2 * W == S::COLS) give_back();
+                            add(r[0], c);
+                            if (c + 2 * W < S::COLS) tmem_load(from + c + 2 * W, r[0]);
+                            add(r[1], c + W);
+                            if (c + 2 * W < S::COLS) tmem_load(from + c + 3 * W, r[1]);
                         }
                     }
                     if (++acc == S::ACCS) acc = 0, acc_phase ^= 1;
                 }
             }
-            if (CG == 1 && splits > 1) {        // to be joined below; the ring is not needed any more
-                float *mine = reinterpret_cast<float *>(smem) + part * S::COLS * 128 + 32 * quarter + lane;
+            if constexpr (CG == 2) {
+                const int token = 128 * (int)rank + row, n0 = 256 * t.n + column0;
+                if (ok && token < t.rows) put_row(a, t.row0 + token, n0, sum);
+            } else if (splits > 1) {            // to be joined below; the ring is not needed any more
+                float *mine = reinterpret_cast<float *>(smem) + column0 * 128 + row;
 #pragma unroll
-                for (int i = 0; i < S::COLS; ++i) mine[i * 128] = sum[i];
-            } else if (ok && n < a.N) {
+                for (int i = 0; i < S::COLS; ++i) mine[i * 128] = i & 1 ? sum[i / 2].y : sum[i / 2].x;
+            } else if (ok && 128 * t.n + row < a.N) {
 #pragma unroll
                 for (int i = 0; i < S::COLS; ++i)
-                    if (i < tokens) put(a, token0 + i, n, sum[i]);
+                    if (column0 + i < t.rows) put(a, t.row0 + column0 + i, 128 * t.n + row, i & 1 ? sum[i / 2].y : sum[i / 2].x);
             }
         }
     }
@@ -371,10 +443,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
     if (CG == 1 && splits > 1) {
         // one tile a cluster at most: each block adds its share of the tokens over the blocks, in the order of k
         cluster_sync();
-        if (cluster < items && warp >= 2) {
+        if (cluster < items && warp >= FIRST_EPI) {
             int e = 0;
             const Tile t = tile_of<NT>(a, ends, first, cluster, e);
-            const int i = threadIdx.x - 64, lane_n = i & 127, n = 128 * t.n + lane_n;
+            const int i = threadIdx.x - 32 * FIRST_EPI, lane_n = i & 127, n = 128 * t.n + lane_n;
             for (int c = NT / splits * (int)rank + (i >> 7); c < NT / splits * ((int)rank + 1); c += 2) {
                 float sum = 0.0f;
                 for (int r = 0; r < splits; ++r) {
