@@ -174,38 +174,57 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
-// 128 neighbouring outputs of a token: whole sectors of 32 bytes where the row allows it
+// 128 neighbouring outputs of each of a warp's 32 tokens, one token a thread.  Rows that start at whole sectors of 32 bytes are
+// written sector by sector; others go through shared memory (`stage`), 64 bytes of a row at a time, so that neighbouring threads
+// write neighbouring elements.  `left`: tokens of the warp's that are there.
+constexpr int STAGE_ROW = 64 + 4, STAGE_WARP = 32 * STAGE_ROW;
 template <class T>
-__device__ __forceinline__ void put_row_as(const Args &a, int token, int n0, const float2 (&sum)[64]) {
-    T *row = static_cast<T *>(a.y) + token * a.ldy + n0;
-    constexpr int N = 32 / sizeof(T);
-    const bool whole = (reinterpret_cast<uintptr_t>(row) & 31) == 0;
+__device__ __forceinline__ void put_rows_as(const Args &a, long long token0, int left, int n0, const float2 (&sum)[64], int lane, char *stage) {
+    constexpr int N = 64 / sizeof(T);           // columns of a step
+    T *y = static_cast<T *>(a.y) + token0 * a.ldy + n0;
+    if ((reinterpret_cast<uintptr_t>(a.y) | (uintptr_t)(a.ldy * sizeof(T))) % 32 == 0 && n0 + 128 <= a.N) {
+        T *row = y + lane * a.ldy;
+        if (lane < left)
+#pragma unroll
+            for (int c = 0; c < 128; c += N / 2) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if constexpr (sizeof(T) == 4)
+                        w[i] = __float_as_uint(i & 1 ? sum[(c + i) / 2].y : sum[(c + i) / 2].x);
+                    else
+                        w[i] = pack2<T>(sum[c / 2 + i].x, sum[c / 2 + i].y);
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                             "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+            }
+        return;
+    }
 #pragma unroll
     for (int c = 0; c < 128; c += N) {
-        if (whole && n0 + c + N <= a.N) {
-            uint32_t w[8];
+        if (n0 + c >= a.N) break;
+        uint32_t *mine = reinterpret_cast<uint32_t *>(stage + lane * STAGE_ROW);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if constexpr (sizeof(T) == 4)
-                    w[i] = __float_as_uint(i & 1 ? sum[(c + i) / 2].y : sum[(c + i) / 2].x);
-                else
-                    w[i] = pack2<T>(sum[c / 2 + i].x, sum[c / 2 + i].y);
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                         ::"l"(row + c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (n0 + c + i < a.N) row[c + i] = from_f32<T>(i & 1 ? sum[(c + i) / 2].y : sum[(c + i) / 2].x);
-        }
+        for (int i = 0; i < 16; ++i)
+            if constexpr (sizeof(T) == 4)
+                mine[i] = __float_as_uint(i & 1 ? sum[(c + i) / 2].y : sum[(c + i) / 2].x);
+            else
+                mine[i] = pack2<T>(sum[c / 2 + i].x, sum[c / 2 + i].y);
+        __syncwarp();
+        const int column = lane % N;
+        if (n0 + c + column < a.N)
+#pragma unroll 4
+            for (int r = lane / N; r < left; r += 32 / N)
+                y[r * a.ldy + c + column] = *reinterpret_cast<const T *>(stage + r * STAGE_ROW + column * sizeof(T));
+        __syncwarp();
     }
 }
-__device__ __forceinline__ void put_row(const Args &a, int token, int n0, const float2 (&sum)[64]) {
+__device__ __forceinline__ void put_rows(const Args &a, long long token0, int left, int n0, const float2 (&sum)[64], int lane, char *stage) {
     if (a.y_type == CCDC_F32)
-        put_row_as<float>(a, token, n0, sum);
+        put_rows_as<float>(a, token0, left, n0, sum, lane, stage);
     else if (a.y_type == CCDC_BF16)
-        put_row_as<bf16>(a, token, n0, sum);
+        put_rows_as<bf16>(a, token0, left, n0, sum, lane, stage);
     else
-        put_row_as<fp16>(a, token, n0, sum);
+        put_rows_as<fp16>(a, token0, left, n0, sum, lane, stage);
 }
 
 template <int CG, int NT>
@@ -214,8 +233,9 @@ struct Shape {
     static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
     static constexpr int COLS = NT / 2;                     // columns of an adding warp
     static constexpr int ACCS = NT <= 128 ? 4 : 2;
-    static constexpr int SCALE_BYTES = CG == 2 ? 0 : EPI_WARPS * 2 * COLS * 4;
-    static constexpr int FIXED = STAGES * STAGE_BYTES + SCALE_BYTES + 256 + 1024;
+    // of each adding warp: the scales of two blocks, or outputs on their way
+    static constexpr int WARP_BYTES = CG == 2 ? STAGE_WARP : 2 * COLS * 4;
+    static constexpr int FIXED = STAGES * STAGE_BYTES + EPI_WARPS * WARP_BYTES + 256 + 1024;
     static constexpr int smem(int experts) { return FIXED + 2 * 4 * (experts + 3); }
 };
 
@@ -232,8 +252,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
     const int splits = CG == 2 ? 1 : a.splits, per = CG == 2 ? 2 : splits;
     const int cluster = blockIdx.x / per, clusters = gridDim.x / per;
     char *smem = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    float *scale_base = reinterpret_cast<float *>(smem + S::STAGES * S::STAGE_BYTES);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(reinterpret_cast<char *>(scale_base) + S::SCALE_BYTES);
+    char *warp_base = smem + S::STAGES * S::STAGE_BYTES;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(warp_base + EPI_WARPS * S::WARP_BYTES);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 31);
     int *ends = reinterpret_cast<int *>(bars + 32), *first = ends + a.experts + 1;      // [experts + 1], [experts + 2]
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 8 * S::ACCS;
@@ -344,7 +364,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
         if constexpr (CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
         const int part = (warp - FIRST_EPI) >> 2;   // two warps a quarter: each takes half of the columns
-        float *scales = scale_base + (warp - FIRST_EPI) * 2 * S::COLS;
+        char *own_bytes = warp_base + (warp - FIRST_EPI) * S::WARP_BYTES;
         uint32_t acc = 0, acc_phase = 0, buffer = 0;
         for (int item = cluster; ok && item < items; item += clusters) {
             const Tile t = tile_of<NT>(a, ends, first, item, expert);
@@ -365,7 +385,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
                 };
                 fetch(b0);
                 for (int b = b0; b < b1; ++b) {
-                    float *s = scales + buffer * S::COLS;
+                    float *s = reinterpret_cast<float *>(own_bytes) + buffer * S::COLS;
                     buffer ^= 1;
                     const float2 own = make_float2(next_w * next_x[0], next_w * next_x[0]);
                     if constexpr (CG == 1) {
@@ -422,8 +442,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
                 }
             }
             if constexpr (CG == 2) {
-                const int token = 128 * (int)rank + row, n0 = 256 * t.n + column0;
-                if (ok && token < t.rows) put_row(a, t.row0 + token, n0, sum);
+                const int token = 128 * (int)rank + 32 * quarter, n0 = 256 * t.n + column0;
+                if (ok && token < t.rows && n0 < a.N) put_rows(a, t.row0 + token, min(32, t.rows - token), n0, sum, lane, own_bytes);
             } else if (splits > 1) {            // to be joined below; the ring is not needed any more
                 float *mine = reinterpret_cast<float *>(smem) + column0 * 128 + row;
 #pragma unroll
