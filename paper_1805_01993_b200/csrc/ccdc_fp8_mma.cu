@@ -230,7 +230,10 @@ __device__ __forceinline__ void put_rows(const Args &a, long long token0, int le
 template <int CG, int NT>
 struct Shape {
     static constexpr int STAGE_BYTES = 128 * 128 + NT / CG * 128;
-    static constexpr int STAGES = RING_BYTES / STAGE_BYTES;
+    // Two blocks an SM where their sums' registers allow it: one adds and writes while the other fetches (200 rows over 64
+    // weights of 2048 x 4096: 99 us with one, 77 with two).
+    static constexpr int PER_SM = CG == 1 && NT <= 64 ? 2 : 1;
+    static constexpr int STAGES = RING_BYTES / PER_SM / STAGE_BYTES;
     static constexpr int COLS = NT / 2;                     // columns of an adding warp
     static constexpr int ACCS = NT <= 128 ? 4 : 2;
     // of each adding warp: the scales of two blocks, or outputs on their way
@@ -241,9 +244,9 @@ struct Shape {
 
 // CG 1: one SM to a tile of 128 weight rows and NT tokens; CG 2: a pair to 256 tokens and 256 weight rows
 template <int CG, int NT>
-__global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __grid_constant__ Args a) {
     using S = Shape<CG, NT>;
-    constexpr int W = S::COLS < 32 ? S::COLS : 32;          // columns of one load from tensor memory
+    constexpr int W = S::COLS == 32 ? 16 : S::COLS < 32 ? S::COLS : 32;     // columns of one load from tensor memory
     constexpr uint32_t TMEM_COLUMNS = S::ACCS * NT;
     extern __shared__ char smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -466,16 +469,27 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp8(const __grid_constant__ Args
         if (cluster < items && warp >= FIRST_EPI) {
             int e = 0;
             const Tile t = tile_of<NT>(a, ends, first, cluster, e);
-            const int i = threadIdx.x - 32 * FIRST_EPI, lane_n = i & 127, n = 128 * t.n + lane_n;
-            for (int c = NT / splits * (int)rank + (i >> 7); c < NT / splits * ((int)rank + 1); c += 2) {
-                float sum = 0.0f;
-                for (int r = 0; r < splits; ++r) {
-                    float v;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                                 : "=f"(v) : "r"(in_block(smem_u32(smem) + (c * 128 + lane_n) * 4, r)) : "memory");
-                    sum += v;
+            // a warp to a token's 128 outputs; the loads of all blocks are under way before the first is added
+            for (int c = NT / splits * (int)rank + warp - FIRST_EPI; c < NT / splits * ((int)rank + 1); c += EPI_WARPS) {
+                if (c >= t.rows) break;
+                float v[MAX_SPLIT][4];
+#pragma unroll
+                for (int r = 0; r < MAX_SPLIT; ++r)
+                    if (r < splits) {
+                        const uint32_t at = in_block(smem_u32(smem) + (c * 128 + lane) * 4, r);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][i]) : "r"(at + 128 * i) : "memory");
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float sum = v[0][i];
+#pragma unroll
+                    for (int r = 1; r < MAX_SPLIT; ++r)
+                        if (r < splits) sum += v[r][i];
+                    const int n = 128 * t.n + 32 * i + lane;
+                    if (n < a.N) put(a, t.row0 + c, n, sum);
                 }
-                if (c < t.rows && n < a.N) put(a, t.row0 + c, n, sum);
             }
         }
     }
@@ -531,7 +545,7 @@ int launch(const Fp8Product &p, int splits, long long most_tiles, int sms, cudaS
     const int per = CG == 2 ? 2 : splits;
     cudaLaunchConfig_t cfg = {};
     // a cluster that cuts k takes one tile
-    cfg.gridDim = dim3((unsigned)((per == 1 || CG == 2 ? std::min<long long>(most_tiles, std::max(1, sms / per)) : most_tiles) * per));
+    cfg.gridDim = dim3((unsigned)((per == 1 || CG == 2 ? std::min<long long>(most_tiles, std::max(1, S::PER_SM * sms / per)) : most_tiles) * per));
     cfg.blockDim = dim3(THREADS), cfg.dynamicSmemBytes = S::smem(p.experts), cfg.stream = s;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -558,7 +572,8 @@ int fp8_mma_launch(const Fp8Product &p, int sms, cudaStream_t s) {
     if (each > 128) return launch<2, 256>(p, 1, most(256, (nb + 1) / 2), sms, s);
     const int nt = each <= 8 ? 16 : each <= 16 ? 32 : each <= 32 ? 64 : 128;
     int splits = 1;
-    while (splits < MAX_SPLIT && most(nt, nb) * splits * 2 <= sms && 2 * splits <= kb) splits *= 2;
+    const int blocks = nt <= 64 ? 2 * sms : sms;
+    while (splits < MAX_SPLIT && most(nt, nb) * splits * 2 <= blocks && 2 * splits <= kb) splits *= 2;
     return nt == 16   ? launch<1, 16>(p, splits, most(16, nb), sms, s)
            : nt == 32 ? launch<1, 32>(p, splits, most(32, nb), sms, s)
            : nt == 64 ? launch<1, 64>(p, splits, most(64, nb), sms, s) : launch<1, 128>(p, splits, most(128, nb), sms, s);
