@@ -71,6 +71,7 @@ __device__ __forceinline__ void put8(uint8_t *row, long long c, long long K, con
 template <class T, bool VEC, int ROWS>
 __global__ void __launch_bounds__(256) k_quantize_rows(QuantArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // a product that follows may set itself up
     const long long c = (long long)blockIdx.y * 256 + lane * 8, m0 = (long long)blockIdx.x * 8 * ROWS + warp;
     float f[ROWS][8];
 #pragma unroll

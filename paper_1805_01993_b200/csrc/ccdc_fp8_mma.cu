@@ -1,14 +1,15 @@
 // The 8-bit product y[m][n] = sum_b xs[m][b] ws[n / 128][b] sum_{k in b} x[m][k] w[n][k] on tcgen05 tensor cores.
 //
 // Few tokens: weights lie along the tensor core's rows and tokens along its columns.  A tile has 128 rows of a weight and NT
-// tokens, so that few tokens cost few columns, and a warp's stores are 32 neighbouring outputs of a token.  Many tokens: a pair
-// of SMs has 256 tokens along its rows and 256 rows of the weight along its columns, so that a thread's scales are one number a
-// block (its token's times the weight's).  A block's 128 products are summed in tensor memory, read out, and added to
+// tokens, so that few tokens cost few columns, and a warp's stores are 32 neighbouring outputs of a token.  More tokens lie along
+// the rows, 128 to an SM or 256 to a pair, and 256 rows of the weight along the columns: a thread's scales are then one number
+// a block (its token's times the weight's), where a scale for each column costs a shared-memory read for every four products
+// (670 cycles a block of 128 x 128).  A block's 128 products are summed in tensor memory, read out, and added to
 // registers with the product of scales, because the scales change from block to block; accumulators alternate, so that the
 // tensor core works on the next blocks meanwhile.  Warps have roles, as in the feed-forward products:
-//   0      fetches 128 rows x 128 bytes of w and NT x 128 bytes of x (a pair: 128 each) by TMA into a ring of stages
+//   0      fetches 128 bytes of each of the tile's rows of w and x (a pair: half of them each) by TMA into a ring of stages
 //   1      issues tcgen05.mma (kind::f8f6f4), one thread, four K = 32 steps a stage
-//   4..11  add blocks: 32 rows and half of the columns a warp.  A pair's need 128 registers for their sums alone, which
+//   4..11  add blocks: 32 rows and half of the columns a warp.  256 columns need 128 registers for their sums alone, which
 //          the other four warps give up.
 // One persistent block per SM walks the tiles.  With offsets, each expert's rows are cut into tiles by themselves; the list of
 // tiles comes from the offsets in every block's shared memory, so that nothing waits for the host.  With few tiles, k is cut
@@ -26,7 +27,7 @@ namespace {
 
 constexpr int EPI_WARPS = 8, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 constexpr int RING_BYTES = 192 * 1024;
-constexpr int MAX_SPLIT = 8;
+constexpr int MAX_SPLIT = 8;                // a power of two, as all splits
 #ifndef CCDC_FP8_WAIT_LIMIT
 #define CCDC_FP8_WAIT_LIMIT (1 << 20)       // polls of a barrier (each may sleep) before a wait has failed
 #endif
@@ -174,19 +175,19 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
-// 128 neighbouring outputs of each of a warp's 32 tokens, one token a thread.  Rows that start at whole sectors of 32 bytes are
+// COLS neighbouring outputs of each of a warp's 32 tokens, one token a thread.  Rows that start at whole sectors of 32 bytes are
 // written sector by sector; others go through shared memory (`stage`), 64 bytes of a row at a time, so that neighbouring threads
 // write neighbouring elements.  `left`: tokens of the warp's that are there.
 constexpr int STAGE_ROW = 64 + 4, STAGE_WARP = 32 * STAGE_ROW;
-template <class T>
-__device__ __forceinline__ void put_rows_as(const Args &a, long long token0, int left, int n0, const float2 (&sum)[64], int lane, char *stage) {
+template <class T, int COLS>
+__device__ __forceinline__ void put_rows_as(const Args &a, long long token0, int left, int n0, const float2 (&sum)[COLS / 2], int lane, char *stage) {
     constexpr int N = 64 / sizeof(T);           // columns of a step
     T *y = static_cast<T *>(a.y) + token0 * a.ldy + n0;
-    if ((reinterpret_cast<uintptr_t>(a.y) | (uintptr_t)(a.ldy * sizeof(T))) % 32 == 0 && n0 + 128 <= a.N) {
+    if ((reinterpret_cast<uintptr_t>(a.y) | (uintptr_t)(a.ldy * sizeof(T))) % 32 == 0 && n0 + COLS <= a.N) {
         T *row = y + lane * a.ldy;
         if (lane < left)
 #pragma unroll
-            for (int c = 0; c < 128; c += N / 2) {
+            for (int c = 0; c < COLS; c += N / 2) {
                 uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -200,7 +201,7 @@ __device__ __forceinline__ void put_rows_as(const Args &a, long long token0, int
         return;
     }
 #pragma unroll
-    for (int c = 0; c < 128; c += N) {
+    for (int c = 0; c < COLS; c += N) {
         if (n0 + c >= a.N) break;
         uint32_t *mine = reinterpret_cast<uint32_t *>(stage + lane * STAGE_ROW);
 #pragma unroll
@@ -218,36 +219,76 @@ __device__ __forceinline__ void put_rows_as(const Args &a, long long token0, int
         __syncwarp();
     }
 }
-__device__ __forceinline__ void put_rows(const Args &a, long long token0, int left, int n0, const float2 (&sum)[64], int lane, char *stage) {
+template <int COLS>
+__device__ __forceinline__ void put_rows(const Args &a, long long token0, int left, int n0, const float2 (&sum)[COLS / 2], int lane, char *stage) {
     if (a.y_type == CCDC_F32)
-        put_rows_as<float>(a, token0, left, n0, sum, lane, stage);
+        put_rows_as<float, COLS>(a, token0, left, n0, sum, lane, stage);
     else if (a.y_type == CCDC_BF16)
-        put_rows_as<bf16>(a, token0, left, n0, sum, lane, stage);
+        put_rows_as<bf16, COLS>(a, token0, left, n0, sum, lane, stage);
     else
-        put_rows_as<fp16>(a, token0, left, n0, sum, lane, stage);
+        put_rows_as<fp16, COLS>(a, token0, left, n0, sum, lane, stage);
 }
 
-template <int CG, int NT>
+// CG SMs to a tile of NT tokens and NW weight rows
+template <int CG, int NT, int NW>
 struct Shape {
-    static constexpr int STAGE_BYTES = 128 * 128 + NT / CG * 128;
+    static constexpr bool ROWS = NT >= 128;                 // tokens lie along the rows
+    static constexpr int N = ROWS ? NW : NT;                // columns
+    static_assert((ROWS ? NT : NW) == 128 * CG, "rows of the tensor core");
+    static constexpr int STAGE_BYTES = 128 * 128 + N / CG * 128;
     // Two blocks an SM where their sums' registers allow it: one adds and writes while the other fetches (200 rows over 64
     // weights of 2048 x 4096: 99 us with one, 77 with two).
-    static constexpr int PER_SM = CG == 1 && NT <= 64 ? 2 : 1;
+    static constexpr int PER_SM = ROWS ? 1 : 2;
     static constexpr int STAGES = RING_BYTES / PER_SM / STAGE_BYTES;
-    static constexpr int COLS = NT / 2;                     // columns of an adding warp
-    static constexpr int ACCS = NT <= 128 ? 4 : 2;
+    static constexpr int COLS = N / 2;                      // columns of an adding warp
+    static constexpr int ACCS = N <= 128 ? 4 : 2;
+    static constexpr bool WIDE = COLS == 128;               // registers move to the adding warps
     // of each adding warp: the scales of two blocks, or outputs on their way
-    static constexpr int WARP_BYTES = CG == 2 ? STAGE_WARP : 2 * COLS * 4;
+    static constexpr int WARP_BYTES = ROWS ? STAGE_WARP : 2 * COLS * 4;
     static constexpr int FIXED = STAGES * STAGE_BYTES + EPI_WARPS * WARP_BYTES + 256 + 1024;
     static constexpr int smem(int experts) { return FIXED + 2 * 4 * (experts + 3); }
 };
 
-// CG 1: one SM to a tile of 128 weight rows and NT tokens; CG 2: a pair to 256 tokens and 256 weight rows
-template <int CG, int NT>
-__global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __grid_constant__ Args a) {
-    using S = Shape<CG, NT>;
+// This block's share of the tokens, each output added over the blocks in the order of k.  A warp to 128 outputs of a token, and
+// to as many tokens at a time as keep the loads of eight sums under way.
+template <int NT, int NW, int SPLITS>
+__device__ __forceinline__ void join(const Args &a, const Tile &t, uint32_t smem, int rank, int warp, int lane) {
+    constexpr int SHARE = NT / SPLITS, UNITS = SHARE * (NW / 128), AT_ONCE = MAX_SPLIT / SPLITS;
+#pragma unroll 1
+    for (int u0 = warp; u0 < UNITS; u0 += EPI_WARPS * AT_ONCE) {
+        float v[AT_ONCE][SPLITS][4];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int u = min(u0 + j * EPI_WARPS, UNITS - 1), token = SHARE * rank + u / (NW / 128), n = 128 * (u % (NW / 128)) + lane;
+#pragma unroll
+            for (int r = 0; r < SPLITS; ++r) {
+                const uint32_t from = in_block(smem + 4 * (token * (NW + 1) + n), r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[j][r][i]) : "r"(from + 128 * i) : "memory");
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int u = u0 + j * EPI_WARPS, token = SHARE * rank + u / (NW / 128);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float sum = v[j][0][i];
+#pragma unroll
+                for (int r = 1; r < SPLITS; ++r) sum += v[j][r][i];
+                const int n = NW * t.n + 128 * (u % (NW / 128)) + 32 * i + lane;
+                if (u < UNITS && token < t.rows && n < a.N) put(a, t.row0 + token, n, sum);
+            }
+        }
+    }
+}
+
+template <int CG, int NT, int NW>
+__global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(const __grid_constant__ Args a) {
+    using S = Shape<CG, NT, NW>;
     constexpr int W = S::COLS == 32 ? 16 : S::COLS < 32 ? S::COLS : 32;     // columns of one load from tensor memory
-    constexpr uint32_t TMEM_COLUMNS = S::ACCS * NT;
+    constexpr int JOIN_ROW = NW + 1;    // words of a token that waits to be joined, so that neither way to write them meets conflicts
+    constexpr uint32_t TMEM_COLUMNS = S::ACCS * S::N;
     extern __shared__ char smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank;
@@ -317,7 +358,7 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
 
     bool ok = true;             // no wait of this thread has run out
     int expert = 0;
-    if constexpr (CG == 2) {
+    if constexpr (S::WIDE) {
         // 128 x 56 + 256 x 224 registers: what 384 threads were launched with at 168
         if (warp < FIRST_EPI) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     }
@@ -328,9 +369,8 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
             for (int item = cluster; ok && item < items; item += clusters) {
                 const Tile t = tile_of<NT>(a, ends, first, item, expert);
                 if (t.expert == a.experts) break;           // what follows is set to zero
-                // 128 rows of the tensor core's: of w, of a pair's x; and what lies along its columns
-                const int own = CG == 2 ? 128 * (int)rank : 0, n = 128 * CG * t.n + own, row = t.row0 + own;
-                constexpr int W_AT = CG == 2 ? 128 * 128 : 0, X_AT = CG == 2 ? 0 : 128 * 128;
+                const int own = CG == 2 ? 128 * (int)rank : 0, n = NW * t.n + own, row = t.row0 + own;
+                constexpr int W_AT = S::ROWS ? 128 * 128 : 0, X_AT = S::ROWS ? 0 : 128 * 128;
                 for (int b = b0; b < b1; ++b) {
                     if (ok = bar_wait(empty + 8 * stage, phase ^ 1); !ok) break;
                     const uint32_t bar = first_full + 8 * stage, dst = ring + stage * S::STAGE_BYTES;
@@ -344,7 +384,7 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
     } else if (warp == 1) {
         if (lane == 0 && (CG == 1 || rank == 0)) {
             // D binary32, A and B e4m3, both along k
-            constexpr uint32_t idesc = 1u << 4 | (uint32_t)(NT >> 3) << 17 | (uint32_t)(128 * CG >> 4) << 24;
+            constexpr uint32_t idesc = 1u << 4 | (uint32_t)(S::N >> 3) << 17 | (uint32_t)(128 * CG >> 4) << 24;
             const uint64_t rows0 = operand_desc(smem_u32(smem)), columns0 = operand_desc(smem_u32(smem) + 128 * 128);
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
             for (int item = cluster; ok && item < items; item += clusters) {
@@ -355,7 +395,7 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t rows = rows0 + stage * (S::STAGE_BYTES >> 4), columns = columns0 + stage * (S::STAGE_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma<CG>(tmem + acc * NT, rows + 2 * k, columns + 2 * k, idesc, k > 0);
+                    for (int k = 0; k < 4; ++k) mma<CG>(tmem + acc * S::N, rows + 2 * k, columns + 2 * k, idesc, k > 0);
                     mma_commit<CG>(empty + 8 * stage);
                     mma_commit<CG>(acc_full + 8 * acc);
                     if (++stage == S::STAGES) stage = 0, phase ^= 1;
@@ -364,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
             }
         }
     } else if (warp >= FIRST_EPI) {
-        if constexpr (CG == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        if constexpr (S::WIDE) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
         const int part = (warp - FIRST_EPI) >> 2;   // two warps a quarter: each takes half of the columns
         char *own_bytes = warp_base + (warp - FIRST_EPI) * S::WARP_BYTES;
@@ -372,35 +412,40 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
         for (int item = cluster; ok && item < items; item += clusters) {
             const Tile t = tile_of<NT>(a, ends, first, item, expert);
             const int row = 32 * quarter + lane, column0 = part * S::COLS;      // this thread's row of the SM's, its first column
-            const int nb = CG == 2 ? 2 * t.n + part : t.n;                      // the weight's block of 128 rows
+            const int nb = NW / 128 * t.n + column0 / 128 * S::ROWS;            // the weight's block of 128 rows
+            const int own_row = (CG == 2 ? 128 * (int)rank : 0) + row;
             float2 sum[S::COLS / 2] = {};
             if (t.expert < a.experts) {
                 const float *ws = a.ws + ((long long)t.expert * a.nb + nb) * a.kb;
-                constexpr int PER = CG == 2 ? 1 : (S::COLS + 31) / 32;          // tokens' scales that a lane fetches
-                float next_x[PER], next_w;
-                const auto fetch = [&](int b) {
-                    next_w = b < b1 && nb < a.nb ? ws[b] : 0.0f;
+                constexpr int PER = S::ROWS ? 1 : (S::COLS + 31) / 32;          // tokens' scales that a lane fetches
+                float xs[3][PER], sw[3];                                        // of this block and the next two
+                const auto fetch = [&](int b, int to) {
+                    sw[to] = b < b1 && nb < a.nb ? ws[b] : 0.0f;
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        const int token = t.row0 + (CG == 2 ? 128 * (int)rank + row : column0 + 32 * i + lane);
-                        next_x[i] = b < b1 && token < a.M ? a.xs[token * a.xs_row + b * a.xs_col] : 0.0f;
+                        const int token = t.row0 + (S::ROWS ? own_row : column0 + 32 * i + lane);
+                        xs[to][i] = b < b1 && token < a.M ? a.xs[token * a.xs_row + b * a.xs_col] : 0.0f;
                     }
                 };
-                fetch(b0);
+                fetch(b0, 1);
+                fetch(b0 + 1, 2);
                 for (int b = b0; b < b1; ++b) {
                     float *s = reinterpret_cast<float *>(own_bytes) + buffer * S::COLS;
                     buffer ^= 1;
-                    const float2 own = make_float2(next_w * next_x[0], next_w * next_x[0]);
-                    if constexpr (CG == 1) {
+                    sw[0] = sw[1], sw[1] = sw[2];
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) xs[0][i] = xs[1][i], xs[1][i] = xs[2][i];
+                    const float2 own = make_float2(sw[0] * xs[0][0], sw[0] * xs[0][0]);
+                    if constexpr (!S::ROWS) {
 #pragma unroll
                         for (int i = 0; i < PER; ++i)
-                            if (32 * i + lane < S::COLS) s[32 * i + lane] = next_w * next_x[i];
+                            if (32 * i + lane < S::COLS) s[32 * i + lane] = sw[0] * xs[0][i];
                     }
-                    fetch(b + 1);                           // on its way during this block
+                    fetch(b + 2, 2);                        // on its way during this block and the next
                     __syncwarp();
                     if (ok = __all_sync(~0u, bar_wait(acc_full + 8 * acc, acc_phase)); !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t from = tmem + acc * NT + column0 + ((uint32_t)(32 * quarter) << 16);
+                    const uint32_t from = tmem + acc * S::N + column0 + ((uint32_t)(32 * quarter) << 16);
                     const auto give_back = [&] {            // read out: the tensor core may have it back
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
@@ -415,18 +460,21 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
 #pragma unroll
                         for (int i = 0; i < W; i += 4) {
                             float4 v = make_float4(own.x, own.y, own.x, own.y);
-                            if constexpr (CG == 1) v = *reinterpret_cast<const float4 *>(s + c + i);
+                            if constexpr (!S::ROWS) v = *reinterpret_cast<const float4 *>(s + c + i);
                             float2 &lo = sum[(c + i) / 2], &hi = sum[(c + i) / 2 + 1];
                             lo = fma2(make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), make_float2(v.x, v.y), lo);
                             hi = fma2(make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3])), make_float2(v.z, v.w), hi);
                         }
                     };
-                    if constexpr (S::COLS == W) {
-                        uint32_t r[W];
-                        tmem_load(from, r);
-                        tmem_wait(r);
-                        give_back();
-                        add(r, 0);
+                    if constexpr (S::PER_SM == 2) {
+#pragma unroll
+                        for (int c = 0; c < S::COLS; c += W) {
+                            uint32_t r[W];
+                            tmem_load(from + c, r);
+                            tmem_wait(r);
+                            if (c + W == S::COLS) give_back();
+                            add(r, c);
+                        }
                     } else {                                // two loads under way at a time
                         uint32_t r[2][W];
                         tmem_load(from, r[0]);
@@ -444,13 +492,14 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
                     if (++acc == S::ACCS) acc = 0, acc_phase ^= 1;
                 }
             }
-            if constexpr (CG == 2) {
-                const int token = 128 * (int)rank + 32 * quarter, n0 = 256 * t.n + column0;
-                if (ok && token < t.rows && n0 < a.N) put_rows(a, t.row0 + token, min(32, t.rows - token), n0, sum, lane, own_bytes);
-            } else if (splits > 1) {            // to be joined below; the ring is not needed any more
-                float *mine = reinterpret_cast<float *>(smem) + column0 * 128 + row;
+            if (CG == 1 && splits > 1) {        // to be joined below, token by token; the ring is not needed any more
+                float *mine = reinterpret_cast<float *>(smem);
 #pragma unroll
-                for (int i = 0; i < S::COLS; ++i) mine[i * 128] = i & 1 ? sum[i / 2].y : sum[i / 2].x;
+                for (int i = 0; i < S::COLS; ++i)
+                    mine[S::ROWS ? row * JOIN_ROW + column0 + i : (column0 + i) * JOIN_ROW + row] = i & 1 ? sum[i / 2].y : sum[i / 2].x;
+            } else if constexpr (S::ROWS) {
+                const int token = own_row - lane, n0 = NW * t.n + column0;
+                if (ok && token < t.rows && n0 < a.N) put_rows<S::COLS>(a, t.row0 + token, min(32, t.rows - token), n0, sum, lane, own_bytes);
             } else if (ok && 128 * t.n + row < a.N) {
 #pragma unroll
                 for (int i = 0; i < S::COLS; ++i)
@@ -469,28 +518,9 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT>::PER_SM) k_fp8(const __
         if (cluster < items && warp >= FIRST_EPI) {
             int e = 0;
             const Tile t = tile_of<NT>(a, ends, first, cluster, e);
-            // a warp to a token's 128 outputs; the loads of all blocks are under way before the first is added
-            for (int c = NT / splits * (int)rank + warp - FIRST_EPI; c < NT / splits * ((int)rank + 1); c += EPI_WARPS) {
-                if (c >= t.rows) break;
-                float v[MAX_SPLIT][4];
-#pragma unroll
-                for (int r = 0; r < MAX_SPLIT; ++r)
-                    if (r < splits) {
-                        const uint32_t at = in_block(smem_u32(smem) + (c * 128 + lane) * 4, r);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][i]) : "r"(at + 128 * i) : "memory");
-                    }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float sum = v[0][i];
-#pragma unroll
-                    for (int r = 1; r < MAX_SPLIT; ++r)
-                        if (r < splits) sum += v[r][i];
-                    const int n = 128 * t.n + 32 * i + lane;
-                    if (n < a.N) put(a, t.row0 + c, n, sum);
-                }
-            }
+            if (splits == 2) join<NT, NW, 2>(a, t, smem_u32(smem), (int)rank, warp - FIRST_EPI, lane);
+            if (splits == 4) join<NT, NW, 4>(a, t, smem_u32(smem), (int)rank, warp - FIRST_EPI, lane);
+            if (splits == 8) join<NT, NW, 8>(a, t, smem_u32(smem), (int)rank, warp - FIRST_EPI, lane);
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -530,18 +560,19 @@ bool encode(CUtensorMap *map, const uint8_t *p, long long cols, long long rows, 
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, int NT>
+template <int CG, int NT, int NW>
 int launch(const Fp8Product &p, int splits, long long most_tiles, int sms, cudaStream_t s) {
-    using S = Shape<CG, NT>;
+    using S = Shape<CG, NT, NW>;
     static std::atomic<unsigned long long> done;
-    const void *kernel = reinterpret_cast<const void *>(k_fp8<CG, NT>);
+    const void *kernel = reinterpret_cast<const void *>(k_fp8<CG, NT, NW>);
     const int rc = block_allow_smem(kernel, S::smem(1024), &done);
     if (rc != CCDC_OK) return rc;
     Args a;
-    if (!encode(&a.x, p.x, p.K, p.M, p.ldx, 1, 0, NT / CG) || !encode(&a.w, p.w, p.K, p.N, p.ldw, p.experts, p.w_expert, 128)) return CCDC_ECUDA;
+    if (!encode(&a.x, p.x, p.K, p.M, p.ldx, 1, 0, NT / CG) ||
+        !encode(&a.w, p.w, p.K, p.N, p.ldw, p.experts, p.w_expert, NW / CG)) return CCDC_ECUDA;
     a.xs = p.xs, a.ws = p.ws, a.xs_row = p.xs_row, a.xs_col = p.xs_col, a.ldy = p.ldy, a.offsets = p.offsets, a.y = p.y;
     a.M = (int)p.M, a.N = (int)p.N, a.kb = (int)((p.K + 127) / 128), a.nb = (int)((p.N + 127) / 128), a.experts = p.experts;
-    a.y_type = p.y_type, a.splits = splits, a.tiles_n = (a.nb + CG - 1) / CG;
+    a.y_type = p.y_type, a.splits = splits, a.tiles_n = (int)((p.N + NW - 1) / NW);
     const int per = CG == 2 ? 2 : splits;
     cudaLaunchConfig_t cfg = {};
     // a cluster that cuts k takes one tile
@@ -553,7 +584,7 @@ int launch(const Fp8Product &p, int splits, long long most_tiles, int sms, cudaS
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = per, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
     cfg.attrs = at, cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_fp8<CG, NT>, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_fp8<CG, NT, NW>, a);
     if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
     ccdc_internal_count_launch();
     return CCDC_OK;
@@ -569,14 +600,32 @@ int fp8_mma_launch(const Fp8Product &p, int sms, cudaStream_t s) {
         return (p.offsets ? p.M / nt + std::min<long long>(p.experts + 1, p.M) : (p.M + nt - 1) / nt) * rows_n;
     };
     if (most(16, nb) > 0x7FFFFFFF) return CCDC_ESIZE;
-    if (each > 128) return launch<2, 256>(p, 1, most(256, (nb + 1) / 2), sms, s);
-    const int nt = each <= 8 ? 16 : each <= 16 ? 32 : each <= 32 ? 64 : 128;
-    int splits = 1;
-    const int blocks = nt <= 64 ? 2 * sms : sms;
-    while (splits < MAX_SPLIT && most(nt, nb) * splits * 2 <= blocks && 2 * splits <= kb) splits *= 2;
-    return nt == 16   ? launch<1, 16>(p, splits, most(16, nb), sms, s)
-           : nt == 32 ? launch<1, 32>(p, splits, most(32, nb), sms, s)
-           : nt == 64 ? launch<1, 64>(p, splits, most(64, nb), sms, s) : launch<1, 128>(p, splits, most(128, nb), sms, s);
+    // k is cut as long as the blocks that run at once are not all taken
+    const auto cuts = [&](long long tiles, int blocks) {
+        int splits = 1;
+        while (splits < MAX_SPLIT && tiles * splits * 2 <= blocks && 2 * splits <= kb) splits *= 2;
+        return splits;
+    };
+    if (each > 64) {
+        // A pair's tile does twice the work of a single SM's in the time of a block (0.6 us: the way into an SM, and the turn of
+        // the accumulators), but there have to be enough of them.  Rounds of tiles in units of that time; a tile's start and
+        // end cost about five.  (256 rows, 8192 x 8192: 41 us by pairs, 27 by single SMs with k cut in two; 8192 rows:
+        // 540 by pairs.)
+        const long long wide = (nb + 1) / 2, single = most(128, wide);
+        const int splits = cuts(single, sms);
+        const auto rounds = [&](long long nt, int at_once) {
+            const long long tiles = (p.offsets ? p.M / nt + (p.experts + 1) / 2 : (p.M + nt - 1) / nt) * wide;
+            return (std::max(tiles, 1LL) + at_once - 1) / at_once;
+        };
+        if (each > 128 && rounds(256, std::max(1, sms / 2)) * (kb + 5) <= rounds(128, std::max(1, sms / splits)) * (kb / splits + 5) + (splits > 1 ? 5 : 0))
+            return launch<2, 256, 256>(p, 1, most(256, wide), sms, s);
+        return launch<1, 128, 256>(p, splits, single, sms, s);
+    }
+    const int nt = each <= 8 ? 16 : each <= 16 ? 32 : 64;      // room for experts with twice their share
+    const long long tiles = most(nt, nb);
+    const int splits = cuts(tiles, 2 * sms);
+    return nt == 16   ? launch<1, 16, 128>(p, splits, tiles, sms, s)
+           : nt == 32 ? launch<1, 32, 128>(p, splits, tiles, sms, s) : launch<1, 64, 128>(p, splits, tiles, sms, s);
 }
 
 int fp8_mma_status(int *failed) {
