@@ -4,15 +4,22 @@
 //     t_j  = softmax(v / T) over the slots that are there, or exp(v_j / T - lse) with the whole teacher's lse
 //     loss = sum_j t_j (log t_j - log s_id(j)),  s = softmax(z / T)
 //     dz   = dloss / T (P s - t),  P = sum_j t_j
-// Reading z is all the work: a block takes a row, each thread keeps a running maximum and sum, and a second walk over
-// the same row (which L2 still holds) writes the gradient.  The k terms are computed in 64 bits.
+// Reading z and writing dz is all the work.  A row belongs to one block or to the blocks of a cluster, which keep it in shared
+// memory between the walk for maximum and sum and the walk that writes the gradient: z is read from memory once.  Parts are
+// small enough for several blocks an SM, so that one row's loads run under another's stores.  Each thread copies 16-byte pieces
+// asynchronously and reads only its own, so nothing waits but for them; the blocks of a cluster exchange their maxima and sums.
+// Exponentials are the next bound (two for each element).  The k terms are computed in 64 bits.
 #include "ccdc_block.h"
 
 #include <algorithm>
 
 namespace {
 
-constexpr int MAX_TOP = 1024;
+constexpr int MAX_TOP = 1024, MAX_CLUSTER = 8;
+constexpr int GROUPS = 4;                   // of copies that are waited for one after the other
+constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 128 threads take; more take 512
+constexpr int PART = 64 << 10;              // bytes of a part that leave room for three blocks an SM
+constexpr int MOST_PART = 200 << 10;
 
 struct DistillArgs {
     long long M, V, ldz, lddz;
@@ -24,6 +31,7 @@ struct DistillArgs {
     void *dz;
     double inv_t;
     float scale;                // log2(e) / T
+    int part_pieces;            // room of a block, in pieces of 16 bytes
 };
 
 template <class T, int N>
@@ -31,15 +39,54 @@ struct alignas(sizeof(T) * N) Pack {
     T v[N];
 };
 
-// exp of z / T above the maximum's; 16-bit logits by the approximate exponential (2^-22), which their rounding hides
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// 16-bit logits by the approximate exponential (2^-22), which their rounding hides
 template <class T>
-__device__ __forceinline__ float above(float z, float top, float scale) {
-    const float d = (z - top) * scale;      // the difference first: no product of a masked row's lowest value overflows
-    if constexpr (sizeof(T) == 4) return exp2f(d);
+__device__ __forceinline__ float power(float x) {
+    if constexpr (sizeof(T) == 4) return exp2f(x);
     float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(d));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
     return e;
 }
+// exp of z / T above the maximum's.  The difference first: no product of a masked row's lowest value overflows.
+template <class T>
+__device__ __forceinline__ float above(float z, float top, float scale) {
+    return power<T>((z - top) * scale);
+}
+template <class T>
+__device__ __forceinline__ float2 above2(float2 z, float top, float scale) {
+    const float2 d = mul2(add2(z, make_float2(-top, -top)), make_float2(scale, scale));
+    return make_float2(power<T>(d.x), power<T>(d.y));
+}
+// the eight (binary32: four) values of a piece of 16 bytes, two by two
+template <class T>
+__device__ __forceinline__ void values_of(const uint4 &v, float2 (&f)[8 / sizeof(T)]) {
+    if constexpr (sizeof(T) == 4) {
+        f[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+        f[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
+    } else {
+        f[0] = unpack2<T>(v.x), f[1] = unpack2<T>(v.y), f[2] = unpack2<T>(v.z), f[3] = unpack2<T>(v.w);
+    }
+}
+template <class T>
+__device__ __forceinline__ uint4 piece_of(const float2 (&f)[8 / sizeof(T)]) {
+    if constexpr (sizeof(T) == 4)
+        return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+    else
+        return make_uint4(pack2<T>(f[0].x, f[0].y), pack2<T>(f[1].x, f[1].y), pack2<T>(f[2].x, f[2].y), pack2<T>(f[3].x, f[3].y));
+}
+
 struct Running {
     float top, sum;
 };
@@ -53,17 +100,17 @@ __device__ __forceinline__ Running join(Running a, Running b, float scale) {
     const float top = fmaxf(a.top, b.top);
     return {top, a.sum * rebase<T>(a.top, top, scale) + b.sum * rebase<T>(b.top, top, scale)};
 }
-template <class T, int COUNT>
-__device__ __forceinline__ void add(Running &r, const float (&f)[COUNT], float scale) {
+template <class T, int PAIRS>
+__device__ __forceinline__ void add(Running &r, const float2 (&f)[PAIRS], float scale) {
     float top = r.top;
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) top = fmaxf(top, f[i]);
+    for (int i = 0; i < PAIRS; ++i) top = fmaxf(top, fmaxf(f[i].x, f[i].y));
     // all -inf so far (or NaN, which fmax leaves out): count from zero, so that -inf adds nothing and NaN stays NaN
     const float from = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
+    float2 sum = above2<T>(f[0], from, scale);
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) sum += above<T>(f[i], from, scale);
-    r.sum = r.sum * rebase<T>(r.top, top, scale) + sum;
+    for (int i = 1; i < PAIRS; ++i) sum = add2(sum, above2<T>(f[i], from, scale));
+    r.sum = r.sum * rebase<T>(r.top, top, scale) + (sum.x + sum.y);
     r.top = top;
 }
 
@@ -91,49 +138,68 @@ __device__ __forceinline__ double block_max(double v, double *part) {
     __syncthreads();
     return s;
 }
+template <int LEFT>
+__device__ __forceinline__ void copies_landed() {       // all but the last LEFT groups of this thread's
+    asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
 
 // LOSS: computes the statistics, writes loss and (where asked) stats.  GRAD: writes dz, from stats without LOSS.
+// A cluster of gridDim.x / M blocks to a row.
 template <class T, bool LOSS, bool GRAD, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_distill(DistillArgs a) {
-    constexpr int N = 16 / sizeof(T), AHEAD = 4;
-    __shared__ int at[MAX_TOP];             // where the teacher's slots point; -1: not there
-    __shared__ double target[MAX_TOP];      // v_j, then t_j
-    __shared__ float chosen[MAX_TOP];       // z there, before dz may overwrite it
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 8) k_distill(DistillArgs a) {
+    constexpr int N = 16 / sizeof(T);       // elements of a piece
+    extern __shared__ uint4 row[];          // this block's pieces, then the teacher's slots
+    double *target = reinterpret_cast<double *>(row + a.part_pieces);       // v_j, then t_j
+    float *chosen = reinterpret_cast<float *>(target + a.k);                // z there, before dz may overwrite it
+    int *at = reinterpret_cast<int *>(chosen + a.k);                        // where the teacher's slots point; -1: not there
     __shared__ double part[THREADS / 32];
-    __shared__ Running runs[THREADS / 32];
+    __shared__ Running runs[THREADS / 32], whole;
     const int tid = threadIdx.x;
-    for (long long m = blockIdx.x; m < a.M; m += gridDim.x) {
-        const T *z = static_cast<const T *>(a.z) + m * a.ldz;
-        // the teacher's side
-        double top = -INFINITY;
-        bool mine = false;
-        for (int j = tid; j < a.k; j += THREADS) {
-            const long long id = a.id_bytes == 8 ? static_cast<const long long *>(a.ids)[m * a.k + j]
-                                                 : static_cast<const int *>(a.ids)[m * a.k + j];
-            const float v = a.values_f32 ? static_cast<const float *>(a.values)[m * a.k + j]
-                                         : to_f32<T>(static_cast<const T *>(a.values)[m * a.k + j]);
-            const bool there = id >= 0 && id < a.V && v != -INFINITY;
-            at[j] = there ? (int)id : -1;
-            target[j] = v;
-            chosen[j] = there ? to_f32<T>(z[id]) : 0.0f;
-            mine = mine || there;
-            if (there) top = fmax(top, (double)v);
+    const unsigned blocks = (unsigned)(gridDim.x / a.M), rank = blockIdx.x % blocks;
+    const long long m = blockIdx.x / blocks;
+    const T *z = static_cast<const T *>(a.z) + m * a.ldz;
+    // The row in pieces from the 16-byte boundary below its start: element i of piece p is z[p N + i - skew].
+    const int skew = (int)(reinterpret_cast<uintptr_t>(z) & 15) / (int)sizeof(T);
+    const long long pieces = (a.V + skew + N - 1) / N, first = pieces * rank / blocks;
+    const int count = (int)(pieces * (rank + 1) / blocks - first);
+    const uint4 *from = reinterpret_cast<const uint4 *>(z - skew) + first;
+    const int each = (count + THREADS - 1) / THREADS, group = (each + GROUPS - 1) / GROUPS;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        for (int j = g * group; j < min(each, (g + 1) * group); ++j)
+            if (tid + j * THREADS < count)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                             ::"r"((uint32_t)__cvta_generic_to_shared(row + tid + j * THREADS)), "l"(from + tid + j * THREADS) : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    // the teacher's side
+    double top = -INFINITY;
+    bool mine = false;
+    for (int j = tid; j < a.k; j += THREADS) {
+        const long long id = a.id_bytes == 8 ? static_cast<const long long *>(a.ids)[m * a.k + j]
+                                             : static_cast<const int *>(a.ids)[m * a.k + j];
+        const float v = a.values_f32 ? static_cast<const float *>(a.values)[m * a.k + j]
+                                     : to_f32<T>(static_cast<const T *>(a.values)[m * a.k + j]);
+        const bool there = id >= 0 && id < a.V && v != -INFINITY;
+        at[j] = there ? (int)id : -1;
+        target[j] = v;
+        chosen[j] = there ? to_f32<T>(z[id]) : 0.0f;
+        mine = mine || there;
+        if (there) top = fmax(top, (double)v);
+    }
+    const bool any = __syncthreads_or(mine);
+    double log_whole = 0.0, P = 0.0, entropy = 0.0;     // entropy: sum of t log t
+    if (any) {
+        if (a.lse) {
+            log_whole = a.lse[m];
+        } else {
+            top = block_max<THREADS>(top, part);
+            double sum = 0.0;
+            for (int j = tid; j < a.k; j += THREADS)
+                if (at[j] >= 0) sum += exp((target[j] - top) * a.inv_t);
+            log_whole = top * a.inv_t + log(block_sum<THREADS>(sum, part));
         }
-        const bool any = __syncthreads_or(mine);
-        double log_whole = 0.0, P = 0.0;
-        if (any) {
-            if (a.lse) {
-                log_whole = a.lse[m];
-            } else {
-                top = block_max<THREADS>(top, part);
-                double sum = 0.0;
-                for (int j = tid; j < a.k; j += THREADS)
-                    if (at[j] >= 0) sum += exp((target[j] - top) * a.inv_t);
-                log_whole = top * a.inv_t + log(block_sum<THREADS>(sum, part));
-            }
-        }
-        // t log t and P
-        double entropy = 0.0;
         for (int j = tid; j < a.k; j += THREADS) {
             double t = 0.0;
             if (at[j] >= 0) {
@@ -144,120 +210,154 @@ __global__ void __launch_bounds__(THREADS) k_distill(DistillArgs a) {
             target[j] = t;
             P += t;
         }
-        P = any ? block_sum<THREADS>(P, part) : 0.0;
-        if (P == 0.0) {                 // a row without targets: padding
-            if (LOSS && tid == 0) {
-                a.loss[m] = 0.0f;
-                if (a.stats) a.stats[m] = make_float2(0.0f, 1.0f);
-            }
-            if (GRAD) {
-                T *dz = static_cast<T *>(a.dz) + m * a.lddz;
-                for (long long i = tid; i < a.V; i += THREADS) dz[i] = from_f32<T>(0.0f);
-            }
-            __syncthreads();
-            continue;
-        }
-        // the row starts anywhere: a head up to a 16-byte boundary, vectors, a tail
-        const int head = (int)min(a.V, (long long)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (long long)sizeof(T));
-        const long long packs = (a.V - head) / N;
-        const int tail = (int)(a.V - head - packs * N);
-        const Pack<T, N> *body = reinterpret_cast<const Pack<T, N> *>(z + head);
-        const long long rim = tid < head ? tid : tid < head + tail ? head + packs * N + (tid - head) : -1;     // head + tail < THREADS
-        Running r = {-INFINITY, 0.0f};
-        if constexpr (LOSS) {
-            if (rim >= 0) {
-                const float f[1] = {to_f32<T>(z[rim])};
+        P = block_sum<THREADS>(P, part);
+    }
+
+    Running r = {-INFINITY, 0.0f};
+    if constexpr (LOSS) {
+        const auto use = [&](int g) {
+            for (int j = g * group; j < min(each, (g + 1) * group); ++j) {
+                const int p = tid + j * THREADS;
+                if (p >= count) break;
+                float2 f[8 / sizeof(T)];
+                values_of<T>(row[p], f);
+                if (first + p == 0 || first + p == pieces - 1) {        // may reach over the row's ends
+                    const long long e = (first + p) * N - skew;
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i) {
+                        if (e + 2 * i < 0 || e + 2 * i >= a.V) f[i].x = -INFINITY;
+                        if (e + 2 * i + 1 < 0 || e + 2 * i + 1 >= a.V) f[i].y = -INFINITY;
+                    }
+                }
                 add<T>(r, f, a.scale);
             }
-            long long i = tid;
-            for (; i + (AHEAD - 1) * THREADS < packs; i += AHEAD * THREADS) {
-                Pack<T, N> v[AHEAD];
+        };
+        copies_landed<3>(), use(0), copies_landed<2>(), use(1), copies_landed<1>(), use(2), copies_landed<0>(), use(3);
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) v[u] = body[i + u * THREADS];
-                float f[AHEAD * N];
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-                    for (int n = 0; n < N; ++n) f[u * N + n] = to_f32<T>(v[u].v[n]);
-                add<T>(r, f, a.scale);
-            }
-            for (; i < packs; i += THREADS) {
-                const Pack<T, N> v = body[i];
-                float f[N];
-#pragma unroll
-                for (int n = 0; n < N; ++n) f[n] = to_f32<T>(v.v[n]);
-                add<T>(r, f, a.scale);
-            }
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2)
-                r = join<T>(r, {__shfl_xor_sync(~0u, r.top, d), __shfl_xor_sync(~0u, r.sum, d)}, a.scale);
-            if ((tid & 31) == 0) runs[tid >> 5] = r;
-            __syncthreads();
-            r = runs[0];
+        for (int d = 1; d < 32; d *= 2)
+            r = join<T>(r, {__shfl_xor_sync(~0u, r.top, d), __shfl_xor_sync(~0u, r.sum, d)}, a.scale);
+        if ((tid & 31) == 0) runs[tid >> 5] = r;
+        __syncthreads();
+        r = runs[0];
 #pragma unroll 1
-            for (int w = 1; w < THREADS / 32; ++w) r = join<T>(r, runs[w], a.scale);
-        } else {
-            const float2 s = a.stats[m];
-            r = {s.x, s.y};
-        }
-        const float from = r.top == -INFINITY ? 0.0f : r.top;
+        for (int w = 1; w < THREADS / 32; ++w) r = join<T>(r, runs[w], a.scale);
+        if (blocks > 1 && tid == 0) whole = r;
+    } else {
+        copies_landed<0>();
+        const float2 s = a.stats[m];
+        r = {s.x, s.y};
+    }
+    if (blocks > 1) {
+        // every block has its sums, and has read what others may overwrite from here on
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if constexpr (LOSS) {
+            r = {-INFINITY, 0.0f};
+            for (unsigned b = 0; b < blocks; ++b) {
+                uint32_t p;
+                Running o;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"((uint32_t)__cvta_generic_to_shared(&whole)), "r"(b));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(o.top), "=f"(o.sum) : "r"(p) : "memory");
+                r = b ? join<T>(r, o, a.scale) : o;
+            }
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // waited for at the end
+        }
+    }
+    const float base = r.top == -INFINITY ? 0.0f : r.top;
+    const bool empty = P == 0.0;                // a row without targets: padding
+    if constexpr (LOSS) {
+        if (rank == 0) {
             const double log_sum = log((double)r.sum);
             double cross = 0.0;
-            for (int j = tid; j < a.k; j += THREADS)
-                if (at[j] >= 0 && target[j] != 0.0)
-                    cross += target[j] * (((double)chosen[j] - (double)from) * (double)a.scale * 0.6931471805599453 - log_sum);
+            if (!empty)
+                for (int j = tid; j < a.k; j += THREADS)
+                    if (at[j] >= 0 && target[j] != 0.0)
+                        cross += target[j] * (((double)chosen[j] - (double)base) * (double)a.scale * 0.6931471805599453 - log_sum);
             const double loss = block_sum<THREADS>(entropy - cross, part);
             if (tid == 0) {
-                a.loss[m] = (float)loss;
+                a.loss[m] = empty ? 0.0f : (float)loss;
                 if (a.stats) a.stats[m] = make_float2(r.top, r.sum);
             }
         }
-        if constexpr (GRAD) {
-            const float c = a.dloss[m] * (float)a.inv_t, cs = (float)((double)a.dloss[m] * a.inv_t * P / (double)r.sum);
-            T *dz = static_cast<T *>(a.dz) + m * a.lddz;
-            if (rim >= 0) dz[rim] = from_f32<T>(cs * above<T>(to_f32<T>(z[rim]), from, a.scale));
-            const bool alike = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
-            Pack<T, N> *out = reinterpret_cast<Pack<T, N> *>(dz + head);
-#pragma unroll 4
-            for (long long i = tid; i < packs; i += THREADS) {
-                Pack<T, N> v = body[i];
+    }
+    if constexpr (GRAD) {
+        const float c = a.dloss[m] * (float)a.inv_t, cs = (float)((double)a.dloss[m] * a.inv_t * P / (double)r.sum);
+        T *dz = static_cast<T *>(a.dz) + m * a.lddz;
+        const int out_skew = (int)(reinterpret_cast<uintptr_t>(dz) & 15) / (int)sizeof(T);
+        const auto gradient = [&](uint4 v) {
+            float2 f[8 / sizeof(T)];
+            values_of<T>(v, f);
 #pragma unroll
-                for (int n = 0; n < N; ++n) v.v[n] = from_f32<T>(cs * above<T>(to_f32<T>(v.v[n]), from, a.scale));
-                if (alike)
-                    out[i] = v;
-                else
+            for (int i = 0; i < N / 2; ++i) f[i] = empty ? make_float2(0.0f, 0.0f) : mul2(above2<T>(f[i], base, a.scale), make_float2(cs, cs));
+            return piece_of<T>(f);
+        };
+        for (int j = 0; j < each; ++j) {
+            const int p = tid + j * THREADS;
+            if (p >= count) break;
+            const long long e = (first + p) * N - skew;
+            const uint4 v = gradient(row[p]);
+            if (skew == out_skew && e >= 0 && e + N <= a.V) {
+                *reinterpret_cast<uint4 *>(dz + e) = v;
+            } else {
+                const Pack<T, N> w = *reinterpret_cast<const Pack<T, N> *>(&v);
 #pragma unroll
-                    for (int n = 0; n < N; ++n) dz[head + i * N + n] = v.v[n];
-            }
-            __syncthreads();            // the targets' elements are written again
-            for (int j = tid; j < a.k; j += THREADS) {
-                if (at[j] < 0) continue;
-                double t = 0.0;         // the slots that name this element add up; the first of them writes it
-                bool first = true;
-                for (int i = 0; i < a.k; ++i)
-                    if (at[i] == at[j]) {
-                        if (i < j) first = false;
-                        t += target[i];
-                    }
-                if (first) dz[at[j]] = from_f32<T>(fmaf(-c, (float)t, cs * above<T>(chosen[j], from, a.scale)));
+                for (int i = 0; i < N; ++i)
+                    if (e + i >= 0 && e + i < a.V) dz[e + i] = w.v[i];
             }
         }
-        __syncthreads();
+        __syncthreads();            // the targets' elements are written again, by the block that wrote them
+        const long long e0 = first * N - skew, e1 = (first + count) * N - skew;
+        if (!empty)
+            for (int j = tid; j < a.k; j += THREADS) {
+                if (at[j] < 0 || at[j] < e0 || at[j] >= e1) continue;
+                double t = 0.0;         // the slots that name this element add up; the first of them writes it
+                bool lead = true;
+                for (int i = 0; i < a.k; ++i)
+                    if (at[i] == at[j]) {
+                        if (i < j) lead = false;
+                        t += target[i];
+                    }
+                if (lead) dz[at[j]] = from_f32<T>(fmaf(-c, (float)t, cs * above<T>(chosen[j], base, a.scale)));
+            }
     }
+    __syncwarp();
+    if (LOSS && blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // `whole` has been read
 }
 
+template <class T, bool LOSS, bool GRAD, int THREADS>
+int launch(DistillArgs &a, int blocks, cudaStream_t s) {
+    auto *kernel = k_distill<T, LOSS, GRAD, THREADS>;
+    static std::atomic<unsigned long long> done;
+    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), MOST_PART + 16 * (MAX_TOP + 2), &done);
+    if (rc != CCDC_OK) return rc;
+    a.part_pieces = (int)((a.V * (long long)sizeof(T) + 30) / 16 / blocks) + 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.M * blocks)), cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = 16 * ((size_t)a.part_pieces + a.k), cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = blocks, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    cfg.attrs = at, cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    return block_launch_status();
+}
 template <class T, bool LOSS, bool GRAD>
-int launch(const DistillArgs &a, cudaStream_t s) {
+int launch(DistillArgs &a, cudaStream_t s) {
     int rc;
     const int sms = block_sm_count(&rc);
     if (rc != CCDC_OK) return rc;
-    constexpr int THREADS = 512;
-    k_distill<T, LOSS, GRAD, THREADS><<<(unsigned)std::min<long long>(a.M, 2LL * sms), THREADS, 0, s>>>(a);
-    return block_launch_status();
+    // parts that leave room for several blocks an SM; smaller ones where rows are few
+    const long long bytes = a.V * (long long)sizeof(T);
+    int blocks = 1;
+    while (blocks < MAX_CLUSTER && (bytes > (long long)PART * blocks || (a.M * blocks * 2 <= sms && bytes > (long long)SMALL_PART * blocks)))
+        blocks *= 2;
+    if (bytes > (long long)MOST_PART * blocks || a.M * blocks > 0x7FFFFFFF) return CCDC_ESIZE;
+    return bytes <= (long long)SMALL_PART * blocks ? launch<T, LOSS, GRAD, 128>(a, blocks, s) : launch<T, LOSS, GRAD, 512>(a, blocks, s);
 }
 template <bool LOSS, bool GRAD>
-int by_type(const DistillArgs &a, int dtype, cudaStream_t s) {
+int by_type(DistillArgs &a, int dtype, cudaStream_t s) {
     return dtype == CCDC_F32    ? launch<float, LOSS, GRAD>(a, s)
            : dtype == CCDC_BF16 ? launch<bf16, LOSS, GRAD>(a, s) : launch<fp16, LOSS, GRAD>(a, s);
 }
@@ -272,7 +372,7 @@ int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits,
     if (M < 0 || V < 1 || k < 1 || !is_float_type(dtype) || (value_dtype != dtype && value_dtype != CCDC_F32) ||
         (id_bytes != 4 && id_bytes != 8) || !(temperature >= 1e-6f && temperature <= 1e6f))
         return CCDC_EINVAL;
-    if (V > 0x7FFFFFFF || k > MAX_TOP) return CCDC_ESIZE;
+    if (V * type_bytes(dtype) > MOST_PART * MAX_CLUSTER || V > 0x7FFFFFFF || k > MAX_TOP) return CCDC_ESIZE;
     if (M == 0) return CCDC_OK;
     if (!logits || ldz < V || !ids || !aligned_to(ids, id_bytes) || !values || !aligned_to(stats, 8)) return CCDC_EINVAL;
     if (dlogits ? !dloss || lddz < V || (!loss && !stats) : !loss) return CCDC_EINVAL;

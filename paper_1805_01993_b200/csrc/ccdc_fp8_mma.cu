@@ -27,6 +27,7 @@ namespace {
 
 constexpr int EPI_WARPS = 8, FIRST_EPI = 4, THREADS = 32 * (FIRST_EPI + EPI_WARPS);
 constexpr int RING_BYTES = 192 * 1024;
+constexpr int JOIN_PAD = 4;                 // words between tokens that wait to be joined, so that writes meet no conflicts
 constexpr int MAX_SPLIT = 8;                // a power of two, as all splits
 #ifndef CCDC_FP8_WAIT_LIMIT
 #define CCDC_FP8_WAIT_LIMIT (1 << 20)       // polls of a barrier (each may sleep) before a wait has failed
@@ -249,6 +250,23 @@ struct Shape {
     static constexpr int smem(int experts) { return FIXED + 2 * 4 * (experts + 3); }
 };
 
+// four neighbouring outputs of a token
+__device__ __forceinline__ void put4(const Args &a, int token, int n, const float (&v)[4]) {
+    const long long at = token * a.ldy + n;
+    const int size = a.y_type == CCDC_F32 ? 4 : 2;
+    if (n + 4 <= a.N && (reinterpret_cast<uintptr_t>(a.y) + at * size) % (4 * size) == 0) {
+        if (a.y_type == CCDC_F32)
+            *reinterpret_cast<float4 *>(static_cast<float *>(a.y) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+            *reinterpret_cast<uint2 *>(static_cast<bf16 *>(a.y) + at) =
+                a.y_type == CCDC_BF16 ? make_uint2(pack2<bf16>(v[0], v[1]), pack2<bf16>(v[2], v[3]))
+                                      : make_uint2(pack2<fp16>(v[0], v[1]), pack2<fp16>(v[2], v[3]));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n + i < a.N) put(a, token, n + i, v[i]);
+}
 // This block's share of the tokens, each output added over the blocks in the order of k.  A warp to 128 outputs of a token, and
 // to as many tokens at a time as keep the loads of eight sums under way.
 template <int NT, int NW, int SPLITS>
@@ -259,26 +277,21 @@ __device__ __forceinline__ void join(const Args &a, const Tile &t, uint32_t smem
         float v[AT_ONCE][SPLITS][4];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-            const int u = min(u0 + j * EPI_WARPS, UNITS - 1), token = SHARE * rank + u / (NW / 128), n = 128 * (u % (NW / 128)) + lane;
+            const int u = min(u0 + j * EPI_WARPS, UNITS - 1), token = SHARE * rank + u / (NW / 128), n = 128 * (u % (NW / 128)) + 4 * lane;
 #pragma unroll
-            for (int r = 0; r < SPLITS; ++r) {
-                const uint32_t from = in_block(smem + 4 * (token * (NW + 1) + n), r);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[j][r][i]) : "r"(from + 128 * i) : "memory");
-            }
+            for (int r = 0; r < SPLITS; ++r)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(v[j][r][0]), "=f"(v[j][r][1]), "=f"(v[j][r][2]), "=f"(v[j][r][3])
+                             : "r"(in_block(smem + 4 * (token * (NW + JOIN_PAD) + n), r)) : "memory");
         }
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
             const int u = u0 + j * EPI_WARPS, token = SHARE * rank + u / (NW / 128);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float sum = v[j][0][i];
+            for (int r = 1; r < SPLITS; ++r)
 #pragma unroll
-                for (int r = 1; r < SPLITS; ++r) sum += v[j][r][i];
-                const int n = NW * t.n + 128 * (u % (NW / 128)) + 32 * i + lane;
-                if (u < UNITS && token < t.rows && n < a.N) put(a, t.row0 + token, n, sum);
-            }
+                for (int i = 0; i < 4; ++i) v[j][0][i] += v[j][r][i];
+            if (u < UNITS && token < t.rows) put4(a, t.row0 + token, NW * t.n + 128 * (u % (NW / 128)) + 4 * lane, v[j][0]);
         }
     }
 }
@@ -287,7 +300,7 @@ template <int CG, int NT, int NW>
 __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(const __grid_constant__ Args a) {
     using S = Shape<CG, NT, NW>;
     constexpr int W = S::COLS == 32 ? 16 : S::COLS < 32 ? S::COLS : 32;     // columns of one load from tensor memory
-    constexpr int JOIN_ROW = NW + 1;    // words of a token that waits to be joined, so that neither way to write them meets conflicts
+    constexpr int JOIN_ROW = NW + JOIN_PAD;
     constexpr uint32_t TMEM_COLUMNS = S::ACCS * S::N;
     extern __shared__ char smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -318,6 +331,10 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
                          ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLUMNS) : "memory");
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
+    }
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&a.x) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&a.w) : "memory");
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -495,8 +512,15 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
             if (CG == 1 && splits > 1) {        // to be joined below, token by token; the ring is not needed any more
                 float *mine = reinterpret_cast<float *>(smem);
 #pragma unroll
-                for (int i = 0; i < S::COLS; ++i)
-                    mine[S::ROWS ? row * JOIN_ROW + column0 + i : (column0 + i) * JOIN_ROW + row] = i & 1 ? sum[i / 2].y : sum[i / 2].x;
+                for (int i = 0; i < S::COLS; i += 4) {
+                    const float4 v = make_float4(sum[i / 2].x, sum[i / 2].y, sum[i / 2 + 1].x, sum[i / 2 + 1].y);
+                    if constexpr (S::ROWS) {
+                        *reinterpret_cast<float4 *>(mine + row * JOIN_ROW + column0 + i) = v;
+                    } else {
+                        mine += i ? 4 * JOIN_ROW : column0 * JOIN_ROW + row;
+                        mine[0] = v.x, mine[JOIN_ROW] = v.y, mine[2 * JOIN_ROW] = v.z, mine[3 * JOIN_ROW] = v.w;
+                    }
+                }
             } else if constexpr (S::ROWS) {
                 const int token = own_row - lane, n0 = NW * t.n + column0;
                 if (ok && token < t.rows && n0 < a.N) put_rows<S::COLS>(a, t.row0 + token, min(32, t.rows - token), n0, sum, lane, own_bytes);
