@@ -8,7 +8,7 @@
 // memory between the walk for maximum and sum and the walk that writes the gradient: z is read from memory once.  Parts are
 // small enough for several blocks an SM, so that one row's loads run under another's stores.  Each thread copies 16-byte pieces
 // asynchronously and reads only its own, so nothing waits but for them; the blocks of a cluster exchange their maxima and sums.
-// Exponentials are the next bound (two for each element).  The k terms are computed in 64 bits.
+// The last warp of a block computes the k terms meanwhile, in 64 bits.  Exponentials are the next bound (two for each element).
 #include "ccdc_block.h"
 
 #include <algorithm>
@@ -16,10 +16,11 @@
 namespace {
 
 constexpr int MAX_TOP = 1024, MAX_CLUSTER = 8;
+constexpr int AHEAD = 4;                    // slots a lane
 constexpr int GROUPS = 4;                   // of copies that are waited for one after the other
-constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 128 threads take; more take 512
+constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 64 threads take; more take 256
 constexpr int PART = 64 << 10;              // bytes of a part that leave room for three blocks an SM
-constexpr int MOST_PART = 200 << 10;
+constexpr int MOST_PART = 192 << 10;
 
 struct DistillArgs {
     long long M, V, ldz, lddz;
@@ -31,7 +32,7 @@ struct DistillArgs {
     void *dz;
     double inv_t;
     float scale;                // log2(e) / T
-    int part_pieces;            // room of a block, in pieces of 16 bytes
+    int part_pieces, table;     // room of a block, in pieces of 16 bytes; of the table of ids
 };
 
 template <class T, int N>
@@ -98,7 +99,8 @@ __device__ __forceinline__ float rebase(float from, float to, float scale) {
 template <class T>
 __device__ __forceinline__ Running join(Running a, Running b, float scale) {
     const float top = fmaxf(a.top, b.top);
-    return {top, a.sum * rebase<T>(a.top, top, scale) + b.sum * rebase<T>(b.top, top, scale)};
+    // the same bits for (a, b) and (b, a): every lane of an exchange gets one result
+    return {top, __fadd_rn(__fmul_rn(a.sum, rebase<T>(a.top, top, scale)), __fmul_rn(b.sum, rebase<T>(b.top, top, scale)))};
 }
 template <class T, int PAIRS>
 __device__ __forceinline__ void add(Running &r, const float2 (&f)[PAIRS], float scale) {
@@ -114,47 +116,114 @@ __device__ __forceinline__ void add(Running &r, const float2 (&f)[PAIRS], float 
     r.top = top;
 }
 
-template <int THREADS>
-__device__ __forceinline__ double block_sum(double v, double *part) {
+__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int d = 16; d; d /= 2) v += __shfl_xor_sync(~0u, v, d);
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double s = 0.0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) s += part[w];
-    __syncthreads();
-    return s;
-}
-template <int THREADS>
-__device__ __forceinline__ double block_max(double v, double *part) {
-#pragma unroll
-    for (int d = 16; d; d /= 2) v = fmax(v, __shfl_xor_sync(~0u, v, d));
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    double s = part[0];
-#pragma unroll
-    for (int w = 1; w < THREADS / 32; ++w) s = fmax(s, part[w]);
-    __syncthreads();
-    return s;
+    return v;
 }
 template <int LEFT>
 __device__ __forceinline__ void copies_landed() {       // all but the last LEFT groups of this thread's
     asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
+// What the k slots come to, in shared memory
+struct Slots {
+    double *target;             // exponentials, then t_j
+    float *value, *chosen;      // v_j; z at the slot's id, before dz may overwrite it
+    int *at;                    // where the slot points; -1: not there
+    int *seen;                  // a table of the ids
+    int mask;                   // its length - 1, a power of two of at least 2 k - 1
+};
+inline int table_length(int k) {
+    int n = 32;
+    while (n < 2 * k) n *= 2;
+    return n;
+}
+struct Teacher {
+    double P, entropy;          // sum of t; of t log t
+    int twice;                  // whether an id comes more than once
+};
+// by one warp
+template <class T>
+__device__ __forceinline__ Teacher teacher_side(const DistillArgs &a, const T *z, long long m, const Slots &s, int lane) {
+    for (int i = lane; i <= s.mask; i += 32) s.seen[i] = -1;
+    __syncwarp();
+    float top = -INFINITY;
+    bool twice = false, any = false;
+    for (int j0 = lane; j0 < a.k; j0 += 32 * AHEAD) {       // the loads of AHEAD slots are under way together
+        long long id[AHEAD];
+        float v[AHEAD], c[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int j = j0 + 32 * u;
+            const long long from = m * a.k + (j < a.k ? j : j0);
+            id[u] = a.id_bytes == 8 ? static_cast<const long long *>(a.ids)[from] : static_cast<const int *>(a.ids)[from];
+            v[u] = a.values_f32 ? static_cast<const float *>(a.values)[from] : to_f32<T>(static_cast<const T *>(a.values)[from]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (id[u] < 0 || id[u] >= a.V || v[u] == -INFINITY) id[u] = -1;
+            c[u] = to_f32<T>(z[max(id[u], 0LL)]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int j = j0 + 32 * u;
+            if (j >= a.k) break;
+            s.at[j] = (int)id[u], s.value[j] = v[u], s.chosen[j] = c[u];
+            if (id[u] < 0) continue;
+            any = true;
+            top = fmaxf(top, v[u]);
+            for (uint32_t h = (uint32_t)id[u] * 2654435761u >> 7;; ++h) {       // ends: the table has room for twice the slots
+                const int there_already = atomicCAS(&s.seen[h & s.mask], -1, (int)id[u]);
+                twice = twice || there_already == (int)id[u];
+                if (there_already == -1 || there_already == (int)id[u]) break;
+            }
+        }
+    }
+    Teacher r = {0.0, 0.0, __any_sync(~0u, twice)};
+    if (!__any_sync(~0u, any)) return r;
+    // t = e / whole with e = exp(v / T - shift)
+    double shift, whole = 1.0;
+    if (a.lse) {
+        shift = a.lse[m];
+    } else {
+#pragma unroll
+        for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        shift = (double)top * a.inv_t;
+    }
+    double sum = 0.0;
+    for (int j = lane; j < a.k; j += 32) {
+        const double e = s.at[j] >= 0 ? exp((double)s.value[j] * a.inv_t - shift) : 0.0;
+        s.target[j] = e;
+        sum += e;
+    }
+    sum = warp_sum(sum);
+    if (!a.lse) whole = sum;
+    const double log_whole = a.lse ? 0.0 : log(whole), scale = 1.0 / whole;
+    for (int j = lane; j < a.k; j += 32) {
+        const double t = s.target[j] * scale;
+        s.target[j] = t;
+        if (t != 0.0) r.entropy += t * ((double)s.value[j] * a.inv_t - shift - log_whole);
+    }
+    r.P = sum * scale, r.entropy = warp_sum(r.entropy);
+    return r;
+}
+
 // LOSS: computes the statistics, writes loss and (where asked) stats.  GRAD: writes dz, from stats without LOSS.
-// A cluster of gridDim.x / M blocks to a row.
+// A cluster of gridDim.x / M blocks to a row; THREADS that walk the row and one warp for the teacher's side.
 template <class T, bool LOSS, bool GRAD, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 8) k_distill(DistillArgs a) {
+__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 10) k_distill(DistillArgs a) {
     constexpr int N = 16 / sizeof(T);       // elements of a piece
-    extern __shared__ uint4 row[];          // this block's pieces, then the teacher's slots
-    double *target = reinterpret_cast<double *>(row + a.part_pieces);       // v_j, then t_j
-    float *chosen = reinterpret_cast<float *>(target + a.k);                // z there, before dz may overwrite it
-    int *at = reinterpret_cast<int *>(chosen + a.k);                        // where the teacher's slots point; -1: not there
-    __shared__ double part[THREADS / 32];
+    extern __shared__ uint4 row[];          // this block's pieces, then the slots
+    Slots slots;
+    slots.target = reinterpret_cast<double *>(row + a.part_pieces);
+    slots.value = reinterpret_cast<float *>(slots.target + a.k), slots.chosen = slots.value + a.k;
+    slots.at = reinterpret_cast<int *>(slots.chosen + a.k);
+    slots.seen = slots.at + a.k, slots.mask = a.table - 1;
     __shared__ Running runs[THREADS / 32], whole;
-    const int tid = threadIdx.x;
+    __shared__ Teacher told;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const bool walks = tid < THREADS;
     const unsigned blocks = (unsigned)(gridDim.x / a.M), rank = blockIdx.x % blocks;
     const long long m = blockIdx.x / blocks;
     const T *z = static_cast<const T *>(a.z) + m * a.ldz;
@@ -162,88 +231,67 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 8) k_distill(Dis
     const int skew = (int)(reinterpret_cast<uintptr_t>(z) & 15) / (int)sizeof(T);
     const long long pieces = (a.V + skew + N - 1) / N, first = pieces * rank / blocks;
     const int count = (int)(pieces * (rank + 1) / blocks - first);
-    const uint4 *from = reinterpret_cast<const uint4 *>(z - skew) + first;
     const int each = (count + THREADS - 1) / THREADS, group = (each + GROUPS - 1) / GROUPS;
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-        for (int j = g * group; j < min(each, (g + 1) * group); ++j)
-            if (tid + j * THREADS < count)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                             ::"r"((uint32_t)__cvta_generic_to_shared(row + tid + j * THREADS)), "l"(from + tid + j * THREADS) : "memory");
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-
-    // the teacher's side
-    double top = -INFINITY;
-    bool mine = false;
-    for (int j = tid; j < a.k; j += THREADS) {
-        const long long id = a.id_bytes == 8 ? static_cast<const long long *>(a.ids)[m * a.k + j]
-                                             : static_cast<const int *>(a.ids)[m * a.k + j];
-        const float v = a.values_f32 ? static_cast<const float *>(a.values)[m * a.k + j]
-                                     : to_f32<T>(static_cast<const T *>(a.values)[m * a.k + j]);
-        const bool there = id >= 0 && id < a.V && v != -INFINITY;
-        at[j] = there ? (int)id : -1;
-        target[j] = v;
-        chosen[j] = there ? to_f32<T>(z[id]) : 0.0f;
-        mine = mine || there;
-        if (there) top = fmax(top, (double)v);
-    }
-    const bool any = __syncthreads_or(mine);
-    double log_whole = 0.0, P = 0.0, entropy = 0.0;     // entropy: sum of t log t
-    if (any) {
-        if (a.lse) {
-            log_whole = a.lse[m];
-        } else {
-            top = block_max<THREADS>(top, part);
-            double sum = 0.0;
-            for (int j = tid; j < a.k; j += THREADS)
-                if (at[j] >= 0) sum += exp((target[j] - top) * a.inv_t);
-            log_whole = top * a.inv_t + log(block_sum<THREADS>(sum, part));
-        }
-        for (int j = tid; j < a.k; j += THREADS) {
-            double t = 0.0;
-            if (at[j] >= 0) {
-                const double log_t = target[j] * a.inv_t - log_whole;
-                t = exp(log_t);
-                if (t != 0.0) entropy += t * log_t;
-            }
-            target[j] = t;
-            P += t;
-        }
-        P = block_sum<THREADS>(P, part);
-    }
 
     Running r = {-INFINITY, 0.0f};
-    if constexpr (LOSS) {
-        const auto use = [&](int g) {
-            for (int j = g * group; j < min(each, (g + 1) * group); ++j) {
-                const int p = tid + j * THREADS;
-                if (p >= count) break;
-                float2 f[8 / sizeof(T)];
-                values_of<T>(row[p], f);
-                if (first + p == 0 || first + p == pieces - 1) {        // may reach over the row's ends
-                    const long long e = (first + p) * N - skew;
+    if (walks) {
+        const uint4 *from = reinterpret_cast<const uint4 *>(z - skew) + first;
 #pragma unroll
-                    for (int i = 0; i < N / 2; ++i) {
-                        if (e + 2 * i < 0 || e + 2 * i >= a.V) f[i].x = -INFINITY;
-                        if (e + 2 * i + 1 < 0 || e + 2 * i + 1 >= a.V) f[i].y = -INFINITY;
+        for (int g = 0; g < GROUPS; ++g) {
+            for (int j = g * group; j < min(each, (g + 1) * group); ++j)
+                if (tid + j * THREADS < count)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                                 ::"r"((uint32_t)__cvta_generic_to_shared(row + tid + j * THREADS)), "l"(from + tid + j * THREADS) : "memory");
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+        if constexpr (LOSS) {
+            constexpr int PAIRS = N / 2;
+            // two pieces at a time, one rise of the maximum for both
+            const auto use = [&](int g) {
+                for (int j = g * group; j < min(each, (g + 1) * group); j += 2) {
+                    float2 f[2 * PAIRS];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int p = tid + (j + u) * THREADS;
+                        float2(&h)[PAIRS] = *reinterpret_cast<float2(*)[PAIRS]>(f + u * PAIRS);
+                        if (p >= count || j + u >= min(each, (g + 1) * group)) {
+#pragma unroll
+                            for (int i = 0; i < PAIRS; ++i) h[i] = make_float2(-INFINITY, -INFINITY);
+                            continue;
+                        }
+                        values_of<T>(row[p], h);
+                        if (first + p == 0 || first + p == pieces - 1) {        // may reach over the row's ends
+                            const long long e = (first + p) * N - skew;
+#pragma unroll
+                            for (int i = 0; i < PAIRS; ++i) {
+                                if (e + 2 * i < 0 || e + 2 * i >= a.V) h[i].x = -INFINITY;
+                                if (e + 2 * i + 1 < 0 || e + 2 * i + 1 >= a.V) h[i].y = -INFINITY;
+                            }
+                        }
                     }
+                    add<T>(r, f, a.scale);
                 }
-                add<T>(r, f, a.scale);
-            }
-        };
-        copies_landed<3>(), use(0), copies_landed<2>(), use(1), copies_landed<1>(), use(2), copies_landed<0>(), use(3);
+            };
+            copies_landed<3>(), use(0), copies_landed<2>(), use(1), copies_landed<1>(), use(2), copies_landed<0>(), use(3);
 #pragma unroll
-        for (int d = 1; d < 32; d *= 2)
+            for (int d = 1; d < 32; d *= 2)
+                r = join<T>(r, {__shfl_xor_sync(~0u, r.top, d), __shfl_xor_sync(~0u, r.sum, d)}, a.scale);
+            if (lane == 0) runs[tid >> 5] = r;
+        } else {
+            copies_landed<0>();
+        }
+    } else {
+        const Teacher t = teacher_side<T>(a, z, m, slots, lane);
+        if (lane == 0) told = t;
+    }
+    __syncthreads();
+    if constexpr (LOSS) {
+        r = runs[lane & (THREADS / 32 - 1)];
+#pragma unroll
+        for (int d = 1; d < THREADS / 32; d *= 2)
             r = join<T>(r, {__shfl_xor_sync(~0u, r.top, d), __shfl_xor_sync(~0u, r.sum, d)}, a.scale);
-        if ((tid & 31) == 0) runs[tid >> 5] = r;
-        __syncthreads();
-        r = runs[0];
-#pragma unroll 1
-        for (int w = 1; w < THREADS / 32; ++w) r = join<T>(r, runs[w], a.scale);
         if (blocks > 1 && tid == 0) whole = r;
     } else {
-        copies_landed<0>();
         const float2 s = a.stats[m];
         r = {s.x, s.y};
     }
@@ -253,7 +301,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 8) k_distill(Dis
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if constexpr (LOSS) {
-            r = {-INFINITY, 0.0f};
             for (unsigned b = 0; b < blocks; ++b) {
                 uint32_t p;
                 Running o;
@@ -265,39 +312,34 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 8) k_distill(Dis
         }
     }
     const float base = r.top == -INFINITY ? 0.0f : r.top;
+    const double P = told.P;
     const bool empty = P == 0.0;                // a row without targets: padding
-    if constexpr (LOSS) {
-        if (rank == 0) {
-            const double log_sum = log((double)r.sum);
-            double cross = 0.0;
-            if (!empty)
-                for (int j = tid; j < a.k; j += THREADS)
-                    if (at[j] >= 0 && target[j] != 0.0)
-                        cross += target[j] * (((double)chosen[j] - (double)base) * (double)a.scale * 0.6931471805599453 - log_sum);
-            const double loss = block_sum<THREADS>(entropy - cross, part);
-            if (tid == 0) {
-                a.loss[m] = empty ? 0.0f : (float)loss;
-                if (a.stats) a.stats[m] = make_float2(r.top, r.sum);
-            }
+    if (LOSS && rank == 0 && !walks) {
+        const double log_sum = log((double)r.sum);
+        double loss = 0.0;
+        for (int j = lane; j < a.k; j += 32)
+            if (slots.at[j] >= 0 && slots.target[j] != 0.0)
+                loss -= slots.target[j] * (((double)slots.chosen[j] - (double)base) * (double)a.scale * 0.6931471805599453 - log_sum);
+        loss = warp_sum(loss) + told.entropy;
+        if (lane == 0) {
+            a.loss[m] = empty ? 0.0f : (float)loss;
+            if (a.stats) a.stats[m] = make_float2(r.top, r.sum);
         }
     }
     if constexpr (GRAD) {
         const float c = a.dloss[m] * (float)a.inv_t, cs = (float)((double)a.dloss[m] * a.inv_t * P / (double)r.sum);
         T *dz = static_cast<T *>(a.dz) + m * a.lddz;
-        const int out_skew = (int)(reinterpret_cast<uintptr_t>(dz) & 15) / (int)sizeof(T);
-        const auto gradient = [&](uint4 v) {
-            float2 f[8 / sizeof(T)];
-            values_of<T>(v, f);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i) f[i] = empty ? make_float2(0.0f, 0.0f) : mul2(above2<T>(f[i], base, a.scale), make_float2(cs, cs));
-            return piece_of<T>(f);
-        };
-        for (int j = 0; j < each; ++j) {
+        const bool alike = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+        for (int j = 0; walks && j < each; ++j) {
             const int p = tid + j * THREADS;
             if (p >= count) break;
             const long long e = (first + p) * N - skew;
-            const uint4 v = gradient(row[p]);
-            if (skew == out_skew && e >= 0 && e + N <= a.V) {
+            float2 f[N / 2];
+            values_of<T>(row[p], f);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) f[i] = empty ? make_float2(0.0f, 0.0f) : mul2(above2<T>(f[i], base, a.scale), make_float2(cs, cs));
+            const uint4 v = piece_of<T>(f);
+            if (alike && e >= 0 && e + N <= a.V) {
                 *reinterpret_cast<uint4 *>(dz + e) = v;
             } else {
                 const Pack<T, N> w = *reinterpret_cast<const Pack<T, N> *>(&v);
@@ -308,18 +350,22 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 3 : 8) k_distill(Dis
         }
         __syncthreads();            // the targets' elements are written again, by the block that wrote them
         const long long e0 = first * N - skew, e1 = (first + count) * N - skew;
-        if (!empty)
-            for (int j = tid; j < a.k; j += THREADS) {
-                if (at[j] < 0 || at[j] < e0 || at[j] >= e1) continue;
-                double t = 0.0;         // the slots that name this element add up; the first of them writes it
-                bool lead = true;
+        const bool twice = told.twice;
+        for (int j = tid; !empty && j < a.k; j += THREADS + 32) {
+            const int id = slots.at[j];
+            if (id < 0 || id < e0 || id >= e1) continue;
+            double t = slots.target[j];
+            bool lead = true;
+            if (twice) {            // the slots that name this element add up; the first of them writes it
+                t = 0.0;
                 for (int i = 0; i < a.k; ++i)
-                    if (at[i] == at[j]) {
+                    if (slots.at[i] == id) {
                         if (i < j) lead = false;
-                        t += target[i];
+                        t += slots.target[i];
                     }
-                if (lead) dz[at[j]] = from_f32<T>(fmaf(-c, (float)t, cs * above<T>(chosen[j], base, a.scale)));
             }
+            if (lead) dz[id] = from_f32<T>(fmaf(-c, (float)t, cs * above<T>(slots.chosen[j], base, a.scale)));
+        }
     }
     __syncwarp();
     if (LOSS && blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // `whole` has been read
@@ -329,12 +375,13 @@ template <class T, bool LOSS, bool GRAD, int THREADS>
 int launch(DistillArgs &a, int blocks, cudaStream_t s) {
     auto *kernel = k_distill<T, LOSS, GRAD, THREADS>;
     static std::atomic<unsigned long long> done;
-    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), MOST_PART + 16 * (MAX_TOP + 2), &done);
+    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), MOST_PART + 32 + 28 * MAX_TOP, &done);
     if (rc != CCDC_OK) return rc;
+    a.table = table_length(a.k);
     a.part_pieces = (int)((a.V * (long long)sizeof(T) + 30) / 16 / blocks) + 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.M * blocks)), cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = 16 * ((size_t)a.part_pieces + a.k), cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(a.M * blocks)), cfg.blockDim = dim3(THREADS + 32);
+    cfg.dynamicSmemBytes = 16 * (size_t)a.part_pieces + 20 * a.k + 4 * a.table, cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = blocks, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
@@ -354,7 +401,7 @@ int launch(DistillArgs &a, cudaStream_t s) {
     while (blocks < MAX_CLUSTER && (bytes > (long long)PART * blocks || (a.M * blocks * 2 <= sms && bytes > (long long)SMALL_PART * blocks)))
         blocks *= 2;
     if (bytes > (long long)MOST_PART * blocks || a.M * blocks > 0x7FFFFFFF) return CCDC_ESIZE;
-    return bytes <= (long long)SMALL_PART * blocks ? launch<T, LOSS, GRAD, 128>(a, blocks, s) : launch<T, LOSS, GRAD, 512>(a, blocks, s);
+    return bytes <= (long long)SMALL_PART * blocks ? launch<T, LOSS, GRAD, 64>(a, blocks, s) : launch<T, LOSS, GRAD, 256>(a, blocks, s);
 }
 template <bool LOSS, bool GRAD>
 int by_type(DistillArgs &a, int dtype, cudaStream_t s) {
