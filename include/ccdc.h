@@ -631,7 +631,7 @@ int ccdc_expert_combine_backward(long long M, int k, long long D, int dtype, con
  *                          lddz), the stats of the same inputs
  *   both in one pass       loss, dloss and dlogits; stats may be NULL
  * dlogits may be the logits themselves (same stride).  1e-6 <= T <= 1e6;
- * k <= 1024, rows of at most 1536 KiB (CCDC_ESIZE). */
+ * k <= 1024, rows of at most 1408 KiB (CCDC_ESIZE). */
 int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits, long long ldz, int id_bytes, const void *ids,
                  int value_dtype, const void *values, const float *teacher_lse, float temperature, const float *dloss, float *loss,
                  void *stats, void *dlogits, long long lddz, void *stream);

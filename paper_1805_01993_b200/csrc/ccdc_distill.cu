@@ -5,13 +5,15 @@
 //     loss = sum_j t_j (log t_j - log s_id(j)),  s = softmax(z / T)
 //     dz   = dloss / T (P s - t),  P = sum_j t_j
 // Reading z and writing dz is all the work.  A row belongs to one block or to the blocks of a cluster, which keep it in shared
-// memory between the walk for maximum and sum and the walk that writes the gradient: z is read from memory once.  Parts are
-// small enough for several blocks an SM, so that one row's loads run under another's stores.  Each thread copies 16-byte pieces
-// asynchronously and reads only its own, so nothing waits but for them; the blocks of a cluster exchange their maxima and sums.
-// The last warp of a block computes the k terms meanwhile, in 64 bits.  Exponentials are the next bound (two for each element).
+// memory between the walk for maximum and sum and the walk that writes the gradient: z is read from memory once.  Blocks stay and
+// take row after row: a thread copies 16-byte pieces asynchronously and reads only its own, so the copy of the next row's piece
+// starts as soon as a piece has been read for the last time, and nothing waits but for copies.  The blocks of a cluster exchange
+// their maxima and sums.  The last warp of a block computes the next row's k terms meanwhile, in 64 bits.  Exponentials are the
+// next bound (two for each element).
 #include "ccdc_block.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -20,7 +22,7 @@ constexpr int AHEAD = 4;                    // slots a lane
 constexpr int GROUPS = 4;                   // of copies that are waited for one after the other
 constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 64 threads take; more take 256
 constexpr int PART = 64 << 10;              // bytes of a part that leave room for three blocks an SM
-constexpr int MOST_PART = 192 << 10;
+constexpr int MOST_PART = 176 << 10, MOST_SMEM = MOST_PART + 32 + 48 * MAX_TOP;
 
 struct DistillArgs {
     long long M, V, ldz, lddz;
@@ -32,7 +34,9 @@ struct DistillArgs {
     void *dz;
     double inv_t;
     float scale;                // log2(e) / T
+    int group;                  // pieces of a thread in a group of copies
     int part_pieces, table;     // room of a block, in pieces of 16 bytes; of the table of ids
+    int log_blocks;             // of the blocks to a row
 };
 
 template <class T, int N>
@@ -40,6 +44,13 @@ struct alignas(sizeof(T) * N) Pack {
     T v[N];
 };
 
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     float2 d;
     asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
@@ -60,19 +71,33 @@ __device__ __forceinline__ float power(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
     return e;
 }
-// exp of z / T above the maximum's.  The difference first: no product of a masked row's lowest value overflows.
+// 2^(z * scale) relative to a reference `top` (a row's or a thread's largest value).  16-bit logits: 2^(z * scale - b), one
+// fused operation for each, with b = top * scale rounded once, so that its rounding is the same in every term; unless b is so
+// large that z * scale may overflow (a row of a type's lowest values).  Those and binary32: 2^((z - top) * scale).
 template <class T>
-__device__ __forceinline__ float above(float z, float top, float scale) {
-    return power<T>((z - top) * scale);
-}
-template <class T>
-__device__ __forceinline__ float2 above2(float2 z, float top, float scale) {
-    const float2 d = mul2(add2(z, make_float2(-top, -top)), make_float2(scale, scale));
-    return make_float2(power<T>(d.x), power<T>(d.y));
-}
+struct Above {
+    float top, scale, b;
+    bool fused;
+    __device__ __forceinline__ Above(float top_, float scale_) : top(top_ == -INFINITY ? 0.0f : top_), scale(scale_) {
+        b = __fmul_rn(top, scale);
+        fused = sizeof(T) == 2 && fabsf(b) < 0x1p100f;
+    }
+    __device__ __forceinline__ float exponent(float z) const { return fused ? fmaf(z, scale, -b) : (z - top) * scale; }
+    __device__ __forceinline__ float operator()(float z) const { return power<T>(exponent(z)); }
+    template <bool FUSED>
+    __device__ __forceinline__ float2 two(float2 z) const {
+        const float2 d = FUSED ? fma2(z, make_float2(scale, scale), make_float2(-b, -b))
+                               : mul2(add2(z, make_float2(-top, -top)), make_float2(scale, scale));
+        return make_float2(power<T>(d.x), power<T>(d.y));
+    }
+    // the exponent in 64 bits, of the same products
+    __device__ __forceinline__ double exact(float z) const {
+        return fused ? (double)z * (double)scale - (double)b : ((double)z - (double)top) * (double)scale;
+    }
+};
 // the eight (binary32: four) values of a piece of 16 bytes, two by two
 template <class T>
-__device__ __forceinline__ void values_of(const uint4 &v, float2 (&f)[8 / sizeof(T)]) {
+__device__ __forceinline__ void values_of(const uint4 &v, float2 (&f)[8 / (int)sizeof(T)]) {
     if constexpr (sizeof(T) == 4) {
         f[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
         f[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
@@ -81,7 +106,7 @@ __device__ __forceinline__ void values_of(const uint4 &v, float2 (&f)[8 / sizeof
     }
 }
 template <class T>
-__device__ __forceinline__ uint4 piece_of(const float2 (&f)[8 / sizeof(T)]) {
+__device__ __forceinline__ uint4 piece_of(const float2 (&f)[8 / (int)sizeof(T)]) {
     if constexpr (sizeof(T) == 4)
         return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
     else
@@ -91,30 +116,42 @@ __device__ __forceinline__ uint4 piece_of(const float2 (&f)[8 / sizeof(T)]) {
 struct Running {
     float top, sum;
 };
-// the sum's factor when its maximum rises from `from` to `to` (a sum of nothing has -inf)
+// the sum's factor when its reference rises from `from` to `to` (a sum of nothing has -inf)
 template <class T>
 __device__ __forceinline__ float rebase(float from, float to, float scale) {
-    return from == to ? 1.0f : above<T>(from, to, scale);
+    if (from == to || from == -INFINITY) return 1.0f;
+    const Above<T> lo(from, scale), hi(to, scale);
+    return power<T>(lo.fused && hi.fused ? lo.b - hi.b : (from - to) * scale);
 }
+// The lanes' sums together, in groups of LANES: every lane of a group gets the same bits.
 template <class T>
-__device__ __forceinline__ Running join(Running a, Running b, float scale) {
-    const float top = fmaxf(a.top, b.top);
-    // the same bits for (a, b) and (b, a): every lane of an exchange gets one result
-    return {top, __fadd_rn(__fmul_rn(a.sum, rebase<T>(a.top, top, scale)), __fmul_rn(b.sum, rebase<T>(b.top, top, scale)))};
-}
-template <class T, int PAIRS>
-__device__ __forceinline__ void add(Running &r, const float2 (&f)[PAIRS], float scale) {
+__device__ __forceinline__ Running join(Running r, float scale, int lanes) {
     float top = r.top;
-#pragma unroll
-    for (int i = 0; i < PAIRS; ++i) top = fmaxf(top, fmaxf(f[i].x, f[i].y));
-    // all -inf so far (or NaN, which fmax leaves out): count from zero, so that -inf adds nothing and NaN stays NaN
-    const float from = top == -INFINITY ? 0.0f : top;
-    float2 sum = above2<T>(f[0], from, scale);
-#pragma unroll
-    for (int i = 1; i < PAIRS; ++i) sum = add2(sum, above2<T>(f[i], from, scale));
-    r.sum = r.sum * rebase<T>(r.top, top, scale) + (sum.x + sum.y);
-    r.top = top;
+    for (int d = 1; d < lanes; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    float sum = r.sum * rebase<T>(r.top, top, scale);
+    for (int d = 1; d < lanes; d *= 2) sum += __shfl_xor_sync(~0u, sum, d);
+    return {top, sum};
 }
+// Largest values piece by piece, 16-bit ones two by two as they lie in memory.  NaN is left out, and shows in the sum.
+template <class T>
+struct Largest {
+    using T2 = typename std::conditional<std::is_same<T, bf16>::value, __nv_bfloat162, __half2>::type;
+    T2 two;
+    __device__ __forceinline__ Largest() : two(T2(from_f32<T>(-INFINITY), from_f32<T>(-INFINITY))) {}
+    __device__ __forceinline__ void take(const uint4 &v) {
+        const T2 *w = reinterpret_cast<const T2 *>(&v);
+        two = __hmax2(two, __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3])));
+    }
+    __device__ __forceinline__ float value() const { return fmaxf(to_f32<T>(two.x), to_f32<T>(two.y)); }
+};
+template <>
+struct Largest<float> {
+    float one = -INFINITY;
+    __device__ __forceinline__ void take(const uint4 &v) {
+        one = fmaxf(one, fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w))));
+    }
+    __device__ __forceinline__ float value() const { return one; }
+};
 
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
@@ -209,184 +246,268 @@ __device__ __forceinline__ Teacher teacher_side(const DistillArgs &a, const T *z
     return r;
 }
 
+// A block's share of a row, in pieces from the 16-byte boundary below the row's start: element i of piece p is z[at + p N + i].
+template <class T>
+struct Share {
+    static constexpr int N = 16 / sizeof(T);
+    const uint4 *from;
+    int at, count, low, high;   // low, high: pieces that may reach over the row's ends, or -1
+    __device__ __forceinline__ Share(const DistillArgs &a, const T *z, int rank) {
+        const int skew = (int)(reinterpret_cast<uintptr_t>(z) & 15) / (int)sizeof(T);
+        const int pieces = ((int)a.V + skew + N - 1) / N, first = rank * a.part_pieces;
+        count = max(0, min(a.part_pieces, pieces - first)), at = first * N - skew;
+        from = reinterpret_cast<const uint4 *>(z + at);
+        low = rank ? -1 : 0, high = first + count == pieces ? count - 1 : -1;
+    }
+    __device__ __forceinline__ bool edge(int p) const { return p == low || p == high; }
+    // what lies outside counts as -inf
+    __device__ __forceinline__ uint4 inside(const DistillArgs &a, uint4 v, int p) const {
+        Pack<T, N> w = *reinterpret_cast<const Pack<T, N> *>(&v);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (at + p * N + i < 0 || at + p * N + i >= (int)a.V) w.v[i] = from_f32<T>(-INFINITY);
+        return *reinterpret_cast<const uint4 *>(&w);
+    }
+};
+__device__ __forceinline__ void copy_piece(uint4 *to, const uint4 *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
 // LOSS: computes the statistics, writes loss and (where asked) stats.  GRAD: writes dz, from stats without LOSS.
-// A cluster of gridDim.x / M blocks to a row; THREADS that walk the row and one warp for the teacher's side.
+// `blocks` to a row (a cluster); THREADS that walk rows and one warp for the teacher's side.
 template <class T, bool LOSS, bool GRAD, int THREADS>
-__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 10) k_distill(DistillArgs a) {
-    constexpr int N = 16 / sizeof(T);       // elements of a piece
-    extern __shared__ uint4 row[];          // this block's pieces, then the slots
-    Slots slots;
-    slots.target = reinterpret_cast<double *>(row + a.part_pieces);
-    slots.value = reinterpret_cast<float *>(slots.target + a.k), slots.chosen = slots.value + a.k;
-    slots.at = reinterpret_cast<int *>(slots.chosen + a.k);
-    slots.seen = slots.at + a.k, slots.mask = a.table - 1;
-    __shared__ Running runs[THREADS / 32], whole;
-    __shared__ Teacher told;
+__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 12) k_distill(DistillArgs a) {
+    constexpr int N = 16 / sizeof(T), PAIRS = N / 2;        // elements of a piece
+    extern __shared__ uint4 row[];          // this block's pieces, then the slots of two rows
+    __shared__ Running runs[2][THREADS / 32], whole[2];
+    __shared__ Teacher told[2];
     const int tid = threadIdx.x, lane = tid & 31;
     const bool walks = tid < THREADS;
-    const unsigned blocks = (unsigned)(gridDim.x / a.M), rank = blockIdx.x % blocks;
-    const long long m = blockIdx.x / blocks;
-    const T *z = static_cast<const T *>(a.z) + m * a.ldz;
-    // The row in pieces from the 16-byte boundary below its start: element i of piece p is z[p N + i - skew].
-    const int skew = (int)(reinterpret_cast<uintptr_t>(z) & 15) / (int)sizeof(T);
-    const long long pieces = (a.V + skew + N - 1) / N, first = pieces * rank / blocks;
-    const int count = (int)(pieces * (rank + 1) / blocks - first);
-    const int each = (count + THREADS - 1) / THREADS, group = (each + GROUPS - 1) / GROUPS;
+    const int blocks = 1 << a.log_blocks, rank = blockIdx.x & (blocks - 1);
+    const long long step = gridDim.x >> a.log_blocks;
+    const auto slots_of = [&](int which) {
+        Slots s;
+        s.target = reinterpret_cast<double *>(row + a.part_pieces) + which * a.k;
+        s.value = reinterpret_cast<float *>(reinterpret_cast<double *>(row + a.part_pieces) + 2 * a.k) + which * 2 * a.k, s.chosen = s.value + a.k;
+        s.at = reinterpret_cast<int *>(reinterpret_cast<double *>(row + a.part_pieces) + 4 * a.k) + which * a.k;
+        s.seen = reinterpret_cast<int *>(reinterpret_cast<double *>(row + a.part_pieces) + 5 * a.k), s.mask = a.table - 1;
+        return s;
+    };
+    const auto row_of = [&](long long m) { return static_cast<const T *>(a.z) + m * a.ldz; };
 
-    Running r = {-INFINITY, 0.0f};
-    if (walks) {
-        const uint4 *from = reinterpret_cast<const uint4 *>(z - skew) + first;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            for (int j = g * group; j < min(each, (g + 1) * group); ++j)
-                if (tid + j * THREADS < count)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                                 ::"r"((uint32_t)__cvta_generic_to_shared(row + tid + j * THREADS)), "l"(from + tid + j * THREADS) : "memory");
-            asm volatile("cp.async.commit_group;" ::: "memory");
+    long long m = blockIdx.x >> a.log_blocks;
+    if (m < a.M) {
+        if (walks) {
+            const Share<T> own(a, row_of(m), rank);
+            for (int g = 0; g < GROUPS; ++g) {
+                for (int p = tid + g * a.group * THREADS; p < min(own.count, tid + (g + 1) * a.group * THREADS); p += THREADS)
+                    copy_piece(row + p, own.from + p);
+                copies_end();
+            }
+        } else {
+            const Teacher t = teacher_side<T>(a, row_of(m), m, slots_of(0), lane);
+            if (lane == 0) told[0] = t;
         }
-        if constexpr (LOSS) {
-            constexpr int PAIRS = N / 2;
-            // two pieces at a time, one rise of the maximum for both
-            const auto use = [&](int g) {
-                for (int j = g * group; j < min(each, (g + 1) * group); j += 2) {
-                    float2 f[2 * PAIRS];
+    }
+    for (int which = 0; m < a.M; m += step, which ^= 1) {
+        const T *z = row_of(m);
+        const bool more = m + step < a.M;
+        const Share<T> own(a, z, rank), next(a, row_of(more ? m + step : m), rank);
+        const int group = a.group;
+        const Slots slots = slots_of(which);
+        const int next_count = more ? next.count : 0;
+        Running r = {-INFINITY, 0.0f};
+        if (walks) {
+            if constexpr (LOSS) {
+                // a group's maximum first: one rise of the reference for all its pieces
+                const auto use = [&](int g) {
+                    const int begin = tid + g * group * THREADS, end = min(own.count, begin + group * THREADS);
+                    Largest<T> largest;
+                    for (int p = begin; p < end; p += THREADS) {
+                        if (own.edge(p)) row[p] = own.inside(a, row[p], p);
+                        largest.take(row[p]);
+                    }
+                    const float top = fmaxf(r.top, largest.value());
+                    r.sum *= rebase<T>(r.top, top, a.scale), r.top = top;
+                    const Above<T> above(top, a.scale);     // all -inf: counted from zero, so that -inf adds nothing and NaN stays NaN
+                    const auto sum_up = [&](auto fused) {
+                        float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll 2
+                        for (int p = begin; p < end; p += THREADS) {
+                            float2 f[PAIRS], e[PAIRS];
+                            values_of<T>(row[p], f);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int p = tid + (j + u) * THREADS;
-                        float2(&h)[PAIRS] = *reinterpret_cast<float2(*)[PAIRS]>(f + u * PAIRS);
-                        if (p >= count || j + u >= min(each, (g + 1) * group)) {
+                            for (int i = 0; i < PAIRS; ++i) e[i] = above.template two<fused>(f[i]);
 #pragma unroll
-                            for (int i = 0; i < PAIRS; ++i) h[i] = make_float2(-INFINITY, -INFINITY);
-                            continue;
+                            for (int d = PAIRS / 2; d; d /= 2)
+#pragma unroll
+                                for (int i = 0; i < d; ++i) e[i] = add2(e[i], e[i + d]);
+                            sum = add2(sum, e[0]);
                         }
-                        values_of<T>(row[p], h);
-                        if (first + p == 0 || first + p == pieces - 1) {        // may reach over the row's ends
-                            const long long e = (first + p) * N - skew;
+                        r.sum += sum.x + sum.y;
+                    };
+                    if (sizeof(T) == 2 && above.fused)
+                        sum_up(std::true_type());
+                    else
+                        sum_up(std::false_type());
+                };
+                copies_landed<3>(), use(0), copies_landed<2>(), use(1), copies_landed<1>(), use(2), copies_landed<0>(), use(3);
+                if constexpr (!GRAD) {
+                    for (int g = 0; g < GROUPS; ++g) {
+                        for (int p = tid + g * group * THREADS; p < min(next_count, tid + (g + 1) * group * THREADS); p += THREADS)
+                            copy_piece(row + p, next.from + p);
+                        copies_end();
+                    }
+                }
+                r = join<T>(r, a.scale, 32);
+                if (lane == 0) runs[which][tid >> 5] = r;
+            } else {
+                copies_landed<0>();
+            }
+        }
+        __syncthreads();
+        if constexpr (LOSS) {
+            r = join<T>(runs[which][lane & (THREADS / 32 - 1)], a.scale, THREADS / 32);
+            if (blocks > 1 && tid == 0) whole[which] = r;
+        } else {
+            const float2 s = a.stats[m];
+            r = {s.x, s.y};
+        }
+        if (blocks > 1) {
+            // every block has its sums, and has read what others may overwrite from here on
+            __syncwarp();
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if constexpr (LOSS) {
+                uint32_t p;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                             : "=r"(p) : "r"((uint32_t)__cvta_generic_to_shared(&whole[which])), "r"(lane & (blocks - 1)));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(r.top), "=f"(r.sum) : "r"(p) : "memory");
+                r = join<T>(r, a.scale, blocks);
+            }
+        }
+        const Above<T> above(r.top, a.scale);
+        const double P = told[which].P;
+        const bool empty = P == 0.0;                // a row without targets: padding
+        if (!walks) {
+            if (LOSS && rank == 0) {
+                const double log_sum = log((double)r.sum);
+                double loss = 0.0;
+                for (int j = lane; j < a.k; j += 32)
+                    if (slots.at[j] >= 0 && slots.target[j] != 0.0)
+                        loss -= slots.target[j] * (above.exact(slots.chosen[j]) * 0.6931471805599453 - log_sum);
+                loss = warp_sum(loss) + told[which].entropy;
+                if (lane == 0) {
+                    a.loss[m] = empty ? 0.0f : (float)loss;
+                    if (a.stats) a.stats[m] = make_float2(r.top, r.sum);
+                }
+            }
+            if (more) {
+                const Teacher t = teacher_side<T>(a, row_of(m + step), m + step, slots_of(which ^ 1), lane);
+                if (lane == 0) told[which ^ 1] = t;
+            }
+        } else if constexpr (GRAD) {
+            const float c = a.dloss[m] * (float)a.inv_t, cs = c * ((float)P / r.sum);
+            T *dz = static_cast<T *>(a.dz) + m * a.lddz;
+            const bool alike = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+            const auto gradient = [&](const uint4 &v, auto fused) {
+                float2 f[PAIRS];
+                values_of<T>(v, f);
 #pragma unroll
-                            for (int i = 0; i < PAIRS; ++i) {
-                                if (e + 2 * i < 0 || e + 2 * i >= a.V) h[i].x = -INFINITY;
-                                if (e + 2 * i + 1 < 0 || e + 2 * i + 1 >= a.V) h[i].y = -INFINITY;
-                            }
+                for (int i = 0; i < PAIRS; ++i) f[i] = mul2(above.template two<fused>(f[i]), make_float2(cs, cs));
+                return piece_of<T>(f);
+            };
+            const auto write = [&](auto fused) {
+                for (int g = 0; g < GROUPS; ++g) {
+                    const int from = tid + g * group * THREADS, to = from + group * THREADS;
+#pragma unroll 2
+                    for (int p = from; p < min(own.count, to); p += THREADS) {
+                        const uint4 v = empty ? make_uint4(0, 0, 0, 0) : gradient(row[p], fused);
+                        if (p < next_count) copy_piece(row + p, next.from + p);
+                        const int e = own.at + p * N;
+                        if (alike && !own.edge(p)) {
+                            *reinterpret_cast<uint4 *>(dz + e) = v;
+                        } else {
+                            const Pack<T, N> w = *reinterpret_cast<const Pack<T, N> *>(&v);
+#pragma unroll
+                            for (int i = 0; i < N; ++i)
+                                if (e + i >= 0 && e + i < (int)a.V) dz[e + i] = w.v[i];
                         }
                     }
-                    add<T>(r, f, a.scale);
+                    // the next row may have a piece more
+                    if (own.count >= from && own.count < to && own.count < next_count && (own.count - from) % THREADS == 0)
+                        copy_piece(row + own.count, next.from + own.count);
+                    copies_end();
                 }
             };
-            copies_landed<3>(), use(0), copies_landed<2>(), use(1), copies_landed<1>(), use(2), copies_landed<0>(), use(3);
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2)
-                r = join<T>(r, {__shfl_xor_sync(~0u, r.top, d), __shfl_xor_sync(~0u, r.sum, d)}, a.scale);
-            if (lane == 0) runs[tid >> 5] = r;
-        } else {
-            copies_landed<0>();
+            if (sizeof(T) == 2 && above.fused)
+                write(std::true_type());
+            else
+                write(std::false_type());
+            // the targets' elements are written again, by the block that wrote them
+            asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+            const int e0 = own.at, e1 = own.at + own.count * N;
+            const bool twice = told[which].twice;
+            for (int j = tid; !empty && j < a.k; j += THREADS) {
+                const int id = slots.at[j];
+                if (id < 0 || id < e0 || id >= e1) continue;
+                double t = slots.target[j];
+                bool lead = true;
+                if (twice) {            // the slots that name this element add up; the first of them writes it
+                    t = 0.0;
+                    for (int i = 0; i < a.k; ++i)
+                        if (slots.at[i] == id) {
+                            if (i < j) lead = false;
+                            t += slots.target[i];
+                        }
+                }
+                if (lead) dz[id] = from_f32<T>(fmaf(-c, (float)t, cs * above(slots.chosen[j])));
+            }
         }
-    } else {
-        const Teacher t = teacher_side<T>(a, z, m, slots, lane);
-        if (lane == 0) told = t;
     }
-    __syncthreads();
-    if constexpr (LOSS) {
-        r = runs[lane & (THREADS / 32 - 1)];
-#pragma unroll
-        for (int d = 1; d < THREADS / 32; d *= 2)
-            r = join<T>(r, {__shfl_xor_sync(~0u, r.top, d), __shfl_xor_sync(~0u, r.sum, d)}, a.scale);
-        if (blocks > 1 && tid == 0) whole = r;
-    } else {
-        const float2 s = a.stats[m];
-        r = {s.x, s.y};
-    }
-    if (blocks > 1) {
-        // every block has its sums, and has read what others may overwrite from here on
+    if (LOSS && blocks > 1) {           // no block leaves while another reads its sums
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if constexpr (LOSS) {
-            for (unsigned b = 0; b < blocks; ++b) {
-                uint32_t p;
-                Running o;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"((uint32_t)__cvta_generic_to_shared(&whole)), "r"(b));
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(o.top), "=f"(o.sum) : "r"(p) : "memory");
-                r = b ? join<T>(r, o, a.scale) : o;
-            }
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // waited for at the end
-        }
     }
-    const float base = r.top == -INFINITY ? 0.0f : r.top;
-    const double P = told.P;
-    const bool empty = P == 0.0;                // a row without targets: padding
-    if (LOSS && rank == 0 && !walks) {
-        const double log_sum = log((double)r.sum);
-        double loss = 0.0;
-        for (int j = lane; j < a.k; j += 32)
-            if (slots.at[j] >= 0 && slots.target[j] != 0.0)
-                loss -= slots.target[j] * (((double)slots.chosen[j] - (double)base) * (double)a.scale * 0.6931471805599453 - log_sum);
-        loss = warp_sum(loss) + told.entropy;
-        if (lane == 0) {
-            a.loss[m] = empty ? 0.0f : (float)loss;
-            if (a.stats) a.stats[m] = make_float2(r.top, r.sum);
-        }
-    }
-    if constexpr (GRAD) {
-        const float c = a.dloss[m] * (float)a.inv_t, cs = (float)((double)a.dloss[m] * a.inv_t * P / (double)r.sum);
-        T *dz = static_cast<T *>(a.dz) + m * a.lddz;
-        const bool alike = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
-        for (int j = 0; walks && j < each; ++j) {
-            const int p = tid + j * THREADS;
-            if (p >= count) break;
-            const long long e = (first + p) * N - skew;
-            float2 f[N / 2];
-            values_of<T>(row[p], f);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i) f[i] = empty ? make_float2(0.0f, 0.0f) : mul2(above2<T>(f[i], base, a.scale), make_float2(cs, cs));
-            const uint4 v = piece_of<T>(f);
-            if (alike && e >= 0 && e + N <= a.V) {
-                *reinterpret_cast<uint4 *>(dz + e) = v;
-            } else {
-                const Pack<T, N> w = *reinterpret_cast<const Pack<T, N> *>(&v);
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (e + i >= 0 && e + i < a.V) dz[e + i] = w.v[i];
-            }
-        }
-        __syncthreads();            // the targets' elements are written again, by the block that wrote them
-        const long long e0 = first * N - skew, e1 = (first + count) * N - skew;
-        const bool twice = told.twice;
-        for (int j = tid; !empty && j < a.k; j += THREADS + 32) {
-            const int id = slots.at[j];
-            if (id < 0 || id < e0 || id >= e1) continue;
-            double t = slots.target[j];
-            bool lead = true;
-            if (twice) {            // the slots that name this element add up; the first of them writes it
-                t = 0.0;
-                for (int i = 0; i < a.k; ++i)
-                    if (slots.at[i] == id) {
-                        if (i < j) lead = false;
-                        t += slots.target[i];
-                    }
-            }
-            if (lead) dz[id] = from_f32<T>(fmaf(-c, (float)t, cs * above<T>(slots.chosen[j], base, a.scale)));
-        }
-    }
-    __syncwarp();
-    if (LOSS && blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // `whole` has been read
 }
 
 template <class T, bool LOSS, bool GRAD, int THREADS>
 int launch(DistillArgs &a, int blocks, cudaStream_t s) {
     auto *kernel = k_distill<T, LOSS, GRAD, THREADS>;
     static std::atomic<unsigned long long> done;
-    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), MOST_PART + 32 + 28 * MAX_TOP, &done);
+    const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), MOST_SMEM, &done);
     if (rc != CCDC_OK) return rc;
-    a.table = table_length(a.k);
-    a.part_pieces = (int)((a.V * (long long)sizeof(T) + 30) / 16 / blocks) + 1;
+    a.table = table_length(a.k), a.log_blocks = blocks == 8 ? 3 : blocks >> 1;
+    // a row has (V + 2 (N - 1)) / N pieces at most
+    a.part_pieces = (int)(((a.V * (long long)sizeof(T) + 30) / 16 + blocks - 1) / blocks);
+    a.group = (a.part_pieces + GROUPS * THREADS - 1) / (GROUPS * THREADS);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.M * blocks)), cfg.blockDim = dim3(THREADS + 32);
-    cfg.dynamicSmemBytes = 16 * (size_t)a.part_pieces + 20 * a.k + 4 * a.table, cfg.stream = s;
+    cfg.blockDim = dim3(THREADS + 32);
+    cfg.dynamicSmemBytes = 16 * (size_t)a.part_pieces + 40 * a.k + 4 * a.table, cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = blocks, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
     cfg.attrs = at, cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    // As many clusters as run at once; more would wait for whole blocks to end.  The answer for the last shape that was asked for
+    // is kept: device, blocks and shared memory in the upper bits, clusters in the lower 16.
+    static std::atomic<unsigned long long> known;
+    int dev = 0, clusters = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    const unsigned long long shape = ((unsigned long long)dev << 32 | (unsigned)blocks << 24 | (unsigned)cfg.dynamicSmemBytes) << 16;
+    const unsigned long long last = known.load(std::memory_order_relaxed);
+    cfg.gridDim = dim3((unsigned)blocks);
+    if (last >> 16 == shape >> 16 && (last & 0xFFFF)) {
+        clusters = (int)(last & 0xFFFF);
+    } else if (e == cudaSuccess) {
+        e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+        clusters = std::min(std::max(clusters, 1), 0xFFFF);
+        if (e == cudaSuccess) known.store(shape | (unsigned)clusters, std::memory_order_relaxed);
+    }
+    if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
+    cfg.gridDim = dim3((unsigned)(std::min<long long>(a.M, clusters) * blocks));
+    e = cudaLaunchKernelEx(&cfg, kernel, a);
     if (e != cudaSuccess) return ccdc_internal_cuda_fail((int)e);
     return block_launch_status();
 }
@@ -400,7 +521,7 @@ int launch(DistillArgs &a, cudaStream_t s) {
     int blocks = 1;
     while (blocks < MAX_CLUSTER && (bytes > (long long)PART * blocks || (a.M * blocks * 2 <= sms && bytes > (long long)SMALL_PART * blocks)))
         blocks *= 2;
-    if (bytes > (long long)MOST_PART * blocks || a.M * blocks > 0x7FFFFFFF) return CCDC_ESIZE;
+    if (bytes > (long long)MOST_PART * blocks) return CCDC_ESIZE;
     return bytes <= (long long)SMALL_PART * blocks ? launch<T, LOSS, GRAD, 64>(a, blocks, s) : launch<T, LOSS, GRAD, 256>(a, blocks, s);
 }
 template <bool LOSS, bool GRAD>

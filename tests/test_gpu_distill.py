@@ -234,4 +234,8 @@ def test_more_than_two_to_the_31_elements(ccdc):
     dloss = torch.ones(M, device="cuda")
     loss, dz = ccdc.distill(dloss, z, ids, values)
     l, g = ccdc.distill(dloss[-3:], z[-3:].clone(), ids[-3:], values[-3:])
-    assert torch.equal(loss[-3:], l) and torch.equal(dz[-3:], g) and not loss[:-3].any() and not dz[:-3].any()
+    # three rows alone are cut into more parts: sums of 131072 positive terms in another order, a thread's at most 512 of them
+    # one after the other and 40 more joins, in each call; a bf16 result may then round to the other side
+    close = 2 * (512 + 40) * 2.0 ** -24
+    assert bool(((loss[-3:] - l).abs() <= close + 2.0 ** -23 * l.abs()).all()) and not loss[:-3].any() and not dz[:-3].any()
+    assert bool(((dz[-3:].float() - g.float()).abs() <= (2.0 ** -7 + close) * g.float().abs() + close * 2.0 ** -10).all())
