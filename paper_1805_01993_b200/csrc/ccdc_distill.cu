@@ -272,6 +272,27 @@ struct Share {
 __device__ __forceinline__ void copy_piece(uint4 *to, const uint4 *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
+// the elements of a piece that fall into [low, high)
+template <class T>
+__device__ __forceinline__ void put_some(const DistillArgs &a, T *dz, int e, const uint4 &v, int low, int high) {
+    const Pack<T, 16 / sizeof(T)> w = *reinterpret_cast<const Pack<T, 16 / sizeof(T)> *>(&v);
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(T); ++i)
+        if (e + i >= low && e + i < high) dz[e + i] = w.v[i];
+}
+// 16 bytes of two pieces, from element `shift` of the first on
+template <class T>
+__device__ __forceinline__ uint4 cut(const uint4 &lo, const uint4 &hi, int shift) {
+    const int bytes = shift * (int)sizeof(T);
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 7; ++i) w[i] = bytes & 4 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = bytes & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (bytes & 2));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
 // LOSS: computes the statistics, writes loss and (where asked) stats.  GRAD: writes dz, from stats without LOSS.
@@ -338,7 +359,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 12) k_disti
                             float2 f[PAIRS], e[PAIRS];
                             values_of<T>(row[p], f);
 #pragma unroll
-                            for (int i = 0; i < PAIRS; ++i) e[i] = above.template two<fused>(f[i]);
+                            for (int i = 0; i < PAIRS; ++i) e[i] = above.template two<decltype(fused)::value>(f[i]);
 #pragma unroll
                             for (int d = PAIRS / 2; d; d /= 2)
 #pragma unroll
@@ -415,7 +436,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 12) k_disti
                 float2 f[PAIRS];
                 values_of<T>(v, f);
 #pragma unroll
-                for (int i = 0; i < PAIRS; ++i) f[i] = mul2(above.template two<fused>(f[i]), make_float2(cs, cs));
+                for (int i = 0; i < PAIRS; ++i) f[i] = mul2(above.template two<decltype(fused)::value>(f[i]), make_float2(cs, cs));
                 return piece_of<T>(f);
             };
             const auto write = [&](auto fused) {
@@ -424,20 +445,42 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 12) k_disti
 #pragma unroll 2
                     for (int p = from; p < min(own.count, to); p += THREADS) {
                         const uint4 v = empty ? make_uint4(0, 0, 0, 0) : gradient(row[p], fused);
+                        if (!alike) {
+                            row[p] = v;
+                            continue;
+                        }
                         if (p < next_count) copy_piece(row + p, next.from + p);
                         const int e = own.at + p * N;
-                        if (alike && !own.edge(p)) {
+                        if (!own.edge(p))
                             *reinterpret_cast<uint4 *>(dz + e) = v;
-                        } else {
-                            const Pack<T, N> w = *reinterpret_cast<const Pack<T, N> *>(&v);
-#pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (e + i >= 0 && e + i < (int)a.V) dz[e + i] = w.v[i];
-                        }
+                        else
+                            put_some<T>(a, dz, e, v, 0, (int)a.V);
                     }
+                    if (!alike) continue;
                     // the next row may have a piece more
                     if (own.count >= from && own.count < to && own.count < next_count && (own.count - from) % THREADS == 0)
                         copy_piece(row + own.count, next.from + own.count);
+                    copies_end();
+                }
+                if (alike) return;
+                // Rows of z and dz that lie differently to 16 bytes: the gradient's pieces, which are in shared memory now, leave cut
+                // anew.  Only then may the next row come.
+                asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+                const int low = max(0, own.at), high = min((int)a.V, own.at + own.count * N);
+                const int skew = (int)(reinterpret_cast<uintptr_t>(dz) & 15) / (int)sizeof(T), first = (low + skew) / N;
+                const int shift = (first * N - skew - own.at) & (N - 1);        // of a cut piece in those it comes from
+                for (int q = first + tid; q * N - skew < high; q += THREADS) {
+                    const int e = q * N - skew, p = (e - own.at) >> (N == 8 ? 3 : 2);
+                    const uint4 v = cut<T>(row[max(p, 0)], row[min(p + 1, own.count - 1)], shift);
+                    if (e >= low && e + N <= high)
+                        *reinterpret_cast<uint4 *>(dz + e) = v;
+                    else
+                        put_some<T>(a, dz, e, v, low, high);
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+                for (int g = 0; g < GROUPS; ++g) {
+                    for (int p = tid + g * group * THREADS; p < min(next_count, tid + (g + 1) * group * THREADS); p += THREADS)
+                        copy_piece(row + p, next.from + p);
                     copies_end();
                 }
             };
