@@ -20,7 +20,7 @@ namespace {
 constexpr int MAX_TOP = 1024, MAX_CLUSTER = 8;
 constexpr int AHEAD = 4;                    // slots a lane
 constexpr int GROUPS = 4;                   // of copies that are waited for one after the other
-constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 64 threads take; more take 256
+constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 64 threads take
 constexpr int PART = 64 << 10;              // bytes of a part that leave room for three blocks an SM
 constexpr int MOST_PART = 176 << 10, MOST_SMEM = MOST_PART + 32 + 48 * MAX_TOP;
 
@@ -298,7 +298,7 @@ __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_gro
 // LOSS: computes the statistics, writes loss and (where asked) stats.  GRAD: writes dz, from stats without LOSS.
 // `blocks` to a row (a cluster); THREADS that walk rows and one warp for the teacher's side.
 template <class T, bool LOSS, bool GRAD, int THREADS>
-__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : 12) k_distill(DistillArgs a) {
+__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 128 ? 6 : THREADS == 64 ? 12 : 16) k_distill(DistillArgs a) {
     constexpr int N = 16 / sizeof(T), PAIRS = N / 2;        // elements of a piece
     extern __shared__ uint4 row[];          // this block's pieces, then the slots of two rows
     __shared__ Running runs[2][THREADS / 32], whole[2];
@@ -565,7 +565,12 @@ int launch(DistillArgs &a, cudaStream_t s) {
     while (blocks < MAX_CLUSTER && (bytes > (long long)PART * blocks || (a.M * blocks * 2 <= sms && bytes > (long long)SMALL_PART * blocks)))
         blocks *= 2;
     if (bytes > (long long)MOST_PART * blocks) return CCDC_ESIZE;
-    return bytes <= (long long)SMALL_PART * blocks ? launch<T, LOSS, GRAD, 64>(a, blocks, s) : launch<T, LOSS, GRAD, 256>(a, blocks, s);
+    // Few threads to a small part: what a row costs beside its bytes is paid by each warp.  (8192 x 8192 bf16 in one pass: 97 us
+    // with 128 threads, 114 with 256; 8192 x 32000: 261 and 231.)
+    const long long part = bytes / blocks;
+    return part <= SMALL_PART / 2   ? launch<T, LOSS, GRAD, 32>(a, blocks, s)
+           : part <= SMALL_PART     ? launch<T, LOSS, GRAD, 64>(a, blocks, s)
+           : part <= 4 * SMALL_PART ? launch<T, LOSS, GRAD, 128>(a, blocks, s) : launch<T, LOSS, GRAD, 256>(a, blocks, s);
 }
 template <bool LOSS, bool GRAD>
 int by_type(DistillArgs &a, int dtype, cudaStream_t s) {
