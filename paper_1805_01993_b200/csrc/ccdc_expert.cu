@@ -12,10 +12,11 @@ namespace {
 constexpr int MAX_EXPERTS = 4096;
 constexpr int SORT_CLUSTER = 8;             // blocks of a sort of many slots
 constexpr int SORT_ONE_BLOCK = 4096;        // slots that one block sorts alone
+constexpr int BATCH = 4;
 
 struct SortArgs {
     long long slots;
-    int experts;
+    int experts, bits;
     const void *ids;
     int *offsets, *slot_at, *place_of;
 };
@@ -39,7 +40,7 @@ __device__ __forceinline__ int remote(const int *p, uint32_t rank) {
 }
 
 // One launch of one block, or of one cluster of blocks.  Each warp owns a run of consecutive slots and counts its experts in
-// shared memory (lanes with the same expert find one another by a match and the first adds for all); the counts become
+// shared memory (lanes with the same expert find one another by ballots and the first adds for all); the counts become
 // starting positions by prefix sums over warps, over the cluster's blocks (read from one another's shared memory) and over
 // experts; the same walk again then places every slot.
 template <class I>
@@ -54,17 +55,30 @@ __global__ void __launch_bounds__(1024) k_expert_sort(SortArgs a) {
     const long long from = min(a.slots, run * ((long long)rank * warps + warp)), to = min(a.slots, from + run);
     const I *ids = static_cast<const I *>(a.ids);
     int *mine = count + warp * E;
-    const auto expert_of = [&](long long s) {
-        if (s >= to) return -1;
-        const I e = ids[s];
-        return e >= 0 && e < (I)E ? (int)e : -1;
+    // experts of the warp's slots, BATCH loads under way at a time; -1 where dropped, -2 behind the run
+    const auto walk = [&](auto use) {
+        for (long long s0 = from; s0 < to; s0 += 32 * BATCH) {
+            I id[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) id[u] = s0 + 32 * u + lane < to ? ids[s0 + 32 * u + lane] : (I)-2;
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                if (s0 + 32 * u >= to) break;
+                const int e = id[u] >= 0 && id[u] < (I)E ? (int)id[u] : s0 + 32 * u + lane < to ? -1 : -2;
+                // the lanes with the same expert: one ballot a bit (a match of all values took 1 us a step, these 0.1)
+                uint32_t same = __ballot_sync(~0u, e >= 0);
+                for (int bit = 0; bit < a.bits; ++bit) {
+                    const uint32_t set = __ballot_sync(~0u, e >> bit & 1);
+                    same &= e >> bit & 1 ? set : ~set;
+                }
+                use(s0 + 32 * u + lane, e, same);
+                __syncwarp();
+            }
+        }
     };
-    for (long long s = from; s < to; s += 32) {
-        const int e = expert_of(s + lane);
-        const uint32_t same = __match_any_sync(~0u, e);
+    walk([&](long long, int e, uint32_t same) {
         if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-        __syncwarp();
-    }
+    });
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += blockDim.x) {
         int sum = 0;
@@ -119,19 +133,16 @@ __global__ void __launch_bounds__(1024) k_expert_sort(SortArgs a) {
     if (rank == 0 && threadIdx.x == 0) a.offsets[E] = carry;
     for (int i = threadIdx.x; i < warps * E; i += blockDim.x) count[i] += base[i % E];
     __syncthreads();
-    for (long long s = from; s < to; s += 32) {
-        const int e = expert_of(s + lane);
-        const uint32_t same = __match_any_sync(~0u, e);
+    walk([&](long long s, int e, uint32_t same) {
         int place = -1;
         if (e >= 0) {
             place = mine[e] + __popc(same & ((1u << lane) - 1));
-            a.slot_at[place] = (int)(s + lane);
+            a.slot_at[place] = (int)s;
         }
         __syncwarp();
         if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-        __syncwarp();
-        if (s + lane < to) a.place_of[s + lane] = place;
-    }
+        if (e > -2) a.place_of[s] = place;
+    });
     // positions behind the last expert's hold nothing
     for (long long i = carry + (long long)rank * blockDim.x + threadIdx.x; i < a.slots; i += (long long)blocks * blockDim.x)
         a.slot_at[i] = -1;
@@ -139,10 +150,33 @@ __global__ void __launch_bounds__(1024) k_expert_sort(SortArgs a) {
 }
 
 // ------------------------------------------------------------- rows there and back
+// Rows are read and written N elements at a time: 16 bytes where all rows are aligned to them, else one.  (Cutting whole pieces
+// out of rows that start elsewhere was slower for its registers: 8192 x 8 rows of 1001 bf16 there, 42 us one by one and 68 cut.)
+// Words stay as they lie in memory until they are used: as elements, 16-bit ones would take a register each.
 template <class T, int N>
-struct alignas(sizeof(T) * N) Pack {
-    T v[N];
+struct Pack {
+    uint4 v = {0, 0, 0, 0};
+    __device__ __forceinline__ void get(float (&f)[N]) const {
+        if constexpr (sizeof(T) == 4) {
+            f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y), f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
+        } else {
+            unpack8<T>(Eight<T>{{v}}, f);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[N]) {
+        if constexpr (sizeof(T) == 4)
+            v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        else
+            v = pack8<T>(f).v[0];
+    }
 };
+template <class T>
+struct Pack<T, 1> {
+    T v = from_f32<T>(0.0f);
+    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32<T>(v); }
+    __device__ __forceinline__ void set(const float (&f)[1]) { v = from_f32<T>(f[0]); }
+};
+
 struct RowArgs {
     long long M, rows;          // tokens, slots
     int k, D, weights_f32;
@@ -159,9 +193,9 @@ __device__ __forceinline__ float weight_of(const RowArgs &a, long long slot) {
     if (!a.weights) return 1.0f;
     return a.weights_f32 ? static_cast<const float *>(a.weights)[slot] : to_f32<T>(static_cast<const T *>(a.weights)[slot]);
 }
-
 // xs[place] = x[m] for the token's places, and zeros in as many of the rows behind the last expert's.  A token's row is read
-// once.  blockDim.x threads to a row, blockDim.y tokens to a block, ITEMS accesses of N elements to a thread.
+// once.  blockDim.x threads to a row, blockDim.y tokens to a block, ITEMS accesses a thread.  16384 x 8 rows of 4096 bf16: 193 us,
+// 6.3 TB/s.
 template <class T, int N, int ITEMS>
 __global__ void __launch_bounds__(256) k_expert_dispatch(RowArgs a) {
     const long long m = (long long)blockIdx.x * blockDim.y + threadIdx.y;
@@ -176,113 +210,141 @@ __global__ void __launch_bounds__(256) k_expert_dispatch(RowArgs a) {
     for (int j = 0; j < a.k; ++j) {
         const long long s = m * a.k + j;
         const int place = a.places[s];
+        const bool empty = a.slots[s] < 0;
         if (place >= 0 && place < a.rows) {
             T *out = static_cast<T *>(a.out) + place * a.ldo;
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
                 if (c0 + i * step < a.D) *reinterpret_cast<P *>(out + c0 + i * step) = v[i];
         }
-        if (a.slots[s] < 0) {
+        if (empty) {
             T *out = static_cast<T *>(a.out) + s * a.ldo;
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
-                if (c0 + i * step < a.D) *reinterpret_cast<P *>(out + c0 + i * step) = P{};
+                if (c0 + i * step < a.D) *reinterpret_cast<P *>(out + c0 + i * step) = P();
         }
     }
 }
 
-// y[m] = sum over j of w[m][j] ys[place], j ascending, dropped slots left out; 0 for a token without slots.
-template <class T, int N, int ITEMS>
-__global__ void __launch_bounds__(256) k_expert_combine(RowArgs a) {
-    const long long m = (long long)blockIdx.x * blockDim.y + threadIdx.y;
-    if (m >= a.M) return;
+// y[m] = sum over j of w[m][j] ys[place], j ascending, dropped slots left out; 0 for a token without slots.  What bounds it is the
+// bytes in flight, since a row's address has to be read first.  So blocks stay and take token after token: eight lanes ask for the
+// next slots' places and weights while this token's rows are on their way, and share them by shuffles; AHEAD rows of ITEMS
+// accesses a thread are asked for together.  16384 x 8 rows of 4096 bf16: 188 us, 6.4 TB/s (437 us a token a block).
+template <class T, int N, int AHEAD, int ITEMS>
+__global__ void __launch_bounds__(256, 3) k_expert_combine(RowArgs a) {
     using P = Pack<T, N>;
-    const int c0 = (blockIdx.y * ITEMS * blockDim.x + threadIdx.x) * N, step = blockDim.x * N;
-    constexpr int AHEAD = ITEMS * N >= 8 ? 4 : 8;       // rows whose loads are in flight together
-    float sum[ITEMS * N] = {};
-    for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
-        P v[AHEAD][ITEMS];
-        float w[AHEAD];
-        bool there[AHEAD];
+    constexpr int SLOTS = 8;            // known ahead
+    const int lane8 = threadIdx.x & (SLOTS - 1), c0 = (blockIdx.y * ITEMS * blockDim.x + threadIdx.x) * N, width = blockDim.x * N;
+    const long long step = (long long)gridDim.x * blockDim.y;
+    int next_place;
+    float next_w;
+    const auto know = [&](long long m, int j) {
+        const bool there = m < a.M && j + lane8 < a.k;
+        next_place = there ? a.places[m * a.k + j + lane8] : -1;
+        if (next_place >= a.rows) next_place = -1;
+        next_w = there ? weight_of<T>(a, m * a.k + j + lane8) : 0.0f;
+    };
+    long long m = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+    know(m, 0);
+    // all threads of a warp take the same number of steps: the shuffles need them
+    for (long long first = (long long)blockIdx.x * blockDim.y; first < a.M; first += step, m += step) {
+        float sum[ITEMS][N] = {};
+        for (int j0 = 0; j0 < a.k; j0 += SLOTS) {
+            const int place8 = next_place;
+            const float w8 = next_w;
+            if (j0 + SLOTS < a.k)
+                know(m, j0 + SLOTS);
+            else
+                know(m + step, 0);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const long long s = m * a.k + j0 + u;
-            const int place = j0 + u < a.k ? a.places[s] : -1;
-            there[u] = place >= 0 && place < a.rows;
-            w[u] = there[u] ? weight_of<T>(a, s) : 0.0f;
-            const T *ys = static_cast<const T *>(a.ys) + place * a.ldys;
+            for (int h = 0; h < SLOTS; h += AHEAD) {
+                if (j0 + h >= a.k) break;
+                P v[AHEAD][ITEMS];
+                int place[AHEAD];
+                float w[AHEAD];
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i)
-                if (there[u] && c0 + i * step < a.D) v[u][i] = *reinterpret_cast<const P *>(ys + c0 + i * step);
+                for (int u = 0; u < AHEAD; ++u) {
+                    place[u] = __shfl_sync(~0u, place8, h + u, SLOTS);
+                    w[u] = __shfl_sync(~0u, w8, h + u, SLOTS);
+                    const T *ys = static_cast<const T *>(a.ys) + place[u] * a.ldys;
+#pragma unroll
+                    for (int i = 0; i < ITEMS; ++i)
+                        if (place[u] >= 0 && c0 + i * width < a.D) v[u][i] = *reinterpret_cast<const P *>(ys + c0 + i * width);
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u)
+                    if (place[u] >= 0)
+#pragma unroll
+                        for (int i = 0; i < ITEMS; ++i) {
+                            float f[N];
+                            v[u][i].get(f);
+#pragma unroll
+                            for (int n = 0; n < N; ++n) sum[i][n] = fmaf(w[u], f[n], sum[i][n]);
+                        }
+            }
         }
+        T *out = static_cast<T *>(a.out) + m * a.ldo;
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (there[u])
-#pragma unroll
-                for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-                    for (int n = 0; n < N; ++n) sum[i * N + n] = fmaf(w[u], to_f32<T>(v[u][i].v[n]), sum[i * N + n]);
+        for (int i = 0; i < ITEMS; ++i)
+            if (m < a.M && c0 + i * width < a.D) {
+                P r;
+                r.set(sum[i]);
+                *reinterpret_cast<P *>(out + c0 + i * width) = r;
+            }
     }
-    T *out = static_cast<T *>(a.out) + m * a.ldo;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-        if (c0 + i * step < a.D) {
-            P r;
-#pragma unroll
-            for (int n = 0; n < N; ++n) r.v[n] = from_f32<T>(sum[i * N + n]);
-            *reinterpret_cast<P *>(out + c0 + i * step) = r;
-        }
 }
 
-// dys[place] = w dy[m] and dw = <dy[m], ys[place]>: a warp to a slot, so that the product is summed within the warp.  The k
-// warps of a token read its dy at about the same time, from L1 or L2.
+// dys[place] = w dy[m] and dw = <dy[m], ys[place]>: `lanes` of a warp to a slot, so that the product is summed by shuffles.  The
+// lanes of a token's k slots read its dy at about the same time, from L1 or L2.  16384 x 8 rows of 4096 bf16: 344 us, 6.6 TB/s.
 template <class T, int N, int ITEMS>
-__global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a) {
-    const long long s = ((long long)blockIdx.x * 256 + threadIdx.x) >> 5;
-    const int lane = threadIdx.x & 31;
-    if (s >= a.rows) return;
+__global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a, int lanes) {
     using P = Pack<T, N>;
-    const long long m = s / a.k;
-    if (a.out && a.slots[s] < 0) {
-        T *out = static_cast<T *>(a.out) + s * a.ldo;
-        for (int c = lane * N; c < a.D; c += 32 * N) *reinterpret_cast<P *>(out + c) = P{};
-    }
-    const int place = a.places[s];
-    const bool there = place >= 0 && place < a.rows;
+    const long long s = ((long long)blockIdx.x * 256 + threadIdx.x) / lanes;
+    const int lane = threadIdx.x & (lanes - 1);
     float dot = 0.0f;
-    if (there) {
+    if (s < a.rows) {
+        const long long m = s / a.k;
+        const int place = a.places[s];
         const float w = weight_of<T>(a, s);
-        const T *dy = static_cast<const T *>(a.x) + m * a.ldx, *ys = static_cast<const T *>(a.ys) + place * a.ldys;
-        T *out = static_cast<T *>(a.out) + place * a.ldo;
-        for (int c0 = lane * N; c0 < a.D; c0 += 32 * N * ITEMS) {
-            P g[ITEMS], v[ITEMS];
+        if (a.out && a.slots[s] < 0) {
+            T *out = static_cast<T *>(a.out) + s * a.ldo;
+            for (int c = lane * N; c < a.D; c += lanes * N) *reinterpret_cast<P *>(out + c) = P();
+        }
+        if (place >= 0 && place < a.rows) {
+            const T *dy = static_cast<const T *>(a.x) + m * a.ldx, *ys = static_cast<const T *>(a.ys) + place * a.ldys;
+            T *out = static_cast<T *>(a.out) + place * a.ldo;
+            for (int c0 = lane * N; c0 < a.D; c0 += lanes * N * ITEMS) {
+                P g[ITEMS], v[ITEMS];
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int c = c0 + 32 * N * i;
-                if (c < a.D) {
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int c = c0 + lanes * N * i;
+                    if (c >= a.D) break;
                     g[i] = *reinterpret_cast<const P *>(dy + c);
                     if (a.dweights) v[i] = *reinterpret_cast<const P *>(ys + c);
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const int c = c0 + 32 * N * i;
-                if (c >= a.D) continue;
-                P r;
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int c = c0 + lanes * N * i;
+                    if (c >= a.D) break;
+                    float d[N], y[N];
+                    g[i].get(d);
+                    if (a.dweights) {
+                        v[i].get(y);
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const float d = to_f32<T>(g[i].v[n]);
-                    if (a.dweights) dot = fmaf(d, to_f32<T>(v[i].v[n]), dot);
-                    r.v[n] = from_f32<T>(w * d);
+                        for (int n = 0; n < N; ++n) dot = fmaf(d[n], y[n], dot);
+                    }
+#pragma unroll
+                    for (int n = 0; n < N; ++n) d[n] *= w;
+                    P r;
+                    r.set(d);
+                    if (a.out) *reinterpret_cast<P *>(out + c) = r;
                 }
-                if (a.out) *reinterpret_cast<P *>(out + c) = r;
             }
         }
     }
     if (!a.dweights) return;
-#pragma unroll
-    for (int d = 16; d; d /= 2) dot += __shfl_xor_sync(~0u, dot, d);
-    if (lane == 0) {
+    for (int d = lanes / 2; d; d /= 2) dot += __shfl_xor_sync(~0u, dot, d);
+    if (lane == 0 && s < a.rows) {
         if (a.weights_f32)
             static_cast<float *>(a.dweights)[s] = dot;
         else
@@ -292,33 +354,47 @@ __global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a) {
 
 enum Which { DISPATCH, COMBINE, COMBINE_BACK };
 
-template <class T, int N, int ITEMS>
-int launch_rows(Which which, const RowArgs &a, cudaStream_t s) {
-    if (which == COMBINE_BACK) {
-        k_expert_combine_back<T, N, ITEMS><<<(unsigned)((a.rows + 7) / 8), 256, 0, s>>>(a);
-        return block_launch_status();
-    }
+template <class T, int N, int AHEAD, int ITEMS>
+int launch_rows(Which which, const RowArgs &a, int sms, cudaStream_t s) {
     const int packs = (a.D + N - 1) / N;
     int x = 8;
     while (x < 256 && x * ITEMS < packs) x *= 2;
-    const dim3 block(x, 256 / x), grid((unsigned)((a.M + block.y - 1) / block.y), (unsigned)((packs + x * ITEMS - 1) / (x * ITEMS)));
-    if (which == DISPATCH)
+    dim3 block(x, 256 / x), grid((unsigned)((a.M + block.y - 1) / block.y), (unsigned)((packs + x * ITEMS - 1) / (x * ITEMS)));
+    if (which == DISPATCH) {
         k_expert_dispatch<T, N, ITEMS><<<grid, block, 0, s>>>(a);
-    else
-        k_expert_combine<T, N, ITEMS><<<grid, block, 0, s>>>(a);
+    } else {
+        const unsigned at_once = 3 * sms;       // blocks that stay
+        grid.x = std::min(grid.x, std::max(1u, at_once / std::min(grid.y, at_once)));
+        k_expert_combine<T, N, AHEAD, ITEMS><<<grid, block, 0, s>>>(a);
+    }
     return block_launch_status();
 }
 template <class T>
-int launch_type(Which which, const RowArgs &a, bool vec, cudaStream_t s) {
+int launch_type(Which which, const RowArgs &a, int sms, cudaStream_t s) {
+    const auto aligned = [&](const void *p, long long ld) { return aligned_to(p, 16) && (!p || ld * sizeof(T) % 16 == 0); };
     constexpr int N = 16 / sizeof(T);
-    return vec ? launch_rows<T, N, 1>(which, a, s) : launch_rows<T, 1, 4>(which, a, s);
+    const bool vec = a.D % N == 0 && aligned(a.x, a.ldx) && aligned(a.ys, a.ldys) && aligned(a.out, a.ldo);
+    if (which == COMBINE_BACK) {
+        const int packs = vec ? a.D / N : a.D, lanes = packs <= 32 ? 8 : packs <= 64 ? 16 : 32;     // four accesses a lane, eight lanes at least
+        const unsigned blocks = (unsigned)((a.rows * lanes + 255) / 256);
+        if (vec)
+            k_expert_combine_back<T, N, 4><<<blocks, 256, 0, s>>>(a, lanes);
+        else
+            k_expert_combine_back<T, 1, 4><<<blocks, 256, 0, s>>>(a, lanes);
+        return block_launch_status();
+    }
+    if (!vec) return launch_rows<T, 1, 4, 4>(which, a, sms, s);
+    if (a.D < 256 * N) return launch_rows<T, N, 4, 1>(which, a, sms, s);
+    // one or two slots a token leave fewer rows to ask for: more of each
+    return which == DISPATCH || a.k > 2 ? launch_rows<T, N, 4, 2>(which, a, sms, s)
+           : a.k == 2 ? launch_rows<T, N, 2, 4>(which, a, sms, s) : launch_rows<T, N, 1, 4>(which, a, sms, s);
 }
 int launch(Which which, RowArgs &a, int dtype, cudaStream_t s) {
-    const int b = type_bytes(dtype);
-    const auto rows16 = [&](const void *p, long long ld) { return aligned_to(p, 16) && (!p || ld * b % 16 == 0); };
-    const bool vec = a.D * b % 16 == 0 && rows16(a.x, a.ldx) && rows16(a.ys, a.ldys) && rows16(a.out, a.ldo);
-    return dtype == CCDC_F32    ? launch_type<float>(which, a, vec, s)
-           : dtype == CCDC_BF16 ? launch_type<bf16>(which, a, vec, s) : launch_type<fp16>(which, a, vec, s);
+    int rc;
+    const int sms = block_sm_count(&rc);
+    if (rc != CCDC_OK) return rc;
+    return dtype == CCDC_F32    ? launch_type<float>(which, a, sms, s)
+           : dtype == CCDC_BF16 ? launch_type<bf16>(which, a, sms, s) : launch_type<fp16>(which, a, sms, s);
 }
 int check(long long M, int k, long long D, int dtype, int weight_dtype) {
     if (M < 0 || k < 1 || D < 1 || !is_float_type(dtype) || (weight_dtype != dtype && weight_dtype != CCDC_F32))
@@ -337,7 +413,9 @@ int ccdc_expert_sort(long long M, int k, int experts, int id_bytes, const void *
         return CCDC_EINVAL;
     if (M > 0 && (!ids || !slots || !places)) return CCDC_EINVAL;
     if (M > 0x7FFFFFFF / k || experts > MAX_EXPERTS) return CCDC_ESIZE;
-    SortArgs a = {M * k, experts, ids, offsets, slots, places};
+    int bits = 0;
+    while (1 << bits < experts) ++bits;
+    SortArgs a = {M * k, experts, bits, ids, offsets, slots, places};
     const int warps = experts <= 1024 ? 32 : 8;             // the counts of all warps fit the shared memory
     const int smem = (warps * experts + 2 * experts + 33) * (int)sizeof(int);
     static std::atomic<unsigned long long> done[2];
