@@ -851,6 +851,8 @@ def _order(order, like, rows=None):
     import torch
 
     slots, places = order.slots, order.places
+    if places.dim() != 2:
+        raise ValueError("order.places: [tokens][k] expected")
     M, k = places.shape
     ps, pp = _vector(slots, "order.slots", like, M * k, torch.int32), _vector(places, "order.places", like, M * k, torch.int32)
     if rows is not None and rows != M:
@@ -870,11 +872,21 @@ def expert_sort(ids, n_experts, offsets=None, slots=None, places=None, stream=No
     size = _ids(ids, "ids")
     M, k = ids.shape
     i32 = torch.int32
-    offsets = ids.new_empty(n_experts + 1, dtype=i32) if offsets is None else offsets
-    slots = ids.new_empty(M * k, dtype=i32) if slots is None else slots
-    places = ids.new_empty((M, k), dtype=i32) if places is None else places
-    status = lib().ccdc_expert_sort(M, k, n_experts, size, ids.data_ptr(), _vector(offsets, "offsets", ids, n_experts + 1, i32),
-                                    _vector(slots, "slots", ids, M * k, i32), _vector(places, "places", ids, M * k, i32),
+    if offsets is None:
+        offsets = ids.new_empty(n_experts + 1, dtype=i32)
+    else:
+        _vector(offsets, "offsets", ids, n_experts + 1, i32)
+    if slots is None:
+        slots = ids.new_empty(M * k, dtype=i32)
+    else:
+        _vector(slots, "slots", ids, M * k, i32)
+    if places is None:
+        places = ids.new_empty((M, k), dtype=i32)
+    else:
+        _vector(places, "places", ids, M * k, i32)
+        if places.shape != ids.shape:
+            raise ValueError(f"places: shape {tuple(ids.shape)} expected, got {tuple(places.shape)}")
+    status = lib().ccdc_expert_sort(M, k, n_experts, size, ids.data_ptr(), offsets.data_ptr(), slots.data_ptr(), places.data_ptr(),
                                     _handle(ids))
     if status:
         _check(status, "ccdc_expert_sort")
