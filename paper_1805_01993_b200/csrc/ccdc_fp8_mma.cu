@@ -446,6 +446,9 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
                 };
                 fetch(b0, 1);
                 fetch(b0 + 1, 2);
+                // Two blocks to a turn where registers allow, so that the scales need not be moved on, which waits for them (200 rows
+                // over 64 weights: 77 and 72 us).
+#pragma unroll(NT <= 32 ? 2 : 1)
                 for (int b = b0; b < b1; ++b) {
                     float *s = reinterpret_cast<float *>(own_bytes) + buffer * S::COLS;
                     buffer ^= 1;
