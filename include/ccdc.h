@@ -630,10 +630,13 @@ int ccdc_expert_combine_backward(long long M, int k, long long D, int dtype, con
  *   gradient from stats    loss NULL, dloss [M] binary32, dlogits (row stride
  *                          lddz), the stats of the same inputs
  *   both in one pass       loss, dloss and dlogits; stats may be NULL
- * dlogits may be the logits themselves (same stride).  1e-6 <= T <= 1e6;
+ * dlogits may be the logits themselves (same stride).  Rows are read in pieces
+ * of 16 bytes: up to 15 bytes beside a row's ends are read, and not used.  A
+ * row's sums depend on M in their order (few rows are cut into more parts).
+ * 1e-6 <= T <= 1e6;
  * k <= 1024, rows of at most 1408 KiB (CCDC_ESIZE). */
 int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits, long long ldz, int id_bytes, const void *ids,
-                 int value_dtype, const void *values, const float *teacher_lse, float temperature, const float *dloss, float *loss,
+                 int value_dtype, const void *values, const float *teacher_lse, double temperature, const float *dloss, float *loss,
                  void *stats, void *dlogits, long long lddz, void *stream);
 
 /* 8-bit products with a scale for each block of 128.  A tensor is e4m3 values

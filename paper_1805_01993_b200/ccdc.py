@@ -108,7 +108,7 @@ SIGNATURES = {
     "ccdc_expert_dispatch": (_I, [_LL, _I, _LL, _I, _P, _LL, _P, _P, _P, _LL, _P]),
     "ccdc_expert_combine": (_I, [_LL, _I, _LL, _I, _P, _LL, _P, _P, _I, _P, _LL, _P]),
     "ccdc_expert_combine_backward": (_I, [_LL, _I, _LL, _I, _P, _LL, _P, _LL, _P, _P, _P, _I, _P, _LL, _P, _P]),
-    "ccdc_distill": (_I, [_LL, _LL, _I, _I, _P, _LL, _I, _P, _I, _P, _P, _FL, _P, _P, _P, _P, _LL, _P]),
+    "ccdc_distill": (_I, [_LL, _LL, _I, _I, _P, _LL, _I, _P, _I, _P, _P, _DB, _P, _P, _P, _P, _LL, _P]),
     "ccdc_quantize_fp8": (_I, [_LL, _LL, _LL, _I, _I, _P, _LL, _LL, _P, _LL, _LL, _P, _LL, _LL, _LL, _P]),
     "ccdc_matmul_fp8": (_I, [_LL, _LL, _LL, _I, _P, _LL, _P, _LL, _LL, _P, _LL, _LL, _P, _P, _P, _I, _LL, _P]),
     "ccdc_strerror": (ctypes.c_char_p, [_I]),

@@ -583,10 +583,10 @@ int by_type(DistillArgs &a, int dtype, cudaStream_t s) {
 extern "C" {
 
 int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits, long long ldz, int id_bytes, const void *ids,
-                 int value_dtype, const void *values, const float *teacher_lse, float temperature, const float *dloss, float *loss,
+                 int value_dtype, const void *values, const float *teacher_lse, double temperature, const float *dloss, float *loss,
                  void *stats, void *dlogits, long long lddz, void *stream) {
     if (M < 0 || V < 1 || k < 1 || !is_float_type(dtype) || (value_dtype != dtype && value_dtype != CCDC_F32) ||
-        (id_bytes != 4 && id_bytes != 8) || !(temperature >= 1e-6f && temperature <= 1e6f))
+        (id_bytes != 4 && id_bytes != 8) || !(temperature >= 1e-6 && temperature <= 1e6))
         return CCDC_EINVAL;
     if (V * type_bytes(dtype) > MOST_PART * MAX_CLUSTER || V > 0x7FFFFFFF || k > MAX_TOP) return CCDC_ESIZE;
     if (M == 0) return CCDC_OK;
@@ -596,7 +596,7 @@ int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits,
     a.M = M, a.V = V, a.ldz = ldz, a.lddz = lddz, a.k = k, a.id_bytes = id_bytes, a.values_f32 = value_dtype == CCDC_F32;
     a.z = logits, a.ids = ids, a.values = values, a.lse = teacher_lse, a.dloss = dloss, a.loss = loss;
     a.stats = static_cast<float2 *>(stats), a.dz = dlogits;
-    a.inv_t = 1.0 / (double)temperature, a.scale = (float)(1.4426950408889634 / (double)temperature);
+    a.inv_t = 1.0 / temperature, a.scale = (float)(1.4426950408889634 / temperature);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return !dlogits ? by_type<true, false>(a, dtype, s) : loss ? by_type<true, true>(a, dtype, s) : by_type<false, true>(a, dtype, s);
 }
