@@ -1059,11 +1059,12 @@ def _bytes_rows(t, name, like=None):
     """row stride of an e4m3 matrix whose rows start at multiples of 16 bytes"""
     import torch
 
-    if t.dtype is not torch.float8_e4m3fn or t.dim() not in (2, 3) or (t.stride(-1) != 1 and t.shape[-1] > 1):
+    shape, strides = t.shape, t.stride()
+    if t.dtype is not torch.float8_e4m3fn or not 2 <= len(shape) <= 3 or (strides[-1] != 1 and shape[-1] > 1):
         raise ValueError(f"{name}: float8_e4m3fn with contiguous columns expected")
     if not t.is_cuda if like is None else t.get_device() != like.get_device():
         raise ValueError(f"{name}: a tensor on {'a CUDA device' if like is None else like.device} expected")
-    ld = t.stride(-2) if t.shape[-2] > 1 else -(-t.shape[-1] // 16) * 16
+    ld = strides[-2] if shape[-2] > 1 else (shape[-1] + 15) // 16 * 16
     if t.data_ptr() % 16 or ld % 16:
         raise ValueError(f"{name}: rows must start at multiples of 16 bytes")
     return ld
@@ -1079,38 +1080,40 @@ def quantize_fp8(x, block_rows=1, out=None, scales=None, stream=None):
     if ctx is not None:
         with ctx:
             return quantize_fp8(x, block_rows, out, scales)
-    if block_rows not in (1, FP8_BLOCK):
+    if block_rows != 1 and block_rows != FP8_BLOCK:
         raise ValueError("block_rows is 1 or 128")
-    if x.dim() == 3 and block_rows == FP8_BLOCK:
-        first = x[0] if x.shape[0] else x.new_empty(x.shape[1:])
-        groups, group, ldx = x.shape[0], x.stride(0), _rows(first, "x")
+    shape, f32 = x.shape, torch.float32
+    if len(shape) == 3 and block_rows == FP8_BLOCK:
+        groups, group = shape[0], x.stride(0)
+        ldx = _rows(x[0] if groups else x.new_empty(shape[1:]), "x")
     else:
         groups, group, ldx = 1, 0, _rows(x, "x")
     code = _block_dtype(x)
-    M, K = x.shape[-2:]
-    kb = -(-K // FP8_BLOCK)
+    M, K = shape[-2:]
+    kb, ldq = (K + 127) // 128, (K + 15) // 16 * 16
     if out is None:
-        ldq = -(-K // 16) * 16
-        out = x.new_empty((*x.shape[:-1], ldq), dtype=torch.float8_e4m3fn)
+        out = x.new_empty(shape if ldq == K else (*shape[:-1], ldq), dtype=torch.float8_e4m3fn)
+        q_group = M * ldq
         if ldq != K:
             out = out[..., :K]
     else:
-        if out.shape != x.shape:
-            raise ValueError(f"out: shape {tuple(x.shape)} expected, got {tuple(out.shape)}")
+        if out.shape != shape:
+            raise ValueError(f"out: shape {tuple(shape)} expected, got {tuple(out.shape)}")
         ldq = _bytes_rows(out, "out", x)
-    if block_rows == 1:
-        shape = M, kb
-        if scales is None:
-            scales = x.new_empty((kb, M), dtype=torch.float32).t()
+        q_group = out.stride(0)
+    if scales is None:
+        if block_rows == 1:
+            scales, strides = x.new_empty((kb, M), dtype=f32).t(), (0, 1, M)
+        else:
+            nb = (M + 127) // 128
+            scales, strides = x.new_empty((*shape[:-2], nb, kb), dtype=f32), (nb * kb, kb, 1)
     else:
-        shape = *x.shape[:-2], -(-M // FP8_BLOCK), kb
-        if scales is None:
-            scales = x.new_empty(shape, dtype=torch.float32)
-    if scales.shape != shape or scales.dtype is not torch.float32 or scales.get_device() != x.get_device():
-        raise ValueError(f"scales: float32 {shape} on {x.device} expected")
-    strides = scales.stride() if scales.dim() == 3 else (0, *scales.stride())
-    status = lib().ccdc_quantize_fp8(groups, M, K, block_rows, code, x.data_ptr(), group, ldx, out.data_ptr(),
-                                     out.stride(0) if x.dim() == 3 else 0, ldq, scales.data_ptr(), *strides, _handle(x))
+        want = (M, kb) if block_rows == 1 else (*shape[:-2], (M + 127) // 128, kb)
+        if scales.shape != want or scales.dtype is not f32 or scales.get_device() != x.get_device():
+            raise ValueError(f"scales: float32 {want} on {x.device} expected")
+        strides = scales.stride() if len(want) == 3 else (0, *scales.stride())
+    status = lib().ccdc_quantize_fp8(groups, M, K, block_rows, code, x.data_ptr(), group, ldx, out.data_ptr(), q_group, ldq,
+                                     scales.data_ptr(), *strides, _handle(x))
     if status:
         _check(status, "ccdc_quantize_fp8")
     return out, scales
@@ -1127,22 +1130,23 @@ def matmul_fp8(x, x_scales, w, w_scales, *, offsets=None, out_dtype=None, out=No
         with ctx:
             return matmul_fp8(x, x_scales, w, w_scales, offsets=offsets, out_dtype=out_dtype, out=out)
     ldx, ldw = _bytes_rows(x, "x"), _bytes_rows(w, "w", x)
-    f32, experts = torch.float32, 1
-    if x.dim() != 2 or w.dim() != (2 if offsets is None else 3) or w.shape[-1] != x.shape[1]:
-        raise ValueError(f"x [M][K] and w [N][K] (with offsets [E][N][K]) expected, got {tuple(x.shape)} and {tuple(w.shape)}")
-    M, K = x.shape
-    N, kb = w.shape[-2], -(-K // FP8_BLOCK)
-    po, expert = None, 0
-    if offsets is not None:
-        experts, expert = w.shape[0], w.stride(0)
+    f32, sx, sw = torch.float32, x.shape, w.shape
+    if len(sx) != 2 or len(sw) != (2 if offsets is None else 3) or sw[-1] != sx[1]:
+        raise ValueError(f"x [M][K] and w [N][K] (with offsets [E][N][K]) expected, got {tuple(sx)} and {tuple(sw)}")
+    M, K = sx
+    N, kb = sw[-2], (K + 127) // 128
+    if offsets is None:
+        experts, expert, po, want = 1, 0, None, ((N + 127) // 128, kb)
+    else:
+        experts, expert = sw[0], w.stride(0)
         po = _vector(offsets, "offsets", x, experts + 1, torch.int32)
+        want = experts, (N + 127) // 128, kb
         if experts > 1 and expert % 16:
             raise ValueError("w: matrices must start at multiples of 16 bytes")
     if x_scales.shape != (M, kb) or x_scales.dtype is not f32 or x_scales.get_device() != x.get_device():
         raise ValueError(f"x_scales: float32 {(M, kb)} on {x.device} expected")
-    shape = (*w.shape[:-2], -(-N // FP8_BLOCK), kb)
-    if w_scales.shape != shape:
-        raise ValueError(f"w_scales: shape {shape} expected, got {tuple(w_scales.shape)}")
+    if w_scales.shape != want:
+        raise ValueError(f"w_scales: shape {want} expected, got {tuple(w_scales.shape)}")
     pws = _vector(w_scales, "w_scales", x, w_scales.numel(), f32)
     if out is None:
         out, ldo = x.new_empty((M, N), dtype=torch.bfloat16 if out_dtype is None else out_dtype), N

@@ -341,9 +341,8 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
         Running r = {-INFINITY, 0.0f};
         if (walks) {
             if constexpr (LOSS) {
-                // a group's maximum first: one rise of the reference for all its pieces
-                const auto use = [&](int g) {
-                    const int begin = tid + g * group * THREADS, end = min(own.count, begin + group * THREADS);
+                // the pieces' maximum first: one rise of the reference for all of them
+                const auto use = [&](int begin, int end) {
                     Largest<T> largest;
                     for (int p = begin; p < end; p += THREADS) {
                         if (own.edge(p)) row[p] = own.inside(a, row[p], p);
@@ -373,11 +372,14 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
                     else
                         sum_up(std::false_type());
                 };
-                copies_landed<3>(), use(0), copies_landed<2>(), use(1), copies_landed<1>(), use(2), copies_landed<0>(), use(3);
-                if constexpr (!GRAD) {
-                    for (int g = 0; g < GROUPS; ++g) {
-                        for (int p = tid + g * group * THREADS; p < min(next_count, tid + (g + 1) * group * THREADS); p += THREADS)
-                            copy_piece(row + p, next.from + p);
+                // group by group in either form, so that the loss has the same bits with and without the gradient
+                if constexpr (GRAD) copies_landed<0>();
+                for (int g = 0; g < GROUPS; ++g) {
+                    const int begin = tid + g * group * THREADS, end = begin + group * THREADS;
+                    if constexpr (!GRAD) copies_landed<GROUPS - 1>();
+                    use(begin, min(own.count, end));
+                    if constexpr (!GRAD) {      // the next row's copies take the place of a group's as soon as it has been used
+                        for (int p = begin; p < min(next_count, end); p += THREADS) copy_piece(row + p, next.from + p);
                         copies_end();
                     }
                 }
