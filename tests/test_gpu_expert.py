@@ -30,7 +30,8 @@ def order_of(ids, E):
     slots, places = np.full(flat.size, -1), np.full(flat.size, -1)
     slots[:len(by)] = by
     places[by] = np.arange(len(by))
-    return np.array([sum(1 for s in inside if flat[s] < e) for e in range(E + 1)]), slots, places.reshape(np.shape(ids))
+    below = np.searchsorted(np.sort(flat[inside]), np.arange(E + 1))        # slots of experts below each
+    return below, slots, places.reshape(np.shape(ids))
 
 
 def draw_ids(rng, M, k, E, drop=0.0):
@@ -52,7 +53,7 @@ def f64(t):
 # one warp's slots, a block's, a cluster's (more than 4096 slots); experts at and beyond the warps' number and at the limit
 @pytest.mark.parametrize("M,k,E,drop", [(1, 1, 1, 0), (1, 8, 128, 0), (5, 3, 2, 0.5), (32, 1, 4, 0), (33, 2, 33, 0.1), (100, 7, 1000, 0),
                                         (1024, 4, 1025, 0.2), (1025, 4, 64, 0.1), (2049, 3, 7, 0.9), (3001, 5, 4096, 0.1), (700, 6, 1, 0),
-                                        (300, 16, 1024, 1.0)])
+                                        (300, 16, 1024, 1.0), (20001, 2, 100, 0.1), (9000, 4, 4096, 0.3)])
 @pytest.mark.parametrize("kind", [torch.int32, torch.int64])
 def test_sort(ccdc, M, k, E, drop, kind):
     ids = draw_ids(np.random.default_rng(M + E), M, k, E, drop)
