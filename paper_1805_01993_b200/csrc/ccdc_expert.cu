@@ -153,8 +153,10 @@ __global__ void __launch_bounds__(1024) k_expert_sort(SortArgs a) {
 }
 
 // ------------------------------------------------------------- rows there and back
-// Rows are read and written N elements at a time: 16 bytes where all rows are aligned to them, else one.  (Cutting whole pieces
-// out of rows that start elsewhere was slower for its registers: 8192 x 8 rows of 1001 bf16 there, 42 us one by one and 68 cut.)
+// Rows are read and written N elements at a time: 16 bytes where the sorted rows are aligned to them, else one.  The tokens' rows,
+// which are fewer, may then still start anywhere (APART: a padded batch), and go element by element into and out of the same
+// registers.  (Cutting whole pieces out of rows that start elsewhere was slower for its registers: 8192 x 8 rows of 1001 bf16
+// there, 42 us one by one and 68 cut.)
 // Words stay as they lie in memory until they are used: as elements, 16-bit ones would take a register each.
 template <class T, int N>
 struct Pack {
@@ -164,6 +166,32 @@ struct Pack {
             f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y), f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
         } else {
             unpack8<T>(Eight<T>{{v}}, f);
+        }
+    }
+    template <bool APART>
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (!APART) {
+            v = *reinterpret_cast<const uint4 *>(p);
+        } else if constexpr (sizeof(T) == 4) {
+            const uint32_t *w = reinterpret_cast<const uint32_t *>(p);
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+            v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        }
+    }
+    template <bool APART>
+    __device__ __forceinline__ void store(T *p) const {
+        if constexpr (!APART) {
+            *reinterpret_cast<uint4 *>(p) = v;
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if constexpr (sizeof(T) == 4)
+                    reinterpret_cast<uint32_t *>(p)[i] = w[i];
+                else
+                    reinterpret_cast<uint16_t *>(p)[2 * i] = (uint16_t)w[i], reinterpret_cast<uint16_t *>(p)[2 * i + 1] = (uint16_t)(w[i] >> 16);
         }
     }
     __device__ __forceinline__ void set(const float (&f)[N]) {
@@ -176,6 +204,10 @@ struct Pack {
 template <class T>
 struct Pack<T, 1> {
     T v = from_f32<T>(0.0f);
+    template <bool APART>
+    __device__ __forceinline__ void load(const T *p) { v = *p; }
+    template <bool APART>
+    __device__ __forceinline__ void store(T *p) const { *p = v; }
     __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32<T>(v); }
     __device__ __forceinline__ void set(const float (&f)[1]) { v = from_f32<T>(f[0]); }
 };
@@ -199,7 +231,7 @@ __device__ __forceinline__ float weight_of(const RowArgs &a, long long slot) {
 // xs[place] = x[m] for the token's places, and zeros in as many of the rows behind the last expert's.  A token's row is read
 // once.  blockDim.x threads to a row, blockDim.y tokens to a block, ITEMS accesses a thread.  16384 x 8 rows of 4096 bf16: 193 us,
 // 6.3 TB/s.
-template <class T, int N, int ITEMS>
+template <class T, int N, int ITEMS, bool APART>
 __global__ void __launch_bounds__(256) k_expert_dispatch(RowArgs a) {
     const long long m = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     if (m >= a.M) return;
@@ -209,7 +241,7 @@ __global__ void __launch_bounds__(256) k_expert_dispatch(RowArgs a) {
     P v[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
-        if (c0 + i * step < a.D) v[i] = *reinterpret_cast<const P *>(x + c0 + i * step);
+        if (c0 + i * step < a.D) v[i].template load<APART>(x + c0 + i * step);
     for (int j = 0; j < a.k; ++j) {
         const long long s = m * a.k + j;
         const int place = a.places[s];
@@ -233,7 +265,7 @@ __global__ void __launch_bounds__(256) k_expert_dispatch(RowArgs a) {
 // bytes in flight, since a row's address has to be read first.  So blocks stay and take token after token: eight lanes ask for the
 // next slots' places and weights while this token's rows are on their way, and share them by shuffles; AHEAD rows of ITEMS
 // accesses a thread are asked for together.  16384 x 8 rows of 4096 bf16: 188 us, 6.4 TB/s (437 us a token a block).
-template <class T, int N, int AHEAD, int ITEMS>
+template <class T, int N, int AHEAD, int ITEMS, bool APART>
 __global__ void __launch_bounds__(256, 3) k_expert_combine(RowArgs a) {
     using P = Pack<T, N>;
     constexpr int SLOTS = 8;            // known ahead
@@ -292,14 +324,14 @@ __global__ void __launch_bounds__(256, 3) k_expert_combine(RowArgs a) {
             if (m < a.M && c0 + i * width < a.D) {
                 P r;
                 r.set(sum[i]);
-                *reinterpret_cast<P *>(out + c0 + i * width) = r;
+                r.template store<APART>(out + c0 + i * width);
             }
     }
 }
 
 // dys[place] = w dy[m] and dw = <dy[m], ys[place]>: `lanes` of a warp to a slot, so that the product is summed by shuffles.  The
 // lanes of a token's k slots read its dy at about the same time, from L1 or L2.  16384 x 8 rows of 4096 bf16: 344 us, 6.6 TB/s.
-template <class T, int N, int ITEMS>
+template <class T, int N, int ITEMS, bool APART>
 __global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a, int lanes) {
     using P = Pack<T, N>;
     const long long s = ((long long)blockIdx.x * 256 + threadIdx.x) / lanes;
@@ -322,7 +354,7 @@ __global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a, int lane
                 for (int i = 0; i < ITEMS; ++i) {
                     const int c = c0 + lanes * N * i;
                     if (c >= a.D) break;
-                    g[i] = *reinterpret_cast<const P *>(dy + c);
+                    g[i].template load<APART>(dy + c);
                     if (a.dweights) v[i] = *reinterpret_cast<const P *>(ys + c);
                 }
 #pragma unroll
@@ -357,40 +389,47 @@ __global__ void __launch_bounds__(256) k_expert_combine_back(RowArgs a, int lane
 
 enum Which { DISPATCH, COMBINE, COMBINE_BACK };
 
-template <class T, int N, int AHEAD, int ITEMS>
+template <class T, int N, int AHEAD, int ITEMS, bool APART>
 int launch_rows(Which which, const RowArgs &a, int sms, cudaStream_t s) {
     const int packs = (a.D + N - 1) / N;
     int x = 8;
     while (x < 256 && x * ITEMS < packs) x *= 2;
     dim3 block(x, 256 / x), grid((unsigned)((a.M + block.y - 1) / block.y), (unsigned)((packs + x * ITEMS - 1) / (x * ITEMS)));
     if (which == DISPATCH) {
-        k_expert_dispatch<T, N, ITEMS><<<grid, block, 0, s>>>(a);
+        k_expert_dispatch<T, N, ITEMS, APART><<<grid, block, 0, s>>>(a);
     } else {
         const unsigned at_once = 3 * sms;       // blocks that stay
         grid.x = std::min(grid.x, std::max(1u, at_once / std::min(grid.y, at_once)));
-        k_expert_combine<T, N, AHEAD, ITEMS><<<grid, block, 0, s>>>(a);
+        k_expert_combine<T, N, AHEAD, ITEMS, APART><<<grid, block, 0, s>>>(a);
     }
     return block_launch_status();
 }
-template <class T>
+template <class T, int N, bool APART>
 int launch_type(Which which, const RowArgs &a, int sms, cudaStream_t s) {
-    const auto aligned = [&](const void *p, long long ld) { return aligned_to(p, 16) && (!p || ld * sizeof(T) % 16 == 0); };
-    constexpr int N = 16 / sizeof(T);
-    const bool vec = a.D % N == 0 && aligned(a.x, a.ldx) && aligned(a.ys, a.ldys) && aligned(a.out, a.ldo);
     if (which == COMBINE_BACK) {
-        const int packs = vec ? a.D / N : a.D, lanes = packs <= 32 ? 8 : packs <= 64 ? 16 : 32;     // four accesses a lane, eight lanes at least
-        const unsigned blocks = (unsigned)((a.rows * lanes + 255) / 256);
-        if (vec)
-            k_expert_combine_back<T, N, 4><<<blocks, 256, 0, s>>>(a, lanes);
-        else
-            k_expert_combine_back<T, 1, 4><<<blocks, 256, 0, s>>>(a, lanes);
+        // four accesses a lane, eight lanes at least
+        const int packs = (a.D + N - 1) / N, lanes = packs <= 32 ? 8 : packs <= 64 ? 16 : 32;
+        k_expert_combine_back<T, N, 4, APART><<<(unsigned)((a.rows * lanes + 255) / 256), 256, 0, s>>>(a, lanes);
         return block_launch_status();
     }
-    if (!vec) return launch_rows<T, 1, 4, 4>(which, a, sms, s);
-    if (a.D < 256 * N) return launch_rows<T, N, 4, 1>(which, a, sms, s);
-    // one or two slots a token leave fewer rows to ask for: more of each
-    return which == DISPATCH || a.k > 2 ? launch_rows<T, N, 4, 2>(which, a, sms, s)
-           : a.k == 2 ? launch_rows<T, N, 2, 4>(which, a, sms, s) : launch_rows<T, N, 1, 4>(which, a, sms, s);
+    if constexpr (N == 1) {
+        return launch_rows<T, 1, 4, 4, APART>(which, a, sms, s);
+    } else {
+        if (a.D < 256 * N) return launch_rows<T, N, 4, 1, APART>(which, a, sms, s);
+        // one or two slots a token leave fewer rows to ask for: more of each
+        return which == DISPATCH || a.k > 2 ? launch_rows<T, N, 4, 2, APART>(which, a, sms, s)
+               : a.k == 2 ? launch_rows<T, N, 2, 4, APART>(which, a, sms, s) : launch_rows<T, N, 1, 4, APART>(which, a, sms, s);
+    }
+}
+template <class T>
+int launch_type(Which which, const RowArgs &a, int sms, cudaStream_t s) {
+    constexpr int N = 16 / sizeof(T);
+    const auto aligned = [&](const void *p, long long ld) { return aligned_to(p, 16) && (!p || ld * sizeof(T) % 16 == 0); };
+    const bool x = aligned(a.x, a.ldx), ys = aligned(a.ys, a.ldys), out = aligned(a.out, a.ldo);
+    // dispatch: x by token, out sorted; combine: out by token, ys sorted; its backward pass: x by token, the others sorted
+    const bool token = which == COMBINE ? out : x, sorted = ys && (which == COMBINE || out);
+    if (a.D % N || !sorted) return launch_type<T, 1, false>(which, a, sms, s);
+    return token ? launch_type<T, N, false>(which, a, sms, s) : launch_type<T, N, true>(which, a, sms, s);
 }
 int launch(Which which, RowArgs &a, int dtype, cudaStream_t s) {
     int rc;

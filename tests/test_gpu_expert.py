@@ -152,6 +152,23 @@ def test_into_given_tensors_only(ccdc):
     assert again.offsets.shape == (41,)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,k,D", [(5, 3, 40), (37, 2, 4096), (9, 1, 2048), (30, 5, 8)])
+def test_rows_of_tokens_that_start_anywhere(ccdc, M, k, D, dtype):
+    """the tokens' rows out of a padded batch, the sorted ones aligned: the bits of aligned tokens"""
+    rng = np.random.default_rng(D)
+    order = ccdc.expert_sort(torch.from_numpy(draw_ids(rng, M, k, 6, 0.1)).cuda(), 6)
+    x, dy = (rows_of(rng, M, D, dtype, 5, 1) for _ in range(2))
+    ys, w = rows_of(rng, M * k, D, dtype), torch.rand((M, k), device="cuda")
+    assert torch.equal(ccdc.expert_dispatch(x, order), ccdc.expert_dispatch(x.contiguous(), order))
+    for a, b in zip(ccdc.expert_combine_backward(dy, ys, order, w), ccdc.expert_combine_backward(dy.contiguous(), ys, order, w)):
+        assert torch.equal(a, b)
+    flat = torch.full((M * (D + 3) + 1,), 7.0, dtype=DT[dtype], device="cuda")
+    out = ccdc.expert_combine(ys, order, w, out=flat[1:].view(M, D + 3)[:, :D])
+    assert torch.equal(out, ccdc.expert_combine(ys, order, w))
+    assert bool((flat[1:].view(M, D + 3)[:, D:] == 7).all()) and float(flat[0]) == 7
+
+
 def test_infinities_and_nan(ccdc):
     """they stay in the tokens that they belong to"""
     order = ccdc.expert_sort(torch.tensor([[0, 1], [1, -1], [-1, -1]], device="cuda"), 2)
