@@ -579,7 +579,7 @@ int ccdc_block_status(void);
  * tokens sorted by expert and back, the loss from a teacher's top logits, and
  * the 8-bit products of a teacher that is not trained.  The conventions of the
  * block operators hold (row strides, types, sums in binary32 or more, one
- * rounding, one order, no atomics, no allocation, capturable); these calls need
+ * rounding, one order, no allocation, capturable); these calls need
  * no workspace.
  *
  * Tokens sorted by expert.  ids [M][k] contiguous (id_bytes 4 or 8: signed

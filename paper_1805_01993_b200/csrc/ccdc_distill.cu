@@ -373,10 +373,18 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
                         sum_up(std::false_type());
                 };
                 // group by group in either form, so that the loss has the same bits with and without the gradient
-                if constexpr (GRAD) copies_landed<0>();
+                static_assert(GROUPS == 4, "waits");
+#pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
                     const int begin = tid + g * group * THREADS, end = begin + group * THREADS;
-                    if constexpr (!GRAD) copies_landed<GROUPS - 1>();
+                    if (!GRAD || g == 0)
+                        copies_landed<3>();
+                    else if (g == 1)
+                        copies_landed<2>();
+                    else if (g == 2)
+                        copies_landed<1>();
+                    else
+                        copies_landed<0>();
                     use(begin, min(own.count, end));
                     if constexpr (!GRAD) {      // the next row's copies take the place of a group's as soon as it has been used
                         for (int p = begin; p < min(next_count, end); p += THREADS) copy_piece(row + p, next.from + p);

@@ -1,8 +1,8 @@
 // Tokens sorted by expert and back, with weights applied, and the gradients.
 //
 // Slot s = m k + j is token m's j-th expert.  The sort is a stable counting sort: offsets[e] = slots of experts before e, the
-// place of a slot = offsets[e] + slots of the same expert before it.  Everything has one order and there are no atomics, so
-// replicas of a file agree bit by bit.  A slot whose expert lies outside [0, E) is dropped: place -1.
+// place of a slot = offsets[e] + slots of the same expert before it.  Everything has one order (atomics count whole numbers
+// alone), so replicas of a file agree bit by bit.  A slot whose expert lies outside [0, E) is dropped: place -1.
 #include "ccdc_block.h"
 
 #include <algorithm>
