@@ -653,7 +653,7 @@ int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits,
  *
  * Product: y[m][n] = sum_b xs[m][b] * ws[n / 128][b] * sum_{k in b} x[m][k] w[n][k].
  * x [M][K] with scales at x_scales[m*x_scale_row + b*x_scale_col]; w [experts][N][K]
- * (w_expert bytes apart, row stride ldw) with scales [experts][ceil(N/128)][ceil(K/128)]
+ * (w_expert > 0 bytes apart, row stride ldw) with scales [experts][ceil(N/128)][ceil(K/128)]
  * contiguous; any binary32 scales whose products are finite.  y [M][N] in y_dtype.
  * offsets NULL: one weight.  Else [experts + 1] on the device: rows offsets[e]
  * up to offsets[e + 1] take weight e (offsets[0] is taken as 0, entries beyond

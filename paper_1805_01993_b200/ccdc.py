@@ -558,7 +558,7 @@ def _elsewhere(x, stream):
         if stream.device != x.device:
             raise ValueError("the stream belongs to another device than the tensors")
         return torch.cuda.stream(stream)
-    if x.is_cuda and x.get_device() != torch.cuda.current_device():
+    if x.is_cuda and x.get_device() != torch._C._cuda_getDevice():
         return torch.cuda.device(x.device)
     return None
 
@@ -854,10 +854,10 @@ def _order(order, like, rows=None):
     if places.dim() != 2:
         raise ValueError("order.places: [tokens][k] expected")
     M, k = places.shape
-    ps, pp = _vector(slots, "order.slots", like, M * k, torch.int32), _vector(places, "order.places", like, M * k, torch.int32)
     if rows is not None and rows != M:
         raise ValueError(f"the order is of {M} tokens, the tensor has {rows} rows")
-    return M, k, ps, pp
+    i32, n = torch.int32, M * k
+    return M, k, _vector(slots, "order.slots", like, n, i32), _vector(places, "order.places", like, n, i32)
 
 
 def expert_sort(ids, n_experts, offsets=None, slots=None, places=None, stream=None):

@@ -8,8 +8,12 @@
 // memory between the walk for maximum and sum and the walk that writes the gradient: z is read from memory once.  Blocks stay and
 // take row after row: a thread copies 16-byte pieces asynchronously and reads only its own, so the copy of the next row's piece
 // starts as soon as a piece has been read for the last time, and nothing waits but for copies.  The blocks of a cluster exchange
-// their maxima and sums.  The last warp of a block computes the next row's k terms meanwhile, in 64 bits.  Exponentials are the
-// next bound (two for each element).
+// their maxima and sums.  The last warp of a block computes the next row's k terms meanwhile, in 64 bits.
+//
+// Measured (one B200): 4096 x 131072 bf16 in one pass 585 us, 3.7 TB/s of z and dz; the loss alone 372 us, the gradient alone
+// 453 us; 1024 x 32000 binary32 39 and 56 us.  Instructions and their latency bound it (27 warps an SM, half of the issue slots):
+// the walk for the sum takes 5 a bf16 element and 700 a row and warp beside, the other 7 and 400.  Slower: 512 threads a block (726 us),
+// 128 (635), parts of 32 KiB (749), rows read again from L2 instead of kept (777).
 #include "ccdc_block.h"
 
 #include <algorithm>

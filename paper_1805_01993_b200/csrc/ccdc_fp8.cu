@@ -163,7 +163,7 @@ int ccdc_matmul_fp8(long long M, long long N, long long K, int experts, const vo
     if (M > (1 << 30) || N > (1 << 22) || K > (1 << 23) || experts > 1024) return CCDC_ESIZE;
     if (M == 0) return CCDC_OK;
     if (!x || !x_scales || !w || !w_scales || !y || ldx < K || ldw < K || ldy < N || !aligned_to(x, 16) || !aligned_to(w, 16) ||
-        ldx % 16 || ldw % 16 || (experts > 1 && (w_expert % 16 || w_expert < 0)))
+        ldx % 16 || ldw % 16 || (experts > 1 && (w_expert % 16 || w_expert <= 0)))
         return CCDC_EINVAL;
     int rc;
     const int sms = block_sm_count(&rc);

@@ -15,6 +15,15 @@
 // tiles comes from the offsets in every block's shared memory, so that nothing waits for the host.  With few tiles, k is cut
 // over the blocks of a cluster, whose sums meet in shared memory in the order of k.
 //
+// Measured (one B200, calls in a stream on changing inputs, without the quantisation of x): 8192^3 550 us, 2.0 PFLOP/s; 2048 rows
+// of 4096 x 4096 45 us; 200 rows over 64 weights of 2048 x 4096 72 us; one row of 16384 x 4096 17 us.  What bounds them:
+//   large   the turn of the two accumulators.  A block of the pair's tile takes about 930 cycles: 512 of products, 425 of reading and
+//           adding, and between them the ways of commit and arrival.  Without reading it is 420 us (TMA and tensor cores).  Tried
+//           and slower: halves of 128 columns with barriers of their own (757 us: their products read shared memory half as
+//           often again), 16 adding warps (625), the scales through a ring of their own (649).  Waits and arrivals that order
+//           memory across the cluster took 1176 us.
+//   few     a block's weights by TMA (128 x 128 bytes a stage) at 5 to 7 TB/s once it runs; start, join and end take 7 us.
+//
 // All waits are bounded: one that runs out sets g_wait_failed, and its warp issues nothing more and waits for the block's end.
 #include <cuda.h>
 

@@ -82,7 +82,7 @@ def test_fp8_refusals():
         return L.ccdc_matmul_fp8(M, N, K, E, x, ldx, xs, 1, 4, w, we, ldw, ws, offsets, y, yt, ldy, None)
 
     refuses(product, ccdc.EINVAL, dict(M=-1), dict(N=0), dict(K=0), dict(E=0), dict(x=None), dict(x=P + 8), dict(ldx=40), dict(ldx=32),
-            dict(xs=None), dict(w=None), dict(w=P + 4), dict(ldw=56), dict(ldw=32), dict(we=968), dict(we=-16), dict(ws=None),
+            dict(xs=None), dict(w=None), dict(w=P + 4), dict(ldw=56), dict(ldw=32), dict(we=968), dict(we=-16), dict(we=0), dict(ws=None),
             dict(offsets=None), dict(y=None), dict(yt=ccdc.I32), dict(ldy=19))
     refuses(product, ccdc.ESIZE, dict(M=(1 << 30) + 1), dict(N=(1 << 22) + 1, ldy=1 << 23), dict(K=(1 << 23) + 1), dict(E=1025))
     assert product(M=0) == ccdc.OK
