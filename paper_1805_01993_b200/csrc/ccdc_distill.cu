@@ -13,7 +13,7 @@
 // Measured (one B200): 4096 x 131072 bf16 in one pass 585 us, 3.7 TB/s of z and dz; the loss alone 372 us, the gradient alone
 // 453 us; 1024 x 32000 binary32 39 and 56 us.  Instructions and their latency bound it (27 warps an SM, half of the issue slots):
 // the walk for the sum takes 5 a bf16 element and 700 a row and warp beside, the other 7 and 400.  Slower: 512 threads a block (726 us),
-// 128 (635), parts of 32 KiB (749), rows read again from L2 instead of kept (777).
+// 128 (635), parts of 52 KiB by four blocks an SM (613) or 42 by five (728), rows read again from L2 instead of kept (777).
 #include "ccdc_block.h"
 
 #include <algorithm>
@@ -25,7 +25,7 @@ constexpr int MAX_TOP = 1024, MAX_CLUSTER = 8;
 constexpr int AHEAD = 4;                    // slots a lane
 constexpr int GROUPS = 4;                   // of copies that are waited for one after the other
 constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 64 threads take
-constexpr int PART = 64 << 10;              // bytes of a part that leave room for three blocks an SM
+constexpr int PART = 65 << 10;              // bytes of a part that leave room for three blocks an SM
 constexpr int MOST_PART = 176 << 10, MOST_SMEM = MOST_PART + 32 + 48 * MAX_TOP;
 
 struct DistillArgs {
@@ -40,7 +40,7 @@ struct DistillArgs {
     float scale;                // log2(e) / T
     int group;                  // pieces of a thread in a group of copies
     int part_pieces, table;     // room of a block, in pieces of 16 bytes; of the table of ids
-    int log_blocks;             // of the blocks to a row
+    int blocks;                 // to a row
 };
 
 template <class T, int N>
@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
     __shared__ Teacher told[2];
     const int tid = threadIdx.x, lane = tid & 31;
     const bool walks = tid < THREADS;
-    const int blocks = 1 << a.log_blocks, rank = blockIdx.x & (blocks - 1);
-    const long long step = gridDim.x >> a.log_blocks;
+    const int blocks = a.blocks, rank = (int)(blockIdx.x % (unsigned)blocks);
+    const long long step = gridDim.x / (unsigned)blocks;
     const auto slots_of = [&](int which) {
         Slots s;
         s.target = reinterpret_cast<double *>(row + a.part_pieces) + which * a.k;
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
     };
     const auto row_of = [&](long long m) { return static_cast<const T *>(a.z) + m * a.ldz; };
 
-    long long m = blockIdx.x >> a.log_blocks;
+    long long m = blockIdx.x / (unsigned)blocks;
     if (m < a.M) {
         if (walks) {
             const Share<T> own(a, row_of(m), rank);
@@ -415,11 +415,15 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
             asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
             asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
             if constexpr (LOSS) {
-                uint32_t p;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                             : "=r"(p) : "r"((uint32_t)__cvta_generic_to_shared(&whole[which])), "r"(lane & (blocks - 1)));
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(r.top), "=f"(r.sum) : "r"(p) : "memory");
-                r = join<T>(r, a.scale, blocks);
+                const int b = lane & (MAX_CLUSTER - 1);
+                r = {-INFINITY, 0.0f};
+                if (b < blocks) {
+                    uint32_t p;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                                 : "=r"(p) : "r"((uint32_t)__cvta_generic_to_shared(&whole[which])), "r"(b));
+                    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(r.top), "=f"(r.sum) : "r"(p) : "memory");
+                }
+                r = join<T>(r, a.scale, MAX_CLUSTER);
             }
         }
         const Above<T> above(r.top, a.scale);
@@ -536,7 +540,7 @@ int launch(DistillArgs &a, int blocks, cudaStream_t s) {
     static std::atomic<unsigned long long> done;
     const int rc = block_allow_smem(reinterpret_cast<const void *>(kernel), MOST_SMEM, &done);
     if (rc != CCDC_OK) return rc;
-    a.table = table_length(a.k), a.log_blocks = blocks == 8 ? 3 : blocks >> 1;
+    a.table = table_length(a.k), a.blocks = blocks;
     // a row has (V + 2 (N - 1)) / N pieces at most
     a.part_pieces = (int)(((a.V * (long long)sizeof(T) + 30) / 16 + blocks - 1) / blocks);
     a.group = (a.part_pieces + GROUPS * THREADS - 1) / (GROUPS * THREADS);
@@ -575,9 +579,8 @@ int launch(DistillArgs &a, cudaStream_t s) {
     if (rc != CCDC_OK) return rc;
     // parts that leave room for several blocks an SM; smaller ones where rows are few
     const long long bytes = a.V * (long long)sizeof(T);
-    int blocks = 1;
-    while (blocks < MAX_CLUSTER && (bytes > (long long)PART * blocks || (a.M * blocks * 2 <= sms && bytes > (long long)SMALL_PART * blocks)))
-        blocks *= 2;
+    int blocks = (int)std::min<long long>(MAX_CLUSTER, (bytes + PART - 1) / PART);
+    while (2 * blocks <= MAX_CLUSTER && a.M * blocks * 2 <= sms && bytes > (long long)SMALL_PART * blocks) blocks *= 2;
     if (bytes > (long long)MOST_PART * blocks) return CCDC_ESIZE;
     // Few threads to a small part: what a row costs beside its bytes is paid by each warp.  (8192 x 8192 bf16 in one pass: 97 us
     // with 128 threads, 114 with 256; 8192 x 32000: 261 and 231.)
