@@ -221,11 +221,18 @@ __device__ __forceinline__ void put_rows_as(const Args &a, long long token0, int
             else
                 mine[i] = pack2<T>(sum[c / 2 + i].x, sum[c / 2 + i].y);
         __syncwarp();
-        const int column = lane % N;
-        if (n0 + c + column < a.N)
-#pragma unroll 4
-            for (int r = lane / N; r < left; r += 32 / N)
-                y[r * a.ldy + c + column] = *reinterpret_cast<const T *>(stage + r * STAGE_ROW + column * sizeof(T));
+        const int column = lane % N, row = lane / N;
+        if (n0 + c + column < a.N) {
+            T *to = y + row * a.ldy + c + column;
+            const char *from = stage + row * STAGE_ROW + column * (int)sizeof(T);
+            const long long step = 32 / N * a.ldy;
+            if (left == 32) {
+#pragma unroll 16
+                for (int r = 0; r < N; ++r, to += step) *to = *reinterpret_cast<const T *>(from + r * (32 / N * STAGE_ROW));
+            } else {
+                for (int r = row; r < left; r += 32 / N, to += step, from += 32 / N * STAGE_ROW) *to = *reinterpret_cast<const T *>(from);
+            }
+        }
         __syncwarp();
     }
 }
