@@ -353,9 +353,8 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
         asm volatile("prefetch.tensormap [%0];" ::"l"(&a.w) : "memory");
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     // the list of tiles: running maximum of the offsets, then running sums of tiles
-    if (warp == 2) {
+    const auto list_tiles = [&] {
         int end = 0, tiles = 0;
         for (int e0 = 0; e0 <= a.experts; e0 += 32) {
             const int e = e0 + lane;
@@ -379,11 +378,18 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
             tiles += __shfl_sync(~0u, sum, 31);
         }
         if (lane == 0) first[0] = 0;
-    }
+    };
+    // all that needs nothing of the kernel before runs under its end
+    if (warp == 2 && !a.offsets) list_tiles();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (per > 1) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.offsets) {
+        if (warp == 2) list_tiles();
+        __syncthreads();
+    }
     const uint32_t tmem = *tmem_slot;
     const int items = first[a.experts + 1];
     // this block's part of k
