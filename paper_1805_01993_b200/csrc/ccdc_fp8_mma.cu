@@ -15,14 +15,16 @@
 // tiles comes from the offsets in every block's shared memory, so that nothing waits for the host.  With few tiles, k is cut
 // over the blocks of a cluster, whose sums meet in shared memory in the order of k.
 //
-// Measured (one B200, calls in a stream on changing inputs, without the quantisation of x): 8192^3 550 us, 2.0 PFLOP/s; 2048 rows
-// of 4096 x 4096 45 us; 200 rows over 64 weights of 2048 x 4096 72 us; one row of 16384 x 4096 17 us.  What bounds them:
+// Measured (one B200, calls in a stream on changing inputs, without the quantisation of x): 8192^3 545 us, 2.0 PFLOP/s; 2048 rows
+// of 4096 x 4096 44 us; 200 rows over 64 weights of 2048 x 4096 72 us; one row of 16384 x 4096 16.4 us.  What bounds them:
 //   large   the turn of the two accumulators.  A block of the pair's tile takes about 930 cycles: 512 of products, 425 of reading and
-//           adding, and between them the ways of commit and arrival.  Without reading it is 420 us (TMA and tensor cores).  Tried
-//           and slower: halves of 128 columns with barriers of their own (757 us: their products read shared memory half as
-//           often again), 16 adding warps (625), the scales through a ring of their own (649).  Waits and arrivals that order
-//           memory across the cluster took 1176 us.
-//   few     a block's weights by TMA (128 x 128 bytes a stage) at 5 to 7 TB/s once it runs; start, join and end take 7 us.
+//           adding, and between them the ways of commit and arrival.  8192^3 takes 330 us without loads and turns, 390 without turns,
+//           455 without reading, 495 with reading but without adding.  Tried and not kept: halves of 128 columns, each with its
+//           barriers and its issuing thread (591: they read shared memory half as often again), two issuing threads in turn (554),
+//           products issued by a warp that goes together (557), 16 adding warps (625), scales through shared memory (551), one
+//           polling thread a warp (560).  Waits and arrivals that order memory across the cluster took 1176 us.
+//   few     a block's weights by TMA (128 x 128 bytes a stage) at 5 to 7 TB/s once it runs; start, join and end take 7 us.  The
+//           first weights on their way to L2 before the kernel before has ended: 0.6 us less for one row, 0.8 more for 512.
 //
 // All waits are bounded: one that runs out sets g_wait_failed, and its warp issues nothing more and waits for the block's end.
 #include <cuda.h>
@@ -98,7 +100,8 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
         asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
                      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-// arrives at the barrier (of both blocks of a pair) when the products issued so far are done
+// arrives at the barrier (of both blocks of a pair) when the products this thread has issued are done: a stage may be filled again,
+// and its products may be added
 template <int CG>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     if constexpr (CG == 2)
@@ -329,12 +332,13 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
     uint64_t *bars = reinterpret_cast<uint64_t *>(warp_base + EPI_WARPS * S::WARP_BYTES);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 31);
     int *ends = reinterpret_cast<int *>(bars + 32), *first = ends + a.experts + 1;      // [experts + 1], [experts + 2]
-    const uint32_t full = smem_u32(bars), empty = full + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 8 * S::ACCS;
-    static_assert(2 * S::STAGES + 2 * S::ACCS <= 31, "barriers");
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::STAGES, acc_empty = empty + 8 * S::STAGES;
+    static_assert(2 * S::STAGES + S::ACCS <= 31, "barriers");
+    static_assert(S::ACCS <= S::STAGES, "a stage's products are added before its next ones end");
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-        for (int i = 0; i < S::ACCS; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, EPI_WARPS * CG);
+        for (int i = 0; i < S::ACCS; ++i) bar_init(acc_empty + 8 * i, EPI_WARPS * CG);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -436,7 +440,6 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mma<CG>(tmem + acc * S::N, rows + 2 * k, columns + 2 * k, idesc, k > 0);
                     mma_commit<CG>(empty + 8 * stage);
-                    mma_commit<CG>(acc_full + 8 * acc);
                     if (++stage == S::STAGES) stage = 0, phase ^= 1;
                     if (++acc == S::ACCS) acc = 0, acc_phase ^= 1;
                 }
@@ -447,7 +450,7 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
         const int quarter = warp & 3;               // the tensor-memory lanes a warp may read
         const int part = (warp - FIRST_EPI) >> 2;   // two warps a quarter: each takes half of the columns
         char *own_bytes = warp_base + (warp - FIRST_EPI) * S::WARP_BYTES;
-        uint32_t acc = 0, acc_phase = 0, buffer = 0;
+        uint32_t acc = 0, stage = 0, phase = 0, buffer = 0;
         for (int item = cluster; ok && item < items; item += clusters) {
             const Tile t = tile_of<NT>(a, ends, first, item, expert);
             const int row = 32 * quarter + lane, column0 = part * S::COLS;      // this thread's row of the SM's, its first column
@@ -485,7 +488,7 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
                     }
                     fetch(b + 2, 2);                        // on its way during this block and the next
                     __syncwarp();
-                    if (ok = __all_sync(~0u, bar_wait(acc_full + 8 * acc, acc_phase)); !ok) break;
+                    if (ok = __all_sync(~0u, bar_wait(empty + 8 * stage, phase)); !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t from = tmem + acc * S::N + column0 + ((uint32_t)(32 * quarter) << 16);
                     const auto give_back = [&] {            // read out: the tensor core may have it back
@@ -531,7 +534,8 @@ __global__ void __launch_bounds__(THREADS, Shape<CG, NT, NW>::PER_SM) k_fp8(cons
                             if (c + 2 * W < S::COLS) tmem_load(from + c + 3 * W, r[1]);
                         }
                     }
-                    if (++acc == S::ACCS) acc = 0, acc_phase ^= 1;
+                    if (++acc == S::ACCS) acc = 0;
+                    if (++stage == S::STAGES) stage = 0, phase ^= 1;
                 }
             }
             if (CG == 1 && splits > 1) {        // to be joined below, token by token; the ring is not needed any more
