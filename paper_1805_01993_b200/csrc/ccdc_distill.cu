@@ -10,8 +10,8 @@
 // starts as soon as a piece has been read for the last time, and nothing waits but for copies.  The blocks of a cluster exchange
 // their maxima and sums.  The last warp of a block computes the next row's k terms meanwhile, in 64 bits.
 //
-// Measured (one B200): 4096 x 131072 bf16 in one pass 585 us, 3.7 TB/s of z and dz; the loss alone 372 us, the gradient alone
-// 453 us; 1024 x 32000 binary32 39 and 56 us.  Instructions and their latency bound it (27 warps an SM, half of the issue slots):
+// Measured (one B200): 4096 x 131072 bf16 in one pass 580 us, 3.7 TB/s of z and dz; the loss alone 321 us, the gradient alone
+// 420 us; 1024 x 32000 binary32 38 and 56 us.  Instructions and their latency bound it (27 warps an SM, half of the issue slots):
 // the walk for the sum takes 5 a bf16 element and 700 a row and warp beside, the other 7 and 400.  Slower: 512 threads a block (726 us),
 // 128 (635), parts of 52 KiB by four blocks an SM (613) or 42 by five (728), rows read again from L2 instead of kept (777).
 #include "ccdc_block.h"
@@ -184,44 +184,62 @@ struct Teacher {
     double P, entropy;          // sum of t; of t log t
     int twice;                  // whether an id comes more than once
 };
-// by one warp
-template <class T>
+// by one warp; TWICE: looks for ids that come more than once
+template <class T, bool TWICE>
 __device__ __forceinline__ Teacher teacher_side(const DistillArgs &a, const T *z, long long m, const Slots &s, int lane) {
-    for (int i = lane; i <= s.mask; i += 32) s.seen[i] = -1;
-    __syncwarp();
+    if constexpr (TWICE) {
+        for (int i = lane; i <= s.mask; i += 32) s.seen[i] = -1;
+        __syncwarp();
+    }
     float top = -INFINITY;
     bool twice = false, any = false;
-    for (int j0 = lane; j0 < a.k; j0 += 32 * AHEAD) {       // the loads of AHEAD slots are under way together
+    for (int k0 = 0; k0 < a.k; k0 += 32 * AHEAD) {          // the loads of AHEAD slots are under way together
+        const int j0 = k0 + lane;
         long long id[AHEAD];
         float v[AHEAD], c[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int j = j0 + 32 * u;
-            const long long from = m * a.k + (j < a.k ? j : j0);
+            const long long from = m * a.k + min(j, a.k - 1);
             id[u] = a.id_bytes == 8 ? static_cast<const long long *>(a.ids)[from] : static_cast<const int *>(a.ids)[from];
             v[u] = a.values_f32 ? static_cast<const float *>(a.values)[from] : to_f32<T>(static_cast<const T *>(a.values)[from]);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (id[u] < 0 || id[u] >= a.V || v[u] == -INFINITY) id[u] = -1;
+            if (id[u] < 0 || id[u] >= a.V || v[u] == -INFINITY || j0 + 32 * u >= a.k) id[u] = -1;
             c[u] = to_f32<T>(z[max(id[u], 0LL)]);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int j = j0 + 32 * u;
-            if (j >= a.k) break;
-            s.at[j] = (int)id[u], s.value[j] = v[u], s.chosen[j] = c[u];
+            if (j < a.k) s.at[j] = (int)id[u], s.value[j] = v[u], s.chosen[j] = c[u];
             if (id[u] < 0) continue;
             any = true;
             top = fmaxf(top, v[u]);
-            for (uint32_t h = (uint32_t)id[u] * 2654435761u >> 7;; ++h) {       // ends: the table has room for twice the slots
-                const int there_already = atomicCAS(&s.seen[h & s.mask], -1, (int)id[u]);
-                twice = twice || there_already == (int)id[u];
-                if (there_already == -1 || there_already == (int)id[u]) break;
-            }
+        }
+        if constexpr (TWICE) {
+            // Into the table, AHEAD slots at a time (one after the other, a warp waits for the longest way of 32 each time: loss and
+            // gradient of 1024 x 32000 binary32 with 400 slots 158 us, 120 so).  Ends: the table has room for twice the slots.
+            uint32_t at[AHEAD];
+            bool open[AHEAD], more;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) at[u] = (uint32_t)id[u] * 2654435761u >> 7, open[u] = id[u] >= 0;
+            do {
+                int old[AHEAD];
+                more = false;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u)
+                    if (k0 + 32 * u < a.k) old[u] = atomicCAS(&s.seen[at[u]++ & s.mask], open[u] ? -1 : -2, (int)id[u]);    // no entry is -2
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    twice = twice || (open[u] && old[u] == (int)id[u]);
+                    open[u] = open[u] && old[u] != -1 && old[u] != (int)id[u];
+                    more = more || open[u];
+                }
+            } while (__any_sync(~0u, more));
         }
     }
-    Teacher r = {0.0, 0.0, __any_sync(~0u, twice)};
+    Teacher r = {0.0, 0.0, TWICE && __any_sync(~0u, twice)};
     if (!__any_sync(~0u, any)) return r;
     // t = e / whole with e = exp(v / T - shift)
     double shift, whole = 1.0;
@@ -331,7 +349,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
                 copies_end();
             }
         } else {
-            const Teacher t = teacher_side<T>(a, row_of(m), m, slots_of(0), lane);
+            const Teacher t = teacher_side<T, GRAD>(a, row_of(m), m, slots_of(0), lane);
             if (lane == 0) told[0] = t;
         }
     }
@@ -443,7 +461,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 3 : THREADS == 
                 }
             }
             if (more) {
-                const Teacher t = teacher_side<T>(a, row_of(m + step), m + step, slots_of(which ^ 1), lane);
+                const Teacher t = teacher_side<T, GRAD>(a, row_of(m + step), m + step, slots_of(which ^ 1), lane);
                 if (lane == 0) told[which ^ 1] = t;
             }
         } else if constexpr (GRAD) {
