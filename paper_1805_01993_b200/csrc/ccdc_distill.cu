@@ -10,7 +10,7 @@
 // starts as soon as a piece has been read for the last time, and nothing waits but for copies.  The blocks of a cluster exchange
 // their maxima and sums.  The last warp of a block computes the next row's k terms meanwhile, in 64 bits.
 //
-// Measured (one B200): 4096 x 131072 bf16 in one pass 580 us, 3.7 TB/s of z and dz; the loss alone 321 us, the gradient alone
+// Measured (one B200): 4096 x 131072 bf16 in one pass 557 us, 3.9 TB/s of z and dz; the loss alone 325 us, the gradient alone
 // 420 us; 1024 x 32000 binary32 38 and 56 us.  Instructions and their latency bound it (27 warps an SM, half of the issue slots):
 // the walk for the sum takes 5 a bf16 element and 700 a row and warp beside, the other 7 and 400.  Slower: 512 threads a block (726 us),
 // 128 (635), parts of 52 KiB by four blocks an SM (613) or 42 by five (728), rows read again from L2 instead of kept (777).
@@ -22,7 +22,9 @@
 namespace {
 
 constexpr int MAX_TOP = 1024, MAX_CLUSTER = 8;
-constexpr int AHEAD = 4;                    // slots a lane
+// Slots that a lane has under way.  Four: 579 us for 557 at 4096 x 131072 bf16 in one pass, 23.7 for 23.1 at 300 x 50257 fp16; but
+// 120 for 137 at 1024 x 32000 binary32 with 400 slots.
+constexpr int AHEAD = 2;
 constexpr int GROUPS = 4;                   // of copies that are waited for one after the other
 constexpr int SMALL_PART = 8 << 10;         // bytes of a row that 64 threads take
 constexpr int PART = 65 << 10;              // bytes of a part that leave room for three blocks an SM
@@ -219,7 +221,7 @@ __device__ __forceinline__ Teacher teacher_side(const DistillArgs &a, const T *z
         }
         if constexpr (TWICE) {
             // Into the table, AHEAD slots at a time (one after the other, a warp waits for the longest way of 32 each time: loss and
-            // gradient of 1024 x 32000 binary32 with 400 slots 158 us, 120 so).  Ends: the table has room for twice the slots.
+            // gradient of 4096 x 131072 bf16 with 128 slots 450 us, 419 so).  Ends: the table has room for twice the slots.
             uint32_t at[AHEAD];
             bool open[AHEAD], more;
 #pragma unroll
