@@ -11,7 +11,7 @@
 // their maxima and sums.  The last warp of a block computes the next row's k terms meanwhile, in 64 bits.
 //
 // Measured (one B200): 4096 x 131072 bf16 in one pass 557 us, 3.9 TB/s of z and dz; the loss alone 325 us, the gradient alone
-// 420 us; 1024 x 32000 binary32 38 and 56 us.  Instructions and their latency bound it (27 warps an SM, half of the issue slots):
+// 420 us; 1024 x 32000 binary32 38 and 56 us.  Instructions and their latency bound it (27 warps an SM, 0.6 of the issue slots):
 // the walk for the sum takes 5 a bf16 element and 700 a row and warp beside, the other 7 and 400.  Slower: 512 threads a block (726 us),
 // 128 (635), parts of 52 KiB by four blocks an SM (613) or 42 by five (728), rows read again from L2 instead of kept (777).
 #include "ccdc_block.h"
