@@ -78,15 +78,17 @@ __device__ __forceinline__ float power(float x) {
     return e;
 }
 // 2^(z * scale) relative to a reference `top` (a row's or a thread's largest value).  16-bit logits: 2^(z * scale - b), one
-// fused operation for each, with b = top * scale rounded once, so that its rounding is the same in every term; unless b is so
-// large that z * scale may overflow (a row of a type's lowest values).  Those and binary32: 2^((z - top) * scale).
+// fused operation for each, with b = top * scale rounded once: its rounding is the same in every term, and a factor of 2^-0.5 to
+// 2^0.5 as long as |b| < 2^24.  Further out (masks of -1e9, low temperatures) it would be a factor of hundreds of octaves, infinity
+// or 0.  There, and for binary32: 2^((z - top) * scale).  A reference that rises from one form to the other passes 2^13 octaves at
+// least, the distance of neighbours among 16-bit values so far out: the sum's factor is 0 in either form.
 template <class T>
 struct Above {
     float top, scale, b;
     bool fused;
     __device__ __forceinline__ Above(float top_, float scale_) : top(top_ == -INFINITY ? 0.0f : top_), scale(scale_) {
         b = __fmul_rn(top, scale);
-        fused = sizeof(T) == 2 && fabsf(b) < 0x1p100f;
+        fused = sizeof(T) == 2 && fabsf(b) < 0x1p24f;
     }
     __device__ __forceinline__ float exponent(float z) const { return fused ? fmaf(z, scale, -b) : (z - top) * scale; }
     __device__ __forceinline__ float operator()(float z) const { return power<T>(exponent(z)); }
