@@ -623,8 +623,10 @@ int ccdc_expert_combine_backward(long long M, int k, long long D, int dtype, con
  *     loss = sum_j t_j * (log t_j - log s[ids_j]),   s = softmax(z / T)
  *     dz   = dloss[m] / T * (P * s - t),   P = sum_j t_j
  * Slots of one id add up.  A row without slots, or with P = 0, has loss 0 and
- * gradient 0, whatever its logits.  Logits of -infinity or of the type's lowest
- * value have s = 0 (loss +infinity where t > 0).
+ * gradient 0, whatever its logits.  A logit of -infinity has s = 0, and the loss
+ * is +infinity where its t > 0.  Finite logits follow the formula wherever they
+ * lie, masks of the type's lowest value too: s falls to 0, the loss is the
+ * formula's (t times the distance / T), +infinity only beyond binary32.
  *   loss alone             dlogits NULL; stats NULL, or [M][2] binary32 (8-byte
  *                          aligned) for the gradient later
  *   gradient from stats    loss NULL, dloss [M] binary32, dlogits (row stride

@@ -1,5 +1,5 @@
-"""The distillation loss of logits far from zero: finite masks of any size, rows that lie far out themselves, and the ends of the
-temperature's range."""
+"""The distillation loss of logits far from zero: finite masks of any size, rows that lie far out themselves, the ends of the
+temperature's range, and targets at a type's lowest value."""
 import numpy as np
 import pytest
 
@@ -86,3 +86,14 @@ def test_ends_of_the_temperature(ccdc, T, V, dtype):
     z[3, V // 2:] = -60000.0
     z[4] = z[4].sign() * 2.0                            # ties
     check(ccdc, z, ids, values, dloss, T, dtype)
+
+@pytest.mark.parametrize("dtype", DT)
+def test_targets_at_the_lowest_value(ccdc, dtype):
+    """the formula's loss, which is finite; minus infinity alone gives an infinite one"""
+    z, ids, values, dloss = inputs(4, 500, 6, dtype, np.arange(250), 9)
+    z[:, 250:] = torch.finfo(DT[dtype]).min
+    ids[:, 0] = 400
+    check(ccdc, z, ids, values, dloss, 2.0, dtype)
+    check(ccdc, z, ids, values, dloss, 1e6, dtype)
+    z[:, 250:] = -float("inf")
+    assert bool((ccdc.distill_forward(z, ids, values, temperature=2.0) == float("inf")).all())
