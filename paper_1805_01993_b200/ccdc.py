@@ -828,11 +828,20 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, act="silu", grad_dtype=None
 # The same conventions; ids, places and offsets are integers on the tensors' device.
 
 
+MAX_EXPERTS = 4096
+
+
 class ExpertOrder(NamedTuple):
     """What ``expert_sort`` returns: ``offsets`` [experts + 1], ``slots`` [M*k] and ``places`` [M][k], all int32."""
     offsets: object
     slots: object
     places: object
+
+
+def _fits(n, where):
+    """raises unless a count fits the C call's 32-bit integer (ctypes would pass its low bits)."""
+    if n > 0x7FFFFFFF:
+        raise CcdcError(ESIZE, where)
 
 
 def _ids(t, name, like=None):
@@ -843,6 +852,7 @@ def _ids(t, name, like=None):
         raise ValueError(f"{name}: contiguous int32 or int64 [rows][k] expected")
     if not t.is_cuda if like is None else t.get_device() != like.get_device():
         raise ValueError(f"{name}: a tensor on {'a CUDA device' if like is None else like.device} expected")
+    _fits(t.shape[1], name)
     return size
 
 
@@ -856,6 +866,7 @@ def _order(order, like, rows=None):
     M, k = places.shape
     if rows is not None and rows != M:
         raise ValueError(f"the order is of {M} tokens, the tensor has {rows} rows")
+    _fits(k, "order.places")
     i32, n = torch.int32, M * k
     return M, k, _vector(slots, "order.slots", like, n, i32), _vector(places, "order.places", like, n, i32)
 
@@ -870,6 +881,8 @@ def expert_sort(ids, n_experts, offsets=None, slots=None, places=None, stream=No
         with ctx:
             return expert_sort(ids, n_experts, offsets, slots, places)
     size = _ids(ids, "ids")
+    if not 0 < n_experts <= MAX_EXPERTS:                # before anything of that length is allocated
+        raise CcdcError(ESIZE if n_experts > 0 else EINVAL, "ccdc_expert_sort")
     M, k = ids.shape
     i32 = torch.int32
     if offsets is None:
@@ -1139,6 +1152,7 @@ def matmul_fp8(x, x_scales, w, w_scales, *, offsets=None, out_dtype=None, out=No
         experts, expert, po, want = 1, 0, None, ((N + 127) // 128, kb)
     else:
         experts, expert = sw[0], w.stride(0)
+        _fits(experts, "w")
         po = _vector(offsets, "offsets", x, experts + 1, torch.int32)
         want = experts, (N + 127) // 128, kb
         if experts > 1 and expert % 16:

@@ -1,4 +1,4 @@
-"""The sort by expert into given tensors, and its refusals."""
+"""The sort by expert into given tensors, its refusals, and counts beyond what the calls take."""
 import numpy as np
 import pytest
 
@@ -39,3 +39,17 @@ def test_refusals(ccdc):
         for t in bad:
             with pytest.raises(ValueError, match=name):
                 ccdc.expert_sort(ids, 4, **{name: t})
+    for n in (4097, 1 << 31, (1 << 32) + 4):            # also counts whose low 32 bits look like few experts
+        with pytest.raises(ccdc.CcdcError) as e:
+            ccdc.expert_sort(ids, n)
+        assert e.value.status == ccdc.ESIZE
+    for n in (0, -1, -4):
+        with pytest.raises(ccdc.CcdcError) as e:
+            ccdc.expert_sort(ids, n)
+        assert e.value.status == ccdc.EINVAL
+    # a stack of weights whose number's low 32 bits are 1
+    x, xs = ccdc.quantize_fp8(torch.ones((4, 128), device="cuda"))
+    w, ws = ccdc.quantize_fp8(torch.ones((1, 16, 128), device="cuda"), 128)
+    with pytest.raises(ccdc.CcdcError) as e:
+        ccdc.matmul_fp8(x, xs, w.expand((1 << 32) + 1, 16, 128), ws, offsets=empty(2))
+    assert e.value.status == ccdc.ESIZE
