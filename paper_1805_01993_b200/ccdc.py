@@ -558,7 +558,7 @@ def _elsewhere(x, stream):
         if stream.device != x.device:
             raise ValueError("the stream belongs to another device than the tensors")
         return torch.cuda.stream(stream)
-    if x.is_cuda and x.get_device() != torch._C._cuda_getDevice():
+    if x.is_cuda and x.get_device() != torch.cuda.current_device():
         return torch.cuda.device(x.device)
     return None
 
