@@ -656,7 +656,9 @@ int ccdc_distill(long long M, long long V, int k, int dtype, const void *logits,
  * Product: y[m][n] = sum_b xs[m][b] * ws[n / 128][b] * sum_{k in b} x[m][k] w[n][k].
  * x [M][K] with scales at x_scales[m*x_scale_row + b*x_scale_col]; w [experts][N][K]
  * (w_expert > 0 bytes apart, row stride ldw) with scales [experts][ceil(N/128)][ceil(K/128)]
- * contiguous; any binary32 scales whose products are finite.  y [M][N] in y_dtype.
+ * contiguous; any binary32 scales whose products xs * ws, which are rounded to
+ * binary32, are finite (below 2^-126 they lose bits, and with them the terms that
+ * they scale).  y [M][N] in y_dtype.
  * offsets NULL: one weight.  Else [experts + 1] on the device: rows offsets[e]
  * up to offsets[e + 1] take weight e (offsets[0] is taken as 0, entries beyond
  * M as M); rows behind the last are set to zero.
