@@ -838,10 +838,7 @@ class ExpertOrder(NamedTuple):
     places: object
 
 
-def _fits(n, where):
-    """raises unless a count fits the C call's 32-bit integer (ctypes would pass its low bits)."""
-    if n > 0x7FFFFFFF:
-        raise CcdcError(ESIZE, where)
+C_INT = 0x7FFFFFFF        # counts beyond it would reach a C call without their upper bits
 
 
 def _ids(t, name, like=None):
@@ -852,7 +849,8 @@ def _ids(t, name, like=None):
         raise ValueError(f"{name}: contiguous int32 or int64 [rows][k] expected")
     if not t.is_cuda if like is None else t.get_device() != like.get_device():
         raise ValueError(f"{name}: a tensor on {'a CUDA device' if like is None else like.device} expected")
-    _fits(t.shape[1], name)
+    if t.shape[1] > C_INT:
+        raise CcdcError(ESIZE, name)
     return size
 
 
@@ -866,7 +864,8 @@ def _order(order, like, rows=None):
     M, k = places.shape
     if rows is not None and rows != M:
         raise ValueError(f"the order is of {M} tokens, the tensor has {rows} rows")
-    _fits(k, "order.places")
+    if k > C_INT:
+        raise CcdcError(ESIZE, "order.places")
     i32, n = torch.int32, M * k
     return M, k, _vector(slots, "order.slots", like, n, i32), _vector(places, "order.places", like, n, i32)
 
@@ -1152,7 +1151,8 @@ def matmul_fp8(x, x_scales, w, w_scales, *, offsets=None, out_dtype=None, out=No
         experts, expert, po, want = 1, 0, None, ((N + 127) // 128, kb)
     else:
         experts, expert = sw[0], w.stride(0)
-        _fits(experts, "w")
+        if experts > C_INT:
+            raise CcdcError(ESIZE, "w")
         po = _vector(offsets, "offsets", x, experts + 1, torch.int32)
         want = experts, (N + 127) // 128, kb
         if experts > 1 and expert % 16:

@@ -3,7 +3,7 @@
 // A block of 128 elements of a row (activations) or of 128 x 128 (weights) is held as e4m3 values q and one binary32
 // scale: x ~ q * scale.  The scale made here is the least power of two that brings the block's largest magnitude to 448 at
 // most.  Quotients by it are exact, so every q has one value whichever way it is computed.  A finer scale would not change the
-// relative error of q's normal values, of which e4m3 has 2^15 to 1 in magnitude; what lies below them (under 2^-6 scale) has a fixed
+// relative error of q's normal values (2^-6 to 448); what lies below them (under 2^-6 scale) has a fixed
 // step, which a scale of up to twice the least possible one makes up to one bit coarser.
 #include "ccdc_block.h"
 #include "ccdc_fp8.h"
